@@ -591,6 +591,124 @@ int iefwd_decode_attention_noalloc(const void *q, const void *k, const void *vt,
                                    uint32_t n_heads, uint32_t n_keys, uint32_t head_dim, uint32_t k_rows,
                                    uint32_t vt_stride, void *stream);
 
+/* ---- token generation over a paged cache ------------------------------------------------
+ * A server that generates tokens for requests of different lengths keeps their
+ * keys and values in pages of a common pool, so that a request holds the memory of its
+ * own length, and its weights in 4 bits.  A step of it: iefwd_paged_plan (pages
+ * and slots of the new tokens), then per layer the QKV product (iefwd_q4_gemm
+ * or iefwd_test_gemm_skinny), iefwd_paged_append, iefwd_paged_attention and the
+ * other products.  Each call launches on `stream` (NULL = the null stream of
+ * the current device), on the device that is current, to which the stream and every buffer
+ * must belong, and returns without synchronising; it allocates nothing and may be
+ * captured into a graph.  The caller owns all buffers; they are device memory unless
+ * stated otherwise.  What does not fit is refused with EINVAL before anything
+ * is launched.  Results do not depend on the other requests of the batch. */
+
+#define IEFWD_KV_BF16  0u
+#define IEFWD_KV_E4M3  1u   /* 8-bit floating point (1-4-3 bits, largest value 448) with a scale per key-value head */
+
+/* A pool of pages.  With E = 16 / bytes per element (8 or 16), both 16-byte aligned:
+ *   k  [n_pages][n_kv_heads][head_dim / E][page_size][E]
+ *   v  [n_pages][n_kv_heads][page_size / 4][head_dim][4]
+ * i.e. K in 16-byte pieces of one token, V in pieces of 4 consecutive tokens of one
+ * column, the orders in which the attention's matrix operands read them.  A slot
+ * is page * page_size + place.  Places that no token was written to may hold any bits. */
+typedef struct iefwd_paged_cache {
+    uint32_t abi_version;   /* must be IEFWD_ABI_VERSION */
+    uint32_t kv_type;       /* IEFWD_KV_* */
+    uint32_t n_pages;       /* 1 .. 2^31 - 1 */
+    uint32_t page_size;     /* tokens: 16, 32, 64, 128 or 256 */
+    uint32_t n_kv_heads;    /* 1 .. 1024 */
+    uint32_t head_dim;      /* 64 or 128 */
+    void *k, *v;
+    const float *k_scale, *v_scale;   /* f32 [n_kv_heads], IEFWD_KV_E4M3 only: value = scale * stored */
+} iefwd_paged_cache;
+
+/* Brings every request b of a batch from lens[b] to new_lens[b] cached tokens
+ * (int32 [batch]): takes pages from the ring of free pages for those that grow,
+ * gives back those of requests that shrink (new_lens[b] = 0: the request has ended),
+ * and writes the slot of every new token.
+ *   table     int32 [batch, table_stride], max_pages columns used: request b's
+ *             pages in order; its first ceil(lens[b] / page_size) entries are read, the
+ *             new ones written, all others left as they were (an entry past a
+ *             request's last page means nothing)
+ *   ring      int32 [ring_size]: free pages, as a ring; ring_size = pages of the pool
+ *   counters  int64 [2] = {head, tail}: entries head .. tail - 1 (mod ring_size) of the ring
+ *             are the free pages.  Taken at the head, given back at the tail; pages given
+ *             back are free from the next call on.
+ *   lens_out  int32 [batch]: new_lens[b], or lens[b] where the request was refused
+ *   counters_out int64 [2]: the counters after the call
+ *   slots     int64 [max_new]: the new tokens' slots, requests in order, each
+ *             request's in order of position; -1 for those of refused requests
+ *             and behind the last
+ *   starts    int32 [batch + 1]: where each request's slots begin (at most max_new)
+ *   refused   int32 [1]: number of refused requests
+ * Requests are served in order.  One that needs pages is refused when the free
+ * pages do not suffice for it and all before it together, one with new tokens
+ * when its slots end past max_new, and one whose lengths lie outside [0, max_pages *
+ * page_size]; it keeps its length and pages.  lens_out must not be lens or new_lens and
+ * counters_out not counters (they swap roles from call to call); a call on
+ * the same inputs again gives the same outputs.  A page in the table belongs to one
+ * request.  1 <= batch <= 4096; page_size as above; max_pages * page_size <= 2^30;
+ * max_new <= 2^31 - 1 (0: slots may be NULL); ring_size 1 .. 2^31 - 1. */
+int iefwd_paged_plan(uint32_t batch, uint32_t page_size, const int32_t *lens, const int32_t *new_lens, int32_t *table,
+                     uint32_t table_stride, uint32_t max_pages, int32_t *ring, uint32_t ring_size,
+                     const int64_t *counters, int32_t *lens_out, int64_t *counters_out, int64_t *slots,
+                     uint32_t max_new, int32_t *starts, int32_t *refused, void *stream);
+
+/* Writes n_tokens new tokens' keys and values to their slots: k and v bf16
+ * [n_tokens][n_kv_heads * head_dim], rows k_stride and v_stride elements apart
+ * (multiples of 8 and at least a row; 16-byte aligned), slots int64 [n_tokens] as from
+ * iefwd_paged_plan.  A token whose slot lies outside the pool is skipped.  No
+ * two tokens may have the same slot.  IEFWD_KV_E4M3: x / scale rounded to the nearest
+ * (ties to even), values beyond +-448 stored as +-448, NaN as NaN.
+ * n_tokens = 0 does nothing. */
+int iefwd_paged_append(const iefwd_paged_cache *cache, const void *k, const void *v, const int64_t *slots,
+                       uint32_t n_tokens, uint64_t k_stride, uint64_t v_stride, void *stream);
+
+/* Bytes of workspace that iefwd_paged_attention needs for a batch and a table of
+ * max_pages columns (0 where no request can be long enough to be split). Host only. */
+int iefwd_paged_attention_workspace(const iefwd_paged_cache *cache, uint32_t batch, uint32_t n_heads,
+                                    uint32_t max_pages, size_t *bytes);
+
+/* ctx bf16 [batch][n_heads * head_dim]: request b's row is, per head h,
+ * sum_j p_j v_j with p = softmax_j(scale * q . k_j) over its cached tokens j < lens[b], k
+ * and v those of key-value head h / (n_heads / n_kv_heads).  q bf16
+ * [batch][n_heads * head_dim], rows q_stride elements apart (as k_stride above);
+ * table int32 [batch, table_stride], max_pages columns used; lens int32 [batch].
+ * Lengths are cut to [0, max_pages * page_size]; a page id outside the pool drops
+ * its tokens; a row with nothing to attend to becomes zeros.  fp32 scores, softmax and
+ * sums; the probabilities enter the product with V in 16 bits.
+ * The keys of a long request are split and joined by a rule on its length and
+ * the head counts alone.  workspace: iefwd_paged_attention_workspace bytes, 16-byte aligned,
+ * any contents; calls that may overlap need one each.  n_heads a multiple of
+ * n_kv_heads, at most 1024; 1 <= batch <= 65535; max_pages >= 1 and
+ * max_pages * page_size <= 2^30; scale finite. */
+int iefwd_paged_attention(const iefwd_paged_cache *cache, const void *q, uint64_t q_stride, uint32_t n_heads,
+                          const int32_t *table, uint32_t table_stride, uint32_t max_pages, const int32_t *lens,
+                          uint32_t batch, float scale, void *ctx, void *workspace, size_t workspace_bytes,
+                          void *stream);
+
+/* The 4-bit form of a weight matrix W [N, K]: W[n][k] = scales[n][g] *
+ * (code[n][k] - zeros[n][g]), g = k / group.  codes uint8 [N, K / 2], weight 2 i in the
+ * low and 2 i + 1 in the high half of byte i; scales bf16 [N, K / group]; zeros
+ * uint8 [N, K / group] in 0 .. 15, or NULL for 8 everywhere.  iefwd_q4_pack lays it
+ * out once for iefwd_q4_gemm into dst (iefwd_q4_packed_bytes bytes, 16-byte aligned): blocks of
+ * 1 KB, one wave load each, with the codes of 16 features x 128 weights, then a
+ * 4-byte {scale, 16 + zero} per group.  group 32, 64 or 128; N a positive
+ * multiple of 16, K of 32 and of group; N * K < 2^31. */
+int iefwd_q4_packed_bytes(uint32_t N, uint32_t K, uint32_t group, size_t *bytes);   /* host only */
+int iefwd_q4_pack(const void *codes, const void *scales, const void *zeros, void *dst, uint32_t N, uint32_t K,
+                  uint32_t group, void *stream);
+
+/* The decode-step product with 4-bit weights: out = epilogue(A W^T + b) for
+ * M <= 16 rows, epilogues IEFWD_EPI_BIAS_BF16, _BIAS_GELU_BF16 and
+ * _BIAS_RESID_F32 and operands as for iefwd_test_gemm_skinny (a 16-byte aligned; bias may be
+ * NULL: none), packed from iefwd_q4_pack.  fp32 sums; out may be resid.  A row's
+ * result depends neither on the other rows nor on M. */
+int iefwd_q4_gemm(uint32_t epilogue, const void *a, const void *packed, const void *bias, const float *resid, void *out,
+                  uint32_t M, uint32_t N, uint32_t K, uint32_t group, void *stream);
+
 /* CU residency probe: launches n_groups workgroups of 64 threads on `stream`;
  * workgroup g writes out[2g] = XCC id, out[2g+1] = the hardware id register
  * (CU, SIMD, shader-array and shader-engine fields).  out: device uint32

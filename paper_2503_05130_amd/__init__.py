@@ -25,6 +25,7 @@ OK, EINVAL, ENODEV, ENOMEM, EHIP, ESTATE, EVERSION = 0, -1, -2, -3, -4, -5, -6
 K_QKV, K_ATTN, K_OUTPROJ, K_FFN1, K_FFN2, K_LN, K_BWD_GEMM, K_BWD, K_OPTIM = range(9)
 TRAIN_MASTER, TRAIN_GRAD, TRAIN_MOMENT1, TRAIN_MOMENT2 = range(4)
 EPI_BIAS_BF16, EPI_BIAS_GELU_BF16, EPI_BIAS_RESID_F32 = 0, 1, 2
+KV_BF16, KV_E4M3 = 0, 1
 EPI_LN_RESID_F32, EPI_F32, EPI_GELU_BWD_BF16, EPI_GELU2_BF16 = 4, 5, 6, 7
 
 _u32, _u64, _i32, _f32, _vp, _sz = (ctypes.c_uint32, ctypes.c_uint64, ctypes.c_int, ctypes.c_float,
@@ -89,6 +90,13 @@ SIGNATURES = {
     "iefwd_test_ln_head": (_i32, [_vp, _vp, _vp, _vp, _vp, _vp, _u32, _u32, _u32, _f32, _vp]),
     "iefwd_test_cu_probe": (_i32, [_vp, _u32, _vp]),
     "iefwd_test_decode_attention": (_i32, [_vp, _vp, _vp, _vp, _u32, _u32, _u32, _u32, _u32, _u32, _vp]),
+    "iefwd_paged_plan": (_i32, [_u32, _u32, _vp, _vp, _vp, _u32, _u32, _vp, _u32, _vp, _vp, _vp, _vp, _u32, _vp, _vp, _vp]),
+    "iefwd_paged_append": (_i32, [_vp, _vp, _vp, _vp, _u32, _u64, _u64, _vp]),
+    "iefwd_paged_attention_workspace": (_i32, [_vp, _u32, _u32, _u32, ctypes.POINTER(_sz)]),
+    "iefwd_paged_attention": (_i32, [_vp, _vp, _u64, _u32, _vp, _u32, _u32, _vp, _u32, _f32, _vp, _vp, _sz, _vp]),
+    "iefwd_q4_packed_bytes": (_i32, [_u32, _u32, _u32, ctypes.POINTER(_sz)]),
+    "iefwd_q4_pack": (_i32, [_vp, _vp, _vp, _vp, _u32, _u32, _u32, _vp]),
+    "iefwd_q4_gemm": (_i32, [_u32, _vp, _vp, _vp, _vp, _vp, _u32, _u32, _u32, _u32, _vp]),
     "iefwd_decode_attention_noalloc": (_i32, [_vp, _vp, _vp, _vp, _u32, _u32, _u32, _u32, _u32, _u32, _vp]),
 }
 
@@ -442,6 +450,181 @@ def decode_attention_noalloc(q, k, vt, ctx, batch, n_heads, n_keys, head_dim, k_
 
 def test_cu_probe(n_groups: int, out, stream=None) -> None:
     _check(lib().iefwd_test_cu_probe(_stream(stream), n_groups, _ptr(out)), "iefwd_test_cu_probe")
+
+
+# ------------------------------------------------------------------ token generation over a paged cache
+class PagedCacheDesc(ctypes.Structure):
+    """Mirror of ``iefwd_paged_cache``."""
+    _fields_ = [("abi_version", _u32), ("kv_type", _u32), ("n_pages", _u32), ("page_size", _u32), ("n_kv_heads", _u32),
+                ("head_dim", _u32), ("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp)]
+
+
+def _tensor(name: str, t, dtype, device=None, shape=None):
+    """The checks of a tensor operand: type, place, and (with `shape`) that and that it is contiguous."""
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or not t.is_cuda:
+        raise ValueError(f"{name} must be a {dtype} tensor on the GPU")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
+    if shape is not None and (tuple(t.shape) != tuple(shape) or not t.is_contiguous()):
+        raise ValueError(f"{name} must be contiguous with shape {tuple(shape)}")
+    return t
+
+
+def _rows(name: str, t, device, rows: int, heads: int, head_dim: int) -> int:
+    """Checks rows of heads (bf16 [rows, heads, head_dim], or the last two as one) that may be
+    slices of wider rows; returns their stride in elements."""
+    _tensor(name, t, torch.bfloat16, device)
+    if t.shape == (rows, heads, head_dim):
+        flat = t.stride(2) == 1 and (heads == 1 or t.stride(1) == head_dim)
+    else:
+        flat = t.shape == (rows, heads * head_dim) and t.stride(1) == 1
+    if not flat:
+        raise ValueError(f"{name} must be [{rows}, {heads}, {head_dim}] with each row contiguous")
+    return t.stride(0) if rows > 1 else heads * head_dim
+
+
+def _call(device: torch.device, stream, name: str, *args) -> None:
+    """Calls a library function with `device` current, on `stream` or else torch's current stream of it."""
+    handle = torch.cuda.current_stream(device).cuda_stream if stream is None else _stream(stream)
+    if torch.cuda.current_device() == device.index:
+        _check(getattr(lib(), name)(*args, handle), name)
+    else:
+        with torch.cuda.device(device):
+            _check(getattr(lib(), name)(*args, handle), name)
+
+
+class PagedCache:
+    """A pool of pages of keys and values (``iefwd_paged_cache``) in the caller's tensors:
+    k [n_pages, n_kv_heads, head_dim // E, page_size, E] and v [n_pages, n_kv_heads, page_size // 4,
+    head_dim, 4], bfloat16 (E = 8) or float8_e4m3fn (E = 16; then with fp32 k_scale and v_scale
+    [n_kv_heads]).  ``PagedCache.empty`` makes them."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        e4m3 = isinstance(k, torch.Tensor) and k.dtype == torch.float8_e4m3fn
+        dtype, e = (torch.float8_e4m3fn, 16) if e4m3 else (torch.bfloat16, 8)
+        _tensor("k", k, dtype)
+        if k.dim() != 5 or k.shape[4] != e:
+            raise ValueError(f"k must be [n_pages, n_kv_heads, head_dim // {e}, page_size, {e}]")
+        n_pages, heads, pieces, page, _ = k.shape
+        self.device, self.page_size, self.n_kv_heads, self.head_dim = k.device, page, heads, pieces * e
+        _tensor("k", k, dtype, shape=k.shape)
+        _tensor("v", v, dtype, self.device, (n_pages, heads, page // 4, self.head_dim, 4))
+        if e4m3:
+            _tensor("k_scale", k_scale, torch.float32, self.device, (heads,))
+            _tensor("v_scale", v_scale, torch.float32, self.device, (heads,))
+        elif k_scale is not None or v_scale is not None:
+            raise ValueError("scales belong to a float8_e4m3fn cache")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.desc = PagedCacheDesc(ABI_VERSION, KV_E4M3 if e4m3 else KV_BF16, n_pages, page, heads, self.head_dim, _ptr(k),
+                                   _ptr(v), _ptr(k_scale), _ptr(v_scale))
+        self._ref = ctypes.byref(self.desc)
+
+    @classmethod
+    def empty(cls, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, k_scale=None, v_scale=None,
+              device="cuda:0") -> "PagedCache":
+        """A pool in new, unset memory; 8-bit if scales are given."""
+        dtype, e = (torch.bfloat16, 8) if k_scale is None else (torch.float8_e4m3fn, 16)
+        return cls(torch.empty((n_pages, n_kv_heads, head_dim // e, page_size, e), dtype=dtype, device=device),
+                   torch.empty((n_pages, n_kv_heads, page_size // 4, head_dim, 4), dtype=dtype, device=device), k_scale,
+                   v_scale)
+
+    def append(self, k, v, slots, stream=None) -> None:
+        """Writes new tokens' keys and values, bf16 [tokens, n_kv_heads, head_dim] (rows may lie apart), to
+        their slots (int64 [tokens], from ``paged_plan``; outside the pool: skipped)."""
+        n = _tensor("slots", slots, torch.int64, self.device).numel()
+        _tensor("slots", slots, torch.int64, self.device, (n,))
+        ks = _rows("k", k, self.device, n, self.n_kv_heads, self.head_dim)
+        vs = _rows("v", v, self.device, n, self.n_kv_heads, self.head_dim)
+        _call(self.device, stream, "iefwd_paged_append", self._ref, k.data_ptr(), v.data_ptr(), slots.data_ptr(), n, ks, vs)
+
+    def workspace(self, batch: int, n_heads: int, max_pages: int) -> torch.Tensor:
+        """A workspace for ``attention`` on a batch and a table of max_pages columns."""
+        n = _sz()
+        _check(lib().iefwd_paged_attention_workspace(self._ref, batch, n_heads, max_pages, ctypes.byref(n)),
+               "iefwd_paged_attention_workspace")
+        return torch.empty(n.value, dtype=torch.uint8, device=self.device)
+
+    def attention(self, q, table, lens, out, workspace, scale: float | None = None, stream=None) -> None:
+        """out bf16 [batch, n_heads, head_dim] = attention of one query per request and head, q of that
+        shape (rows may lie apart), over the pages in `table` (int32 [batch, max_pages], rows may lie apart) of
+        lens (int32 [batch]) cached tokens.  scale: 1 / sqrt(head_dim) by default."""
+        batch, d = _tensor("lens", lens, torch.int32, self.device).numel(), self.head_dim
+        _tensor("lens", lens, torch.int32, self.device, (batch,))
+        _tensor("table", table, torch.int32, self.device)
+        if table.dim() != 2 or table.shape[0] != batch or (table.shape[1] > 1 and table.stride(1) != 1):
+            raise ValueError("table must be [batch, max_pages] with each row contiguous")
+        _tensor("out", out, torch.bfloat16, self.device)
+        heads = out.numel() // (batch * d) if batch else 0
+        if out.shape not in ((batch, heads, d), (batch, heads * d)) or not out.is_contiguous():
+            raise ValueError("out must be contiguous, [batch, n_heads, head_dim]")
+        qs = _rows("q", q, self.device, batch, heads, d)
+        _tensor("workspace", workspace, torch.uint8, self.device)
+        if not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous")
+        cols = table.shape[1]
+        _call(self.device, stream, "iefwd_paged_attention", self._ref, q.data_ptr(), qs, heads, table.data_ptr(),
+              table.stride(0) if batch > 1 else cols, cols, lens.data_ptr(), batch, d ** -0.5 if scale is None else scale,
+              out.data_ptr(), workspace.data_ptr(), workspace.numel())
+
+
+def paged_plan(page_size: int, lens, new_lens, table, ring, counters, lens_out, counters_out, slots, starts, refused,
+               stream=None) -> None:
+    """Pages and slots of a step (``iefwd_paged_plan``): requests of lens cached tokens come to new_lens ones.
+    int32 lens, new_lens, lens_out [batch], table [batch, max_pages] (rows may lie apart), ring [pages of the pool],
+    starts [batch + 1], refused [1]; int64 counters, counters_out [2], slots [most new tokens]."""
+    n = _tensor("lens", lens, torch.int32).numel()
+    dev, n_pages = lens.device, _tensor("ring", ring, torch.int32).numel()
+    room = _tensor("slots", slots, torch.int64).numel()
+    for name, t, dtype, shape in (("lens", lens, torch.int32, (n,)), ("new_lens", new_lens, torch.int32, (n,)),
+                                  ("lens_out", lens_out, torch.int32, (n,)), ("ring", ring, torch.int32, (n_pages,)),
+                                  ("counters", counters, torch.int64, (2,)), ("counters_out", counters_out, torch.int64, (2,)),
+                                  ("slots", slots, torch.int64, (room,)), ("starts", starts, torch.int32, (n + 1,)),
+                                  ("refused", refused, torch.int32, (1,))):
+        _tensor(name, t, dtype, dev, shape)
+    _tensor("table", table, torch.int32, dev)
+    if table.dim() != 2 or table.shape[0] != n or (table.shape[1] > 1 and table.stride(1) != 1):
+        raise ValueError("table must be [batch, max_pages] with each row contiguous")
+    cols = table.shape[1]
+    _call(dev, stream, "iefwd_paged_plan", n, page_size, lens.data_ptr(), new_lens.data_ptr(), table.data_ptr(),
+          table.stride(0) if n > 1 else cols, cols, ring.data_ptr(), n_pages, counters.data_ptr(), lens_out.data_ptr(),
+          counters_out.data_ptr(), slots.data_ptr(), room, starts.data_ptr(), refused.data_ptr())
+
+
+class Q4Weight:
+    """A weight matrix [N, K] in 4 bits, laid out for ``product`` once: codes uint8 [N, K / 2] (weight 2 i in
+    the low half of byte i), scales bf16 [N, K / group], zeros uint8 [N, K / group] or None (8 everywhere);
+    W = scales (codes - zeros).  The tensors given are not kept."""
+
+    def __init__(self, codes, scales, zeros=None, stream=None):
+        _tensor("codes", codes, torch.uint8)
+        if codes.dim() != 2 or not isinstance(scales, torch.Tensor) or scales.dim() != 2 or not scales.shape[1]:
+            raise ValueError("codes must be [N, K / 2] and scales [N, K / group]")
+        self.device, self.N, self.K = codes.device, codes.shape[0], 2 * codes.shape[1]
+        self.group = self.K // scales.shape[1]
+        shape = (self.N, self.K // self.group if self.group else 0)
+        _tensor("codes", codes, torch.uint8, shape=codes.shape)
+        _tensor("scales", scales, torch.bfloat16, self.device, shape)
+        if zeros is not None:
+            _tensor("zeros", zeros, torch.uint8, self.device, shape)
+        n = _sz()
+        _check(lib().iefwd_q4_packed_bytes(self.N, self.K, self.group, ctypes.byref(n)), "iefwd_q4_packed_bytes")
+        self.packed = torch.empty(n.value, dtype=torch.uint8, device=self.device)
+        _call(self.device, stream, "iefwd_q4_pack", codes.data_ptr(), scales.data_ptr(), _ptr(zeros), self.packed.data_ptr(), self.N,
+              self.K, self.group)
+
+    def product(self, a, out, epilogue: int = EPI_BIAS_BF16, bias=None, resid=None, stream=None) -> None:
+        """out [M, N] = epilogue(a W^T + bias), a bf16 [M, K], M <= 16; out bf16, or fp32 (as resid) for
+        EPI_BIAS_RESID_F32; bias bf16 [N] or None."""
+        m = _tensor("a", a, torch.bfloat16, self.device).numel() // self.K
+        _tensor("a", a, torch.bfloat16, self.device, (m, self.K))
+        f32 = epilogue == EPI_BIAS_RESID_F32
+        _tensor("out", out, torch.float32 if f32 else torch.bfloat16, self.device, (m, self.N))
+        if bias is not None:
+            _tensor("bias", bias, torch.bfloat16, self.device, (self.N,))
+        if f32:
+            _tensor("resid", resid, torch.float32, self.device, (m, self.N))
+        _call(self.device, stream, "iefwd_q4_gemm", epilogue, a.data_ptr(), self.packed.data_ptr(), _ptr(bias),
+              _ptr(resid) if f32 else None, out.data_ptr(), m, self.N, self.K, self.group)
 
 
 # ------------------------------------------------------------------ quota controller

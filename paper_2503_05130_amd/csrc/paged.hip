@@ -1,0 +1,601 @@
+// The paged key-value cache's kernels for gfx950: planning of pages and slots,
+// appending new tokens, and attention of one query per request over pages.
+#include "paged.h"
+
+#include <algorithm>
+
+#include "gemm_device.h"
+#include "paged_split.h"
+
+namespace iefwd {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+
+// ------------------------------------------------------------------------------ plan
+//
+// For request b with o cached and n wanted tokens in pages of P: it holds
+// ceil(o / P) pages and needs ceil(n / P).  Every workgroup makes the same
+// prefix sums over the batch (new tokens, pages taken, pages given back) from
+// the lengths, which it reads from L2; they say where each request's slots begin and
+// which entries of the ring of free pages are its own.  The slots are then
+// spread over the workgroups whatever request they belong to (a binary search
+// in the sums finds it), so that one long prompt is as parallel as many short
+// ones; the slot that opens a page also writes the table's entry.  One launch, no
+// scratch, no atomics: what one workgroup writes none reads.
+constexpr int kPlanSlots = 1024;   // slots a workgroup makes per round
+
+struct PlanSums {
+    int64_t tokens, taken, given;
+};
+
+__device__ inline PlanSums operator+(PlanSums a, PlanSums b) {
+    return {a.tokens + b.tokens, a.taken + b.taken, a.given + b.given};
+}
+
+__device__ inline PlanSums shift_up(PlanSums a, int by) {
+    return {__shfl_up(a.tokens, by), __shfl_up(a.taken, by), __shfl_up(a.given, by)};
+}
+
+struct PlanRequest {
+    int held, want, tokens;
+    bool valid;
+};
+
+__device__ inline PlanRequest plan_request(const PlanArgs &p, int b) {
+    const int o = p.lens[b], n = p.new_lens[b];
+    const int64_t cap = (int64_t)p.max_pages << p.page_log2;
+    PlanRequest r{0, 0, 0, o >= 0 && n >= 0 && o <= cap && n <= cap};
+    if (r.valid) {
+        const int up = (1 << p.page_log2) - 1;
+        r.held = (int)(((int64_t)o + up) >> p.page_log2);
+        r.want = (int)(((int64_t)n + up) >> p.page_log2);
+        r.tokens = n > o ? n - o : 0;
+    }
+    return r;
+}
+
+__global__ __launch_bounds__(kThreads) void paged_plan_kernel(PlanArgs p) {
+    __shared__ int ends[kPlanMaxBatch];      // new tokens up to and with request b, at most room
+    __shared__ int at[kPlanMaxBatch];        // the request's first entry of the ring (taken from or given to), -1: refused
+    __shared__ PlanSums wave_sum[kWaves];
+    __shared__ int granted_total[2], refused_total;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t head = p.counters[0], tail = p.counters[1];
+    const bool sane = head >= 0 && tail >= head && tail - head <= p.ring_size;
+    const int64_t avail = sane ? tail - head : 0, space = sane ? p.ring_size - avail : 0;
+    const int head_at = sane ? (int)(head % p.ring_size) : 0, tail_at = sane ? (int)(tail % p.ring_size) : 0;
+
+    // each thread sums a run of requests, then the runs are scanned
+    const int run = (p.batch + kThreads - 1) / kThreads;
+    const int first = min(tid * run, p.batch), last = min(first + run, p.batch);
+    PlanSums mine{0, 0, 0};
+    for (int b = first; b < last; ++b) {
+        const PlanRequest r = plan_request(p, b);
+        mine = mine + PlanSums{r.tokens, max(0, r.want - r.held), max(0, r.held - r.want)};
+    }
+    PlanSums incl = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const PlanSums below = shift_up(incl, o);
+        if (lane >= o) incl = incl + below;
+    }
+    if (lane == 63) wave_sum[wave] = incl;
+    if (tid < 2) granted_total[tid] = 0;
+    if (tid == 2) refused_total = 0;
+    __syncthreads();
+    PlanSums sum{incl.tokens - mine.tokens, incl.taken - mine.taken, incl.given - mine.given};
+    for (int w = 0; w < wave; ++w) sum = sum + wave_sum[w];
+    int taken = 0, given = 0, refused = 0;
+    for (int b = first; b < last; ++b) {
+        const PlanRequest r = plan_request(p, b);
+        const int take = max(0, r.want - r.held), give = max(0, r.held - r.want);
+        const PlanSums to = sum + PlanSums{r.tokens, take, give};
+        const bool ok = r.valid && (take == 0 || to.taken <= avail) && (r.tokens == 0 || to.tokens <= p.room) &&
+                        (give == 0 || to.given <= space);
+        ends[b] = (int)min(to.tokens, (int64_t)p.room);
+        // a granted request's sums are at most the ring's size
+        const int64_t place = !ok ? -1 : give ? tail_at + sum.given : take ? head_at + sum.taken : 0;
+        at[b] = (int)(place >= p.ring_size ? place - p.ring_size : place);
+        taken += ok ? take : 0;
+        given += ok ? give : 0;
+        refused += !ok;
+        if (blockIdx.x == 0) {
+            p.lens_out[b] = ok ? p.new_lens[b] : p.lens[b];
+            p.starts[b] = (int)min(sum.tokens, (int64_t)p.room);
+            if (b == p.batch - 1) p.starts[p.batch] = ends[b];
+        }
+        sum = to;
+    }
+    if (taken) atomicAdd(&granted_total[0], taken);     // whole numbers in LDS: any order gives the same
+    if (given) atomicAdd(&granted_total[1], given);
+    if (refused) atomicAdd(&refused_total, refused);
+    __syncthreads();
+    if (blockIdx.x == 0 && tid == 0) {
+        p.counters_out[0] = head + granted_total[0];
+        p.counters_out[1] = tail + granted_total[1];
+        *p.refused = refused_total;
+    }
+
+    // slots and the table's new entries
+    const int page = 1 << p.page_log2;
+    const int total = p.batch ? ends[p.batch - 1] : 0;
+    for (int64_t i0 = (int64_t)blockIdx.x * kPlanSlots; i0 < p.room; i0 += (int64_t)gridDim.x * kPlanSlots) {
+        for (int j = tid; j < kPlanSlots; j += kThreads) {
+            const int64_t i = i0 + j;
+            if (i >= p.room) break;
+            int64_t slot = -1;
+            if (i < total) {
+                int lo = 0, hi = p.batch - 1;            // the first request whose tokens end past i
+                while (lo < hi) {
+                    const int mid = (lo + hi) >> 1;
+                    if (ends[mid] > i) hi = mid;
+                    else lo = mid + 1;
+                }
+                if (at[lo] >= 0) {
+                    const int o = p.lens[lo];
+                    const int pos = o + (int)(i - (lo ? ends[lo - 1] : 0));
+                    const int held = (int)(((int64_t)o + page - 1) >> p.page_log2);
+                    const int column = pos >> p.page_log2;
+                    int32_t *entry = p.table + (int64_t)lo * p.table_stride + column;
+                    int32_t id;
+                    if (column < held) {
+                        id = *entry;
+                    } else {
+                        int64_t place = (int64_t)at[lo] + column - held;
+                        id = p.ring[place >= p.ring_size ? place - p.ring_size : place];
+                        if ((pos & (page - 1)) == 0) *entry = id;
+                    }
+                    if (id >= 0 && id < p.ring_size) slot = ((int64_t)id << p.page_log2) + (pos & (page - 1));
+                }
+            }
+            p.slots[i] = slot;
+        }
+    }
+    // pages given back, a wave a request
+    for (int b = blockIdx.x * kWaves + wave; b < p.batch; b += gridDim.x * kWaves) {
+        const PlanRequest r = plan_request(p, b);
+        if (r.want >= r.held || at[b] < 0) continue;
+        for (int c = r.want + lane; c < r.held; c += 64) {
+            const int64_t place = (int64_t)at[b] + c - r.want;
+            p.ring[place >= p.ring_size ? place - p.ring_size : place] = p.table[(int64_t)b * p.table_stride + c];
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------ append
+
+__device__ inline float to_e4m3_range(float x, float scale) {
+    const float y = x / scale;
+    return y != y ? y : fminf(fmaxf(y, -448.f), 448.f);
+}
+
+// One thread: 8 columns of one token and head.
+template <bool E4M3>
+__global__ __launch_bounds__(kThreads) void paged_append_kernel(PagedCache c, const bf16_t *__restrict__ k,
+                                                                const bf16_t *__restrict__ v,
+                                                                const int64_t *__restrict__ slots, int tokens,
+                                                                int64_t k_stride, int64_t v_stride) {
+    const int per_head = c.head_dim / 8, per_token = c.kv_heads * per_head;
+    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (i >= (int64_t)tokens * per_token) return;
+    const int64_t t = i / per_token;
+    const int part = (int)(i - t * per_token), head = part / per_head, d = (part - head * per_head) * 8;
+    const int64_t slot = slots[t];
+    if (slot < 0 || slot >= ((int64_t)c.n_pages << c.page_log2)) return;
+    const int page = 1 << c.page_log2, place = (int)(slot & (page - 1));
+    const u32x4 kw = *reinterpret_cast<const u32x4 *>(k + t * k_stride + part * 8);
+    const u32x4 vw = *reinterpret_cast<const u32x4 *>(v + t * v_stride + part * 8);
+    const size_t base = ((size_t)(slot >> c.page_log2) * c.kv_heads + head) * page * c.head_dim;
+    if constexpr (!E4M3) {
+        bf16_t *kp = static_cast<bf16_t *>(c.k) + base + ((size_t)(d / 8) * page + place) * 8;
+        *reinterpret_cast<u32x4 *>(kp) = kw;
+        bf16_t *vp = static_cast<bf16_t *>(c.v) + base + ((size_t)(place / 4) * c.head_dim + d) * 4 + place % 4;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) vp[4 * e] = (bf16_t)(vw[e / 2] >> (16 * (e % 2)));
+    } else {
+        const float ks = c.k_scale[head], vs = c.v_scale[head];
+        uint32_t kq[2], vq[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float a[4], b[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t x = kw[2 * h + e / 2], y = vw[2 * h + e / 2];
+                a[e] = to_e4m3_range(__uint_as_float(e % 2 ? x & 0xffff0000u : x << 16), ks);
+                b[e] = to_e4m3_range(__uint_as_float(e % 2 ? y & 0xffff0000u : y << 16), vs);
+            }
+            int w = __builtin_amdgcn_cvt_pk_fp8_f32(a[0], a[1], 0, false);
+            kq[h] = __builtin_amdgcn_cvt_pk_fp8_f32(a[2], a[3], w, true);
+            w = __builtin_amdgcn_cvt_pk_fp8_f32(b[0], b[1], 0, false);
+            vq[h] = __builtin_amdgcn_cvt_pk_fp8_f32(b[2], b[3], w, true);
+        }
+        uint8_t *kp = static_cast<uint8_t *>(c.k) + base + ((size_t)(d / 16) * page + place) * 16 + d % 16;
+        *reinterpret_cast<u32x2 *>(kp) = u32x2{kq[0], kq[1]};
+        uint8_t *vp = static_cast<uint8_t *>(c.v) + base + ((size_t)(place / 4) * c.head_dim + d) * 4 + place % 4;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) vp[4 * e] = (uint8_t)(vq[e / 4] >> (8 * (e % 4)));
+    }
+}
+
+// ------------------------------------------------------------------------------ attention
+//
+// One query per request and head, ctx = sum_j softmax_j(scale q . k_j) v_j over
+// the request's pages.  A workgroup takes one part of one request's keys for one
+// key-value head and up to 16 of its query heads; its 4 waves take steps
+// of 32 keys in turn, each with its own running maximum, sum and context, and
+// join them through LDS.  A request of several parts is joined by a second kernel.
+//
+// Both products run on the matrix cores with the query heads as columns:
+// S^T = K Q^T (rows: keys), O^T = V^T P^T (rows: columns of V).  A lane then
+// holds the scores of one head and of the keys 4 c .. 4 c + 3 of two tiles of 16
+// (c = lane / 16), which is just what the second product wants from it as its
+// operand, so the probabilities never leave the lane's registers; the
+// pages are laid out so that K's and V's operands are 16-byte loads in the
+// same sense.  P goes in as two bf16 numbers, the rounded value and the rounded
+// rest, which keeps 16 bits of it for two products where there is ample room.
+struct AttnArgs {
+    PagedCache c;
+    const bf16_t *q;
+    int64_t q_stride;
+    const int32_t *table;
+    const int32_t *lens;
+    bf16_t *ctx;
+    float *part_o;       // [batch, heads, slots, head_dim]
+    float *part_ml;      // [batch, heads, slots, 2]
+    int table_stride, batch, heads, max_keys, max_parts, slots;
+    float scale_log2e;
+};
+
+__device__ inline int wave_scan(int v) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int below = __shfl_up(v, o);
+        if (lane >= o) v += below;
+    }
+    return v;
+}
+
+__device__ inline int part_count(int n, int max_parts) { return max(1, paged_parts(n, max_parts)); }
+
+struct AttnItem {
+    int b, part, keys;
+};
+
+// The item-th (request, part) of the batch, requests in order; false past the last.
+// Every wave finds it by itself from the lengths, 64 requests at a time.
+__device__ inline bool find_item(const AttnArgs &a, int item, int &b0, int &before, AttnItem &out) {
+    const int lane = threadIdx.x & 63;
+    for (; b0 < a.batch; b0 += 64) {
+        const bool in = b0 + lane < a.batch;
+        const int n = in ? min(max(a.lens[b0 + lane], 0), a.max_keys) : 0;
+        const int parts = in ? part_count(n, a.max_parts) : 0;
+        const int to = before + wave_scan(parts);
+        const int total = __builtin_amdgcn_readlane(to, 63);
+        if (item < total) {
+            const int src = __builtin_ctzll(__ballot(to > item));
+            out.b = b0 + src;
+            out.part = item - (__builtin_amdgcn_readlane(to, src) - __builtin_amdgcn_readlane(parts, src));
+            out.keys = __builtin_amdgcn_readlane(n, src);
+            return true;
+        }
+        before = total;
+    }
+    return false;
+}
+
+__device__ inline float across_rows_max(float v) {
+    v = fmaxf(v, __shfl_xor(v, 16));
+    return fmaxf(v, __shfl_xor(v, 32));
+}
+
+__device__ inline float across_rows_sum(float v) {
+    v += __shfl_xor(v, 16);
+    return v + __shfl_xor(v, 32);
+}
+
+// four e4m3 values as four bf16 (exact)
+__device__ inline u32x2 widen(uint32_t w) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false);
+    const bf16x2 hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true);
+    return u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+}
+
+__device__ inline bf16x8 operand(u32x2 a, u32x2 b) { return __builtin_bit_cast(bf16x8, u32x4{a[0], a[1], b[0], b[1]}); }
+
+template <int DH, bool E4M3>
+__global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttnArgs a) {
+    constexpr int ES = E4M3 ? 1 : 2;             // bytes per element
+    constexpr int NK = DH * ES / 64;             // 16-byte loads per lane and key tile: DH columns of 16 keys
+    constexpr int W = E4M3 ? 4 : 2;              // columns of V in a 16-byte load
+    constexpr int NV = DH / (16 * W);            // such loads per key tile
+    constexpr int ROW = DH + 4;
+    __shared__ __attribute__((aligned(16))) float o_lds[kWaves][16][ROW];
+    __shared__ float m_lds[kWaves][16], l_lds[kWaves][16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int r = lane & 15, c = lane >> 4;
+    const int group = a.heads / a.c.kv_heads, tiles = (group + 15) / 16;
+    const int kvh = blockIdx.y / tiles, tile = blockIdx.y - kvh * tiles;
+    const int head0 = kvh * group + tile * 16, n_heads = min(16, group - tile * 16);
+    const int page = 1 << a.c.page_log2;
+    const size_t page_bytes = (size_t)page * DH * ES;
+    const char *K = static_cast<const char *>(a.c.k), *V = static_cast<const char *>(a.c.v);
+    const float scale = E4M3 ? a.scale_log2e * a.c.k_scale[kvh] : a.scale_log2e;
+    const float v_scale = E4M3 ? a.c.v_scale[kvh] : 1.f;
+
+    int b0 = 0, before = 0;
+    AttnItem it;
+    for (int item = blockIdx.x; find_item(a, item, b0, before, it); item += gridDim.x) {
+        const int part_keys = paged_part_keys(it.keys, a.max_parts);
+        const int k0 = it.part * part_keys, k1 = min(it.keys, k0 + part_keys);
+        const int32_t *row = a.table + (size_t)it.b * a.table_stride;
+        // the queries as the first product's second operand: column r, rows as K's pieces have them
+        bf16x8 q[DH / 32];
+        {
+            const bf16_t *qh = a.q + (int64_t)it.b * a.q_stride + (head0 + min(r, n_heads - 1)) * DH;
+#pragma unroll
+            for (int i = 0; i < DH / 32; ++i) {
+                const int d = E4M3 ? 16 * (4 * (i / 2) + c) + 8 * (i % 2) : 8 * (4 * i + c);
+                q[i] = *reinterpret_cast<const bf16x8 *>(qh + d);
+            }
+        }
+        float m = -INFINITY, l = 0.f;
+        f32x4 o[NV][W] = {};
+        const int steps = (k1 - k0 + 31) / 32;
+        for (int s0 = 0; s0 < steps; s0 += 32 * kWaves) {
+            // lane 2 i + t: the page of key tile t of this wave's i-th step from s0 on
+            int pages;
+            {
+                const int key = k0 + (s0 + wave + kWaves * (lane >> 1)) * 32 + (lane & 1) * 16;
+                pages = key < k1 ? row[key >> a.c.page_log2] : -1;
+                if (pages >= a.c.n_pages) pages = -1;
+            }
+            for (int i = 0; i < 32 && s0 + wave + kWaves * i < steps; ++i) {
+                const int key0 = k0 + (s0 + wave + kWaves * i) * 32;
+                u32x4 kr[2][NK], vr[2][NV];
+                int limit[2];     // keys of each tile that take part
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const int id = __builtin_amdgcn_readlane(pages, 2 * i + t);
+                    const int key = key0 + 16 * t, off = key & (page - 1);
+                    limit[t] = id < 0 ? 0 : min(16, k1 - key);
+                    const size_t at = ((size_t)max(id, 0) * a.c.kv_heads + kvh) * page_bytes;
+                    const char *kp = K + at + off * 16, *vp = V + at + (size_t)off * DH * ES;
+#pragma unroll
+                    for (int j = 0; j < NK; ++j)
+                        kr[t][j] = *reinterpret_cast<const u32x4 *>(kp + (uint32_t)(((4 * j + c) * page + r) * 16));
+#pragma unroll
+                    for (int j = 0; j < NV; ++j)
+                        vr[t][j] = *reinterpret_cast<const u32x4 *>(vp + (uint32_t)(c * DH * 4 * ES + (16 * j + r) * 16));
+                }
+                float p[8];
+                float mx = m;
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int j = 0; j < NK; ++j) {
+                        if constexpr (E4M3) {
+                            s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(widen(kr[t][j][0]), widen(kr[t][j][1])),
+                                                                        q[2 * j], s, 0, 0, 0);
+                            s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(widen(kr[t][j][2]), widen(kr[t][j][3])),
+                                                                        q[2 * j + 1], s, 0, 0, 0);
+                        } else {
+                            s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[t][j]), q[j], s, 0,
+                                                                        0, 0);
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        p[4 * t + e] = 4 * c + e < limit[t] ? s[e] * scale : -INFINITY;
+                        mx = fmaxf(mx, p[4 * t + e]);
+                    }
+                }
+                mx = across_rows_max(mx);
+                // nothing but -inf so far: any finite maximum gives p = 0
+                const float ref = mx == -INFINITY ? 0.f : mx;
+                if (__any(mx > m)) {
+                    const float f = __builtin_amdgcn_exp2f(m - ref);
+                    l *= f;
+#pragma unroll
+                    for (int j = 0; j < NV; ++j)
+#pragma unroll
+                        for (int w = 0; w < W; ++w) o[j][w] *= f;
+                    m = mx;
+                }
+                uint32_t hi[4], lo[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float x = __builtin_amdgcn_exp2f(p[2 * e] - ref), y = __builtin_amdgcn_exp2f(p[2 * e + 1] - ref);
+                    l += x + y;
+                    hi[e] = pack2(x, y);
+                    lo[e] = pack2(x - __uint_as_float(hi[e] << 16), y - __uint_as_float(hi[e] & 0xffff0000u));
+                }
+                const bf16x8 p_hi = __builtin_bit_cast(bf16x8, u32x4{hi[0], hi[1], hi[2], hi[3]});
+                const bf16x8 p_lo = __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], lo[2], lo[3]});
+                // places past the last key hold any bits: cleared, since 0 times NaN is NaN
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    if (limit[t] < 16) {
+                        const int n = min(max(limit[t] - 4 * c, 0), 4);
+#pragma unroll
+                        for (int j = 0; j < NV; ++j)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const int have = E4M3 ? 8 * n : min(max(16 * n - 32 * (e % 2), 0), 32);
+                                vr[t][j][e] &= have == 32 ? 0xffffffffu : (1u << have) - 1u;
+                            }
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+#pragma unroll
+                    for (int w = 0; w < W; ++w) {
+                        bf16x8 x;
+                        if constexpr (E4M3)
+                            x = operand(widen(vr[0][j][w]), widen(vr[1][j][w]));
+                        else
+                            x = operand(u32x2{vr[0][j][2 * w], vr[0][j][2 * w + 1]},
+                                        u32x2{vr[1][j][2 * w], vr[1][j][2 * w + 1]});
+                        o[j][w] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, p_hi, o[j][w], 0, 0, 0);
+                        o[j][w] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, p_lo, o[j][w], 0, 0, 0);
+                    }
+            }
+        }
+        // join the waves.  Lane (r, c) holds of head r the columns 16 W j + 4 W c + W e + w
+        l = across_rows_sum(l);
+        if (r < n_heads) {
+            if (c == 0) {
+                m_lds[wave][r] = m;
+                l_lds[wave][r] = l;
+            }
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                float *dst = &o_lds[wave][r][16 * W * j + 4 * W * c];
+                float flat[4 * W];
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int w = 0; w < W; ++w) flat[W * e + w] = o[j][w][e];
+#pragma unroll
+                for (int e = 0; e < W; ++e)
+                    *reinterpret_cast<f32x4 *>(dst + 4 * e) =
+                        f32x4{flat[4 * e], flat[4 * e + 1], flat[4 * e + 2], flat[4 * e + 3]};
+            }
+        }
+        __syncthreads();
+        const bool whole = part_count(it.keys, a.max_parts) == 1;
+        for (int i = tid; i < n_heads * (DH / 4); i += kThreads) {
+            const int h = i / (DH / 4), d = (i - h * (DH / 4)) * 4;
+            float top = m_lds[0][h];
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) top = fmaxf(top, m_lds[w][h]);
+            const float ref = top == -INFINITY ? 0.f : top;
+            float sum = 0.f;
+            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                const float f = __builtin_amdgcn_exp2f(m_lds[w][h] - ref);
+                sum += f * l_lds[w][h];
+                acc += f * *reinterpret_cast<const f32x4 *>(&o_lds[w][h][d]);
+            }
+            const size_t bh = (size_t)it.b * a.heads + head0 + h;
+            if (whole) {
+                const float inv = sum == 0.f ? 0.f : v_scale / sum;     // nothing to attend to: zeros
+                *reinterpret_cast<u32x2 *>(a.ctx + bh * DH + d) =
+                    u32x2{pack2(acc[0] * inv, acc[1] * inv), pack2(acc[2] * inv, acc[3] * inv)};
+            } else {
+                const size_t slot = bh * a.slots + it.part;
+                *reinterpret_cast<f32x4 *>(a.part_o + slot * DH + d) = acc * v_scale;
+                if (d == 0) *reinterpret_cast<f32x2 *>(a.part_ml + 2 * slot) = f32x2{top, sum};
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// Joins a request's parts: M = max m, ctx = sum 2^(m - M) o / sum 2^(m - M) l.
+// One workgroup per (request, head); a group of DH / 4 threads takes every
+// (4 * kThreads / DH)-th part, in order.
+template <int DH>
+__global__ __launch_bounds__(kThreads) void paged_join_kernel(AttnArgs a) {
+    constexpr int TPP = DH / 4, PAR = kThreads / TPP;
+    __shared__ __attribute__((aligned(16))) f32x4 acc_lds[PAR][TPP];
+    __shared__ float sum_lds[PAR];
+    const int bh = blockIdx.x, b = bh / a.heads;
+    const int parts = part_count(min(max(a.lens[b], 0), a.max_keys), a.max_parts);
+    if (parts == 1) return;
+    const float *ml = a.part_ml + (size_t)bh * a.slots * 2;
+    const int lane = threadIdx.x & 63;
+    float top = -INFINITY;
+    for (int i = lane; i < parts; i += 64) top = fmaxf(top, ml[2 * i]);
+#pragma unroll
+    for (int s = 32; s >= 1; s >>= 1) top = fmaxf(top, __shfl_xor(top, s));
+    const float ref = top == -INFINITY ? 0.f : top;
+    const int g = threadIdx.x / TPP, d = threadIdx.x % TPP;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    float sum = 0.f;
+    const f32x4 *o = reinterpret_cast<const f32x4 *>(a.part_o + (size_t)bh * a.slots * DH) + d;
+    for (int i = g; i < parts; i += PAR) {
+        const f32x2 x = *reinterpret_cast<const f32x2 *>(ml + 2 * i);
+        const float f = __builtin_amdgcn_exp2f(x[0] - ref);
+        sum += f * x[1];
+        acc += f * o[(size_t)i * TPP];
+    }
+    acc_lds[g][d] = acc;
+    if (d == 0) sum_lds[g] = sum;
+    __syncthreads();
+    if (g != 0) return;
+#pragma unroll
+    for (int i = 1; i < PAR; ++i) {
+        acc += acc_lds[i][d];
+        sum += sum_lds[i];
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    *reinterpret_cast<u32x2 *>(a.ctx + (size_t)bh * DH + 4 * d) =
+        u32x2{pack2(acc[0] * inv, acc[1] * inv), pack2(acc[2] * inv, acc[3] * inv)};
+}
+
+template <int DH>
+hipError_t launch_attention_dh(const AttnArgs &a, bool e4m3, dim3 grid, hipStream_t stream) {
+    const hipError_t e = e4m3 ? launch_kernel(paged_attention_kernel<DH, true>, grid, dim3(kThreads), stream, a)
+                              : launch_kernel(paged_attention_kernel<DH, false>, grid, dim3(kThreads), stream, a);
+    if (e != hipSuccess || a.slots == 1) return e;     // no request can have a second part
+    return launch_kernel(paged_join_kernel<DH>, dim3(a.batch * a.heads), dim3(kThreads), stream, a);
+}
+
+}  // namespace
+
+hipError_t launch_paged_plan(const PlanArgs &p, hipStream_t stream) {
+    // a workgroup for every kPlanSlots slots and every 16 requests, whichever is more
+    const int64_t groups = std::max<int64_t>((p.room + (int64_t)kPlanSlots - 1) / kPlanSlots, (p.batch + 15) / 16);
+    return launch_kernel(paged_plan_kernel, dim3((unsigned)std::min<int64_t>(groups, 1024)), dim3(kThreads), stream, p);
+}
+
+hipError_t launch_paged_append(const PagedCache &c, const bf16_t *k, const bf16_t *v, const int64_t *slots, int tokens,
+                               int64_t k_stride, int64_t v_stride, hipStream_t stream) {
+    const int64_t threads = (int64_t)tokens * c.kv_heads * (c.head_dim / 8);
+    const dim3 grid((unsigned)((threads + kThreads - 1) / kThreads));
+    return c.e4m3 ? launch_kernel(paged_append_kernel<true>, grid, dim3(kThreads), stream, c, k, v, slots, tokens, k_stride,
+                                  v_stride)
+                  : launch_kernel(paged_append_kernel<false>, grid, dim3(kThreads), stream, c, k, v, slots, tokens,
+                                  k_stride, v_stride);
+}
+
+size_t paged_workspace_floats(int batch, int heads, int kv_heads, int head_dim, int max_keys) {
+    const size_t slots = paged_parts(max_keys, paged_max_parts(heads, kv_heads));
+    return slots <= 1 ? 0 : (size_t)batch * heads * slots * (head_dim + 2);
+}
+
+hipError_t launch_paged_attention(const PagedCache &c, const bf16_t *q, int64_t q_stride, const int32_t *table,
+                                  int table_stride, int max_pages, const int32_t *lens, bf16_t *ctx, float *partials,
+                                  int batch, int heads, float scale, hipStream_t stream) {
+    AttnArgs a{};
+    a.c = c;
+    a.q = q;
+    a.q_stride = q_stride;
+    a.table = table;
+    a.table_stride = table_stride;
+    a.lens = lens;
+    a.ctx = ctx;
+    a.batch = batch;
+    a.heads = heads;
+    a.max_keys = max_pages << c.page_log2;
+    a.max_parts = paged_max_parts(heads, c.kv_heads);
+    a.slots = std::max(1, paged_parts(a.max_keys, a.max_parts));
+    a.scale_log2e = scale * 1.4426950408889634f;
+    a.part_o = partials;
+    a.part_ml = partials + (size_t)batch * heads * a.slots * c.head_dim;
+    // as many workgroups as the chip holds twice over, each going on to further items
+    const int y = c.kv_heads * paged_tiles(heads, c.kv_heads);
+    const int64_t items = (int64_t)batch * a.slots;
+    const int64_t x = std::min<int64_t>(items, std::max(1, 2048 / y));
+    const dim3 grid((unsigned)x, (unsigned)y);
+    return c.head_dim == 64 ? launch_attention_dh<64>(a, c.e4m3, grid, stream)
+                            : launch_attention_dh<128>(a, c.e4m3, grid, stream);
+}
+
+}  // namespace iefwd
