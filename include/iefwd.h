@@ -602,7 +602,9 @@ int iefwd_decode_attention_noalloc(const void *q, const void *k, const void *vt,
  * must belong, and returns without synchronising; it allocates nothing and may be
  * captured into a graph.  The caller owns all buffers; they are device memory unless
  * stated otherwise.  What does not fit is refused with EINVAL before anything
- * is launched.  Results do not depend on the other requests of the batch. */
+ * is launched.  A request's results do not depend on the other requests of the batch;
+ * iefwd_paged_attention's bits may differ between batch sizes, whose class (a power of
+ * two) chooses the order of the sums. */
 
 #define IEFWD_KV_BF16  0u
 #define IEFWD_KV_E4M3  1u   /* 8-bit floating point (1-4-3 bits, largest value 448) with a scale per key-value head */
@@ -679,8 +681,8 @@ int iefwd_paged_attention_workspace(const iefwd_paged_cache *cache, uint32_t bat
  * Lengths are cut to [0, max_pages * page_size]; a page id outside the pool drops
  * its tokens; a row with nothing to attend to becomes zeros.  fp32 scores, softmax and
  * sums; the probabilities enter the product with V in 16 bits.
- * The keys of a long request are split and joined by a rule on its length and
- * the head counts alone.  workspace: iefwd_paged_attention_workspace bytes, 16-byte aligned,
+ * The keys of a long request are split and joined by a rule on its length, the head
+ * counts and the batch size (iefwd_test_paged_split).  workspace: iefwd_paged_attention_workspace bytes, 16-byte aligned,
  * any contents; calls that may overlap need one each.  n_heads a multiple of
  * n_kv_heads, at most 1024; 1 <= batch <= 65535; max_pages >= 1 and
  * max_pages * page_size <= 2^30; scale finite. */
@@ -688,6 +690,12 @@ int iefwd_paged_attention(const iefwd_paged_cache *cache, const void *q, uint64_
                           const int32_t *table, uint32_t table_stride, uint32_t max_pages, const int32_t *lens,
                           uint32_t batch, float scale, void *ctx, void *workspace, size_t workspace_bytes,
                           void *stream);
+
+/* Pure host function: the keys in each part that iefwd_paged_attention splits a
+ * request of n_keys into, and the waves that work on a part, for a batch of this
+ * many requests.  n_keys <= 2^30, the rest as there. */
+int iefwd_test_paged_split(uint32_t batch, uint32_t n_heads, uint32_t n_kv_heads, uint32_t n_keys, uint32_t *part_keys,
+                           uint32_t *waves);
 
 /* The 4-bit form of a weight matrix W [N, K]: W[n][k] = scales[n][g] *
  * (code[n][k] - zeros[n][g]), g = k / group.  codes uint8 [N, K / 2], weight 2 i in the

@@ -94,6 +94,7 @@ SIGNATURES = {
     "iefwd_paged_append": (_i32, [_vp, _vp, _vp, _vp, _u32, _u64, _u64, _vp]),
     "iefwd_paged_attention_workspace": (_i32, [_vp, _u32, _u32, _u32, ctypes.POINTER(_sz)]),
     "iefwd_paged_attention": (_i32, [_vp, _vp, _u64, _u32, _vp, _u32, _u32, _vp, _u32, _f32, _vp, _vp, _sz, _vp]),
+    "iefwd_test_paged_split": (_i32, [_u32, _u32, _u32, _u32, ctypes.POINTER(_u32), ctypes.POINTER(_u32)]),
     "iefwd_q4_packed_bytes": (_i32, [_u32, _u32, _u32, ctypes.POINTER(_sz)]),
     "iefwd_q4_pack": (_i32, [_vp, _vp, _vp, _vp, _u32, _u32, _u32, _vp]),
     "iefwd_q4_gemm": (_i32, [_u32, _vp, _vp, _vp, _vp, _vp, _u32, _u32, _u32, _u32, _vp]),
@@ -459,59 +460,85 @@ class PagedCacheDesc(ctypes.Structure):
                 ("head_dim", _u32), ("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp)]
 
 
-def _tensor(name: str, t, dtype, device=None, shape=None):
-    """The checks of a tensor operand: type, place, and (with `shape`) that and that it is contiguous."""
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype or not t.is_cuda:
+def _is(t, dtype, device: int, shape) -> bool:
+    """Whether t is a contiguous tensor of this type, shape and GPU.  The calls of a decode step take a few
+    microseconds on the GPU, so their checks are one expression here and explained only when they fail."""
+    return isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == device and t.shape == shape and t.is_contiguous()
+
+
+def _need(name: str, t, dtype, device: int | None = None, shape=None):
+    """Raises unless t is a tensor of this type on the GPU and, if given, `device` and of `shape` and contiguous."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or not t.is_cuda:
         raise ValueError(f"{name} must be a {dtype} tensor on the GPU")
-    if device is not None and t.device != device:
-        raise ValueError(f"{name} is on {t.device}, not on {device}")
-    if shape is not None and (tuple(t.shape) != tuple(shape) or not t.is_contiguous()):
+    if device is not None and t.get_device() != device:
+        raise ValueError(f"{name} is on {t.device}, not on cuda:{device}")
+    if shape is not None and (t.shape != tuple(shape) or not t.is_contiguous()):
         raise ValueError(f"{name} must be contiguous with shape {tuple(shape)}")
     return t
 
 
-def _rows(name: str, t, device, rows: int, heads: int, head_dim: int) -> int:
+def _rows(name: str, t, device: int, rows: int, heads: int, head_dim: int) -> int:
     """Checks rows of heads (bf16 [rows, heads, head_dim], or the last two as one) that may be
     slices of wider rows; returns their stride in elements."""
-    _tensor(name, t, torch.bfloat16, device)
-    if t.shape == (rows, heads, head_dim):
-        flat = t.stride(2) == 1 and (heads == 1 or t.stride(1) == head_dim)
-    else:
-        flat = t.shape == (rows, heads * head_dim) and t.stride(1) == 1
-    if not flat:
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.bfloat16 or t.get_device() != device:
+        _need(name, t, torch.bfloat16, device)
+    shape, stride = t.shape, t.stride()
+    if not (shape == (rows, heads, head_dim) and stride[2] == 1 and (heads == 1 or stride[1] == head_dim) or
+            shape == (rows, heads * head_dim) and stride[1] == 1):
         raise ValueError(f"{name} must be [{rows}, {heads}, {head_dim}] with each row contiguous")
-    return t.stride(0) if rows > 1 else heads * head_dim
+    return stride[0] if rows > 1 else heads * head_dim
 
 
-def _call(device: torch.device, stream, name: str, *args) -> None:
+def _table(table, device: int, batch: int) -> tuple[int, int]:
+    """Checks int32 [batch, max_pages] with contiguous rows; returns the rows' stride and max_pages."""
+    if not isinstance(table, torch.Tensor) or table.dtype is not torch.int32 or table.get_device() != device:
+        _need("table", table, torch.int32, device)
+    if table.dim() != 2 or table.shape[0] != batch or (table.shape[1] > 1 and table.stride(1) != 1):
+        raise ValueError("table must be [batch, max_pages] with each row contiguous")
+    cols = table.shape[1]
+    return (table.stride(0) if batch > 1 else cols), cols
+
+
+# The handle of torch's current stream of a device: torch.cuda.current_stream(device).cuda_stream without the object around
+# it, which takes longer (1.7 us) than a launch does.
+_current_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else (
+    lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
+def _call(device: int, stream, name: str, *args) -> None:
     """Calls a library function with `device` current, on `stream` or else torch's current stream of it."""
-    handle = torch.cuda.current_stream(device).cuda_stream if stream is None else _stream(stream)
-    if torch.cuda.current_device() == device.index:
-        _check(getattr(lib(), name)(*args, handle), name)
+    handle = _current_stream(device) if stream is None else _stream(stream)
+    fn = getattr(_lib or lib(), name)
+    if torch.cuda.current_device() == device:
+        status = fn(*args, handle)
     else:
         with torch.cuda.device(device):
-            _check(getattr(lib(), name)(*args, handle), name)
+            status = fn(*args, handle)
+    if status != OK:
+        _check(status, name)
 
 
 class PagedCache:
     """A pool of pages of keys and values (``iefwd_paged_cache``) in the caller's tensors:
     k [n_pages, n_kv_heads, head_dim // E, page_size, E] and v [n_pages, n_kv_heads, page_size // 4,
     head_dim, 4], bfloat16 (E = 8) or float8_e4m3fn (E = 16; then with fp32 k_scale and v_scale
-    [n_kv_heads]).  ``PagedCache.empty`` makes them."""
+    [n_kv_heads]).  ``PagedCache.empty`` makes them.  Calls run on `stream`, by default torch's
+    current stream of the cache's GPU."""
 
     def __init__(self, k, v, k_scale=None, v_scale=None):
         e4m3 = isinstance(k, torch.Tensor) and k.dtype == torch.float8_e4m3fn
         dtype, e = (torch.float8_e4m3fn, 16) if e4m3 else (torch.bfloat16, 8)
-        _tensor("k", k, dtype)
+        _need("k", k, dtype)
         if k.dim() != 5 or k.shape[4] != e:
             raise ValueError(f"k must be [n_pages, n_kv_heads, head_dim // {e}, page_size, {e}]")
         n_pages, heads, pieces, page, _ = k.shape
-        self.device, self.page_size, self.n_kv_heads, self.head_dim = k.device, page, heads, pieces * e
-        _tensor("k", k, dtype, shape=k.shape)
-        _tensor("v", v, dtype, self.device, (n_pages, heads, page // 4, self.head_dim, 4))
+        self.device, self._dev = k.device, k.get_device()
+        self.page_size, self.n_kv_heads, self.head_dim = page, heads, pieces * e
+        _need("k", k, dtype, shape=k.shape)
+        _need("v", v, dtype, self._dev, (n_pages, heads, page // 4, self.head_dim, 4))
         if e4m3:
-            _tensor("k_scale", k_scale, torch.float32, self.device, (heads,))
-            _tensor("v_scale", v_scale, torch.float32, self.device, (heads,))
+            _need("k_scale", k_scale, torch.float32, self._dev, (heads,))
+            _need("v_scale", v_scale, torch.float32, self._dev, (heads,))
         elif k_scale is not None or v_scale is not None:
             raise ValueError("scales belong to a float8_e4m3fn cache")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
@@ -531,11 +558,13 @@ class PagedCache:
     def append(self, k, v, slots, stream=None) -> None:
         """Writes new tokens' keys and values, bf16 [tokens, n_kv_heads, head_dim] (rows may lie apart), to
         their slots (int64 [tokens], from ``paged_plan``; outside the pool: skipped)."""
-        n = _tensor("slots", slots, torch.int64, self.device).numel()
-        _tensor("slots", slots, torch.int64, self.device, (n,))
-        ks = _rows("k", k, self.device, n, self.n_kv_heads, self.head_dim)
-        vs = _rows("v", v, self.device, n, self.n_kv_heads, self.head_dim)
-        _call(self.device, stream, "iefwd_paged_append", self._ref, k.data_ptr(), v.data_ptr(), slots.data_ptr(), n, ks, vs)
+        dev = self._dev
+        n = len(slots)
+        if not _is(slots, torch.int64, dev, (n,)):
+            _need("slots", slots, torch.int64, dev, (n,))
+        ks = _rows("k", k, dev, n, self.n_kv_heads, self.head_dim)
+        vs = _rows("v", v, dev, n, self.n_kv_heads, self.head_dim)
+        _call(dev, stream, "iefwd_paged_append", self._ref, k.data_ptr(), v.data_ptr(), slots.data_ptr(), n, ks, vs)
 
     def workspace(self, batch: int, n_heads: int, max_pages: int) -> torch.Tensor:
         """A workspace for ``attention`` on a batch and a table of max_pages columns."""
@@ -548,83 +577,91 @@ class PagedCache:
         """out bf16 [batch, n_heads, head_dim] = attention of one query per request and head, q of that
         shape (rows may lie apart), over the pages in `table` (int32 [batch, max_pages], rows may lie apart) of
         lens (int32 [batch]) cached tokens.  scale: 1 / sqrt(head_dim) by default."""
-        batch, d = _tensor("lens", lens, torch.int32, self.device).numel(), self.head_dim
-        _tensor("lens", lens, torch.int32, self.device, (batch,))
-        _tensor("table", table, torch.int32, self.device)
-        if table.dim() != 2 or table.shape[0] != batch or (table.shape[1] > 1 and table.stride(1) != 1):
-            raise ValueError("table must be [batch, max_pages] with each row contiguous")
-        _tensor("out", out, torch.bfloat16, self.device)
+        dev, d = self._dev, self.head_dim
+        batch = len(lens)
+        if not _is(lens, torch.int32, dev, (batch,)):
+            _need("lens", lens, torch.int32, dev, (batch,))
+        stride, cols = _table(table, dev, batch)
         heads = out.numel() // (batch * d) if batch else 0
-        if out.shape not in ((batch, heads, d), (batch, heads * d)) or not out.is_contiguous():
-            raise ValueError("out must be contiguous, [batch, n_heads, head_dim]")
-        qs = _rows("q", q, self.device, batch, heads, d)
-        _tensor("workspace", workspace, torch.uint8, self.device)
-        if not workspace.is_contiguous():
-            raise ValueError("workspace must be contiguous")
-        cols = table.shape[1]
-        _call(self.device, stream, "iefwd_paged_attention", self._ref, q.data_ptr(), qs, heads, table.data_ptr(),
-              table.stride(0) if batch > 1 else cols, cols, lens.data_ptr(), batch, d ** -0.5 if scale is None else scale,
-              out.data_ptr(), workspace.data_ptr(), workspace.numel())
+        if not (_is(out, torch.bfloat16, dev, (batch, heads, d)) or _is(out, torch.bfloat16, dev, (batch, heads * d))):
+            _need("out", out, torch.bfloat16, dev, (batch, heads, d))
+        qs = _rows("q", q, dev, batch, heads, d)
+        if workspace.dtype is not torch.uint8 or workspace.get_device() != dev or not workspace.is_contiguous():
+            _need("workspace", workspace, torch.uint8, dev, (workspace.numel(),))
+        _call(dev, stream, "iefwd_paged_attention", self._ref, q.data_ptr(), qs, heads, table.data_ptr(), stride, cols,
+              lens.data_ptr(), batch, d ** -0.5 if scale is None else scale, out.data_ptr(), workspace.data_ptr(),
+              workspace.numel())
 
 
 def paged_plan(page_size: int, lens, new_lens, table, ring, counters, lens_out, counters_out, slots, starts, refused,
                stream=None) -> None:
     """Pages and slots of a step (``iefwd_paged_plan``): requests of lens cached tokens come to new_lens ones.
     int32 lens, new_lens, lens_out [batch], table [batch, max_pages] (rows may lie apart), ring [pages of the pool],
-    starts [batch + 1], refused [1]; int64 counters, counters_out [2], slots [most new tokens]."""
-    n = _tensor("lens", lens, torch.int32).numel()
-    dev, n_pages = lens.device, _tensor("ring", ring, torch.int32).numel()
-    room = _tensor("slots", slots, torch.int64).numel()
-    for name, t, dtype, shape in (("lens", lens, torch.int32, (n,)), ("new_lens", new_lens, torch.int32, (n,)),
-                                  ("lens_out", lens_out, torch.int32, (n,)), ("ring", ring, torch.int32, (n_pages,)),
-                                  ("counters", counters, torch.int64, (2,)), ("counters_out", counters_out, torch.int64, (2,)),
-                                  ("slots", slots, torch.int64, (room,)), ("starts", starts, torch.int32, (n + 1,)),
-                                  ("refused", refused, torch.int32, (1,))):
-        _tensor(name, t, dtype, dev, shape)
-    _tensor("table", table, torch.int32, dev)
-    if table.dim() != 2 or table.shape[0] != n or (table.shape[1] > 1 and table.stride(1) != 1):
-        raise ValueError("table must be [batch, max_pages] with each row contiguous")
-    cols = table.shape[1]
-    _call(dev, stream, "iefwd_paged_plan", n, page_size, lens.data_ptr(), new_lens.data_ptr(), table.data_ptr(),
-          table.stride(0) if n > 1 else cols, cols, ring.data_ptr(), n_pages, counters.data_ptr(), lens_out.data_ptr(),
-          counters_out.data_ptr(), slots.data_ptr(), room, starts.data_ptr(), refused.data_ptr())
+    starts [batch + 1], refused [1]; int64 counters, counters_out [2], slots [most new tokens].  Runs on `stream`, by
+    default torch's current stream of lens' GPU."""
+    dev = _need("lens", lens, torch.int32).get_device()
+    n, n_pages, room = len(lens), len(ring), len(slots)
+    i32, i64 = torch.int32, torch.int64
+    if not (_is(lens, i32, dev, (n,)) and _is(new_lens, i32, dev, (n,)) and _is(lens_out, i32, dev, (n,)) and
+            _is(ring, i32, dev, (n_pages,)) and _is(counters, i64, dev, (2,)) and _is(counters_out, i64, dev, (2,)) and
+            _is(slots, i64, dev, (room,)) and _is(starts, i32, dev, (n + 1,)) and _is(refused, i32, dev, (1,))):
+        for name, t, dtype, count in (("lens", lens, i32, n), ("new_lens", new_lens, i32, n), ("lens_out", lens_out, i32, n),
+                                      ("ring", ring, i32, n_pages), ("counters", counters, i64, 2),
+                                      ("counters_out", counters_out, i64, 2), ("slots", slots, i64, room),
+                                      ("starts", starts, i32, n + 1), ("refused", refused, i32, 1)):
+            _need(name, t, dtype, dev, (count,))
+    stride, cols = _table(table, dev, n)
+    _call(dev, stream, "iefwd_paged_plan", n, page_size, lens.data_ptr(), new_lens.data_ptr(), table.data_ptr(), stride, cols,
+          ring.data_ptr(), n_pages, counters.data_ptr(), lens_out.data_ptr(), counters_out.data_ptr(), slots.data_ptr(), room,
+          starts.data_ptr(), refused.data_ptr())
+
+
+def test_paged_split(batch: int, n_heads: int, n_kv_heads: int, n_keys: int) -> tuple[int, int]:
+    """(keys in a part, waves of a workgroup): how ``PagedCache.attention`` splits a request of n_keys."""
+    keys, waves = _u32(), _u32()
+    _check(lib().iefwd_test_paged_split(batch, n_heads, n_kv_heads, n_keys, ctypes.byref(keys), ctypes.byref(waves)),
+           "iefwd_test_paged_split")
+    return keys.value, waves.value
 
 
 class Q4Weight:
     """A weight matrix [N, K] in 4 bits, laid out for ``product`` once: codes uint8 [N, K / 2] (weight 2 i in
     the low half of byte i), scales bf16 [N, K / group], zeros uint8 [N, K / group] or None (8 everywhere);
-    W = scales (codes - zeros).  The tensors given are not kept."""
+    W = scales (codes - zeros).  The tensors given are not kept.  Calls run on `stream`, by default torch's
+    current stream of the weight's GPU."""
 
     def __init__(self, codes, scales, zeros=None, stream=None):
-        _tensor("codes", codes, torch.uint8)
+        _need("codes", codes, torch.uint8)
         if codes.dim() != 2 or not isinstance(scales, torch.Tensor) or scales.dim() != 2 or not scales.shape[1]:
             raise ValueError("codes must be [N, K / 2] and scales [N, K / group]")
-        self.device, self.N, self.K = codes.device, codes.shape[0], 2 * codes.shape[1]
+        self.device, self._dev, self.N, self.K = codes.device, codes.get_device(), codes.shape[0], 2 * codes.shape[1]
         self.group = self.K // scales.shape[1]
         shape = (self.N, self.K // self.group if self.group else 0)
-        _tensor("codes", codes, torch.uint8, shape=codes.shape)
-        _tensor("scales", scales, torch.bfloat16, self.device, shape)
+        _need("codes", codes, torch.uint8, shape=codes.shape)
+        _need("scales", scales, torch.bfloat16, self._dev, shape)
         if zeros is not None:
-            _tensor("zeros", zeros, torch.uint8, self.device, shape)
+            _need("zeros", zeros, torch.uint8, self._dev, shape)
         n = _sz()
         _check(lib().iefwd_q4_packed_bytes(self.N, self.K, self.group, ctypes.byref(n)), "iefwd_q4_packed_bytes")
         self.packed = torch.empty(n.value, dtype=torch.uint8, device=self.device)
-        _call(self.device, stream, "iefwd_q4_pack", codes.data_ptr(), scales.data_ptr(), _ptr(zeros), self.packed.data_ptr(), self.N,
-              self.K, self.group)
+        _call(self._dev, stream, "iefwd_q4_pack", codes.data_ptr(), scales.data_ptr(), _ptr(zeros), self.packed.data_ptr(),
+              self.N, self.K, self.group)
 
     def product(self, a, out, epilogue: int = EPI_BIAS_BF16, bias=None, resid=None, stream=None) -> None:
         """out [M, N] = epilogue(a W^T + bias), a bf16 [M, K], M <= 16; out bf16, or fp32 (as resid) for
         EPI_BIAS_RESID_F32; bias bf16 [N] or None."""
-        m = _tensor("a", a, torch.bfloat16, self.device).numel() // self.K
-        _tensor("a", a, torch.bfloat16, self.device, (m, self.K))
+        dev, m, n, k = self._dev, len(a), self.N, self.K
         f32 = epilogue == EPI_BIAS_RESID_F32
-        _tensor("out", out, torch.float32 if f32 else torch.bfloat16, self.device, (m, self.N))
-        if bias is not None:
-            _tensor("bias", bias, torch.bfloat16, self.device, (self.N,))
-        if f32:
-            _tensor("resid", resid, torch.float32, self.device, (m, self.N))
-        _call(self.device, stream, "iefwd_q4_gemm", epilogue, a.data_ptr(), self.packed.data_ptr(), _ptr(bias),
-              _ptr(resid) if f32 else None, out.data_ptr(), m, self.N, self.K, self.group)
+        kind = torch.float32 if f32 else torch.bfloat16
+        if not (_is(a, torch.bfloat16, dev, (m, k)) and _is(out, kind, dev, (m, n)) and
+                (bias is None or _is(bias, torch.bfloat16, dev, (n,))) and (not f32 or _is(resid, kind, dev, (m, n)))):
+            _need("a", a, torch.bfloat16, dev, (m, k))
+            _need("out", out, kind, dev, (m, n))
+            if bias is not None:
+                _need("bias", bias, torch.bfloat16, dev, (n,))
+            _need("resid", resid, kind, dev, (m, n))
+        _call(dev, stream, "iefwd_q4_gemm", epilogue, a.data_ptr(), self.packed.data_ptr(),
+              None if bias is None else bias.data_ptr(), resid.data_ptr() if f32 else None, out.data_ptr(), m, n, k, self.group)
 
 
 # ------------------------------------------------------------------ quota controller

@@ -25,6 +25,7 @@
 #include "attention_place.h"
 #include "kernels.h"
 #include "paged.h"
+#include "paged_split.h"
 #include "q4.h"
 #include "quota.h"
 
@@ -1953,11 +1954,15 @@ void check_row_stride(const char *what, const void *p, uint64_t stride, uint64_t
         fail(IEFWD_EINVAL, std::string(what) + ": rows must be 16-byte aligned and not overlap");
 }
 
+void check_batch_heads(uint32_t batch, uint32_t n_heads, uint32_t n_kv_heads) {
+    if (batch == 0 || batch > 65535) fail(IEFWD_EINVAL, "batch must be in [1, 65535]");
+    if (n_heads == 0 || n_heads > 1024 || n_kv_heads == 0 || n_heads % n_kv_heads)
+        fail(IEFWD_EINVAL, "n_heads must be a multiple of n_kv_heads, at most 1024");
+}
+
 // The workspace's size, with the argument checks that it shares with the launch.
 size_t paged_workspace(const PagedCache &c, uint32_t batch, uint32_t n_heads, uint32_t max_pages) {
-    if (batch == 0 || batch > 65535) fail(IEFWD_EINVAL, "batch must be in [1, 65535]");
-    if (n_heads == 0 || n_heads > 1024 || n_heads % c.kv_heads)
-        fail(IEFWD_EINVAL, "n_heads must be a multiple of n_kv_heads, at most 1024");
+    check_batch_heads(batch, n_heads, (uint32_t)c.kv_heads);
     return 4 * paged_workspace_floats((int)batch, (int)n_heads, c.kv_heads, c.head_dim, (int)(max_pages << c.page_log2));
 }
 
@@ -2050,6 +2055,18 @@ int iefwd_paged_attention(const iefwd_paged_cache *cache, const void *q, uint64_
                                          lens, (bf16_t *)ctx, static_cast<float *>(workspace), (int)batch, (int)n_heads,
                                          scale, (hipStream_t)stream),
                   "paged attention launch");
+    });
+}
+
+int iefwd_test_paged_split(uint32_t batch, uint32_t n_heads, uint32_t n_kv_heads, uint32_t n_keys, uint32_t *part_keys,
+                           uint32_t *waves) {
+    return guarded([&] {
+        if (!part_keys || !waves) fail(IEFWD_EINVAL, "NULL pointer");
+        check_batch_heads(batch, n_heads, n_kv_heads);
+        if (n_keys > (1u << 30)) fail(IEFWD_EINVAL, "n_keys must be at most 2^30");
+        const PagedSplit split = paged_split((int)batch, (int)n_heads, (int)n_kv_heads);
+        *part_keys = 1u << paged_part_log2((int)n_keys, split);
+        *waves = (uint32_t)split.waves;
     });
 }
 

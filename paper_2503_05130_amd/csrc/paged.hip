@@ -244,40 +244,51 @@ struct AttnArgs {
     bf16_t *ctx;
     float *part_o;       // [batch, heads, slots, head_dim]
     float *part_ml;      // [batch, heads, slots, 2]
-    int table_stride, batch, heads, max_keys, max_parts, slots;
+    int table_stride, batch, heads, max_keys, slots;
+    PagedSplit split;
     float scale_log2e;
 };
 
-__device__ inline int wave_scan(int v) {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int below = __shfl_up(v, o);
-        if (lane >= o) v += below;
-    }
-    return v;
+// The lane, hidden from the compiler: what is computed from it inside the loop over
+// items stays there instead of being held in registers through it (153 -> 140 VGPRs).
+__device__ inline int opaque_lane() {
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    return lane;
 }
 
-__device__ inline int part_count(int n, int max_parts) { return max(1, paged_parts(n, max_parts)); }
+// Inclusive sum over the wave's lanes: row shifts by 1, 2, 4, 8, then lane 15's row
+// total to the next row and lane 31's to the upper half.
+__device__ inline int wave_scan(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
+    return v;
+}
 
 struct AttnItem {
     int b, part, keys;
 };
 
 // The item-th (request, part) of the batch, requests in order; false past the last.
-// Every wave finds it by itself from the lengths, 64 requests at a time.
+// Every wave finds it by itself from the lengths, 64 requests at a time.  A request
+// without keys has one part, which writes its zeros.
 __device__ inline bool find_item(const AttnArgs &a, int item, int &b0, int &before, AttnItem &out) {
-    const int lane = threadIdx.x & 63;
+    const int lane = opaque_lane();
     for (; b0 < a.batch; b0 += 64) {
         const bool in = b0 + lane < a.batch;
         const int n = in ? min(max(a.lens[b0 + lane], 0), a.max_keys) : 0;
-        const int parts = in ? part_count(n, a.max_parts) : 0;
+        const int parts = in ? paged_parts(n, a.split) : 0;
         const int to = before + wave_scan(parts);
         const int total = __builtin_amdgcn_readlane(to, 63);
         if (item < total) {
             const int src = __builtin_ctzll(__ballot(to > item));
-            out.b = b0 + src;
-            out.part = item - (__builtin_amdgcn_readlane(to, src) - __builtin_amdgcn_readlane(parts, src));
+            out.b = __builtin_amdgcn_readfirstlane(b0 + src);
+            out.part = __builtin_amdgcn_readfirstlane(item - __builtin_amdgcn_readlane(to, src) +
+                                                      __builtin_amdgcn_readlane(parts, src));
             out.keys = __builtin_amdgcn_readlane(n, src);
             return true;
         }
@@ -286,14 +297,22 @@ __device__ inline bool find_item(const AttnArgs &a, int item, int &b0, int &befo
     return false;
 }
 
+// v of lanes l, l ^ 16, l ^ 32 and l ^ 48 together: each swap leaves a row's (half's) value
+// in one result and its neighbour's in the other.
 __device__ inline float across_rows_max(float v) {
-    v = fmaxf(v, __shfl_xor(v, 16));
-    return fmaxf(v, __shfl_xor(v, 32));
+    const uint32_t x = __float_as_uint(v);
+    const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    const uint32_t y = __float_as_uint(fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1])));
+    const auto b = __builtin_amdgcn_permlane32_swap(y, y, false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
 __device__ inline float across_rows_sum(float v) {
-    v += __shfl_xor(v, 16);
-    return v + __shfl_xor(v, 32);
+    const uint32_t x = __float_as_uint(v);
+    const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    const uint32_t y = __float_as_uint(__uint_as_float(a[0]) + __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(y, y, false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
 // four e4m3 values as four bf16 (exact)
@@ -306,32 +325,43 @@ __device__ inline u32x2 widen(uint32_t w) {
 
 __device__ inline bf16x8 operand(u32x2 a, u32x2 b) { return __builtin_bit_cast(bf16x8, u32x4{a[0], a[1], b[0], b[1]}); }
 
-template <int DH, bool E4M3>
-__global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttnArgs a) {
+// A page of one head as a buffer: its base in scalar registers, so that a load needs one
+// 32-bit offset a lane, and nothing past the page is read.
+__device__ inline __amdgpu_buffer_rsrc_t page_buffer(const char *base, size_t at, uint32_t bytes) {
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)at), hi = __builtin_amdgcn_readfirstlane((uint32_t)(at >> 32));
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base + ((uint64_t)hi << 32 | lo)), 0, bytes, 0x00027000);
+}
+
+template <int DH, bool E4M3, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void paged_attention_kernel(AttnArgs a) {
     constexpr int ES = E4M3 ? 1 : 2;             // bytes per element
     constexpr int NK = DH * ES / 64;             // 16-byte loads per lane and key tile: DH columns of 16 keys
     constexpr int W = E4M3 ? 4 : 2;              // columns of V in a 16-byte load
     constexpr int NV = DH / (16 * W);            // such loads per key tile
     constexpr int ROW = DH + 4;
-    __shared__ __attribute__((aligned(16))) float o_lds[kWaves][16][ROW];
-    __shared__ float m_lds[kWaves][16], l_lds[kWaves][16];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    __shared__ __attribute__((aligned(16))) float o_lds[WAVES][16][ROW];
+    __shared__ float m_lds[WAVES][16], l_lds[WAVES][16];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, c = lane >> 4;
     const int group = a.heads / a.c.kv_heads, tiles = (group + 15) / 16;
-    const int kvh = blockIdx.y / tiles, tile = blockIdx.y - kvh * tiles;
+    // the heads of one item next to each other: their parts of a page are neighbours in memory
+    const int rows = a.c.kv_heads * tiles, step = gridDim.x / rows;
+    const int item0 = blockIdx.x / rows, row = blockIdx.x - item0 * rows;
+    const int kvh = row / tiles, tile = row - kvh * tiles;
     const int head0 = kvh * group + tile * 16, n_heads = min(16, group - tile * 16);
     const int page = 1 << a.c.page_log2;
-    const size_t page_bytes = (size_t)page * DH * ES;
+    const uint32_t page_bytes = page * DH * ES;
     const char *K = static_cast<const char *>(a.c.k), *V = static_cast<const char *>(a.c.v);
     const float scale = E4M3 ? a.scale_log2e * a.c.k_scale[kvh] : a.scale_log2e;
     const float v_scale = E4M3 ? a.c.v_scale[kvh] : 1.f;
+    const uint32_t k_lane = (c * page + r) * 16, v_lane = c * DH * 4 * ES + r * 16;
 
     int b0 = 0, before = 0;
     AttnItem it;
-    for (int item = blockIdx.x; find_item(a, item, b0, before, it); item += gridDim.x) {
-        const int part_keys = paged_part_keys(it.keys, a.max_parts);
-        const int k0 = it.part * part_keys, k1 = min(it.keys, k0 + part_keys);
-        const int32_t *row = a.table + (size_t)it.b * a.table_stride;
+    for (int item = item0; find_item(a, item, b0, before, it); item += step) {
+        const int part_log2 = paged_part_log2(it.keys, a.split);
+        const int k0 = it.part << part_log2, k1 = min(it.keys, k0 + (1 << part_log2));
+        const int32_t *ids = a.table + (size_t)it.b * a.table_stride;
         // the queries as the first product's second operand: column r, rows as K's pieces have them
         bf16x8 q[DH / 32];
         {
@@ -345,16 +375,16 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttnArgs a
         float m = -INFINITY, l = 0.f;
         f32x4 o[NV][W] = {};
         const int steps = (k1 - k0 + 31) / 32;
-        for (int s0 = 0; s0 < steps; s0 += 32 * kWaves) {
+        for (int s0 = 0; s0 < steps; s0 += 32 * WAVES) {
             // lane 2 i + t: the page of key tile t of this wave's i-th step from s0 on
             int pages;
             {
-                const int key = k0 + (s0 + wave + kWaves * (lane >> 1)) * 32 + (lane & 1) * 16;
-                pages = key < k1 ? row[key >> a.c.page_log2] : -1;
+                const int key = k0 + (s0 + wave + WAVES * (lane >> 1)) * 32 + (lane & 1) * 16;
+                pages = key < k1 ? ids[key >> a.c.page_log2] : -1;
                 if (pages >= a.c.n_pages) pages = -1;
             }
-            for (int i = 0; i < 32 && s0 + wave + kWaves * i < steps; ++i) {
-                const int key0 = k0 + (s0 + wave + kWaves * i) * 32;
+            for (int i = 0; i < 32 && s0 + wave + WAVES * i < steps; ++i) {
+                const int key0 = k0 + (s0 + wave + WAVES * i) * 32;
                 u32x4 kr[2][NK], vr[2][NV];
                 int limit[2];     // keys of each tile that take part
 #pragma unroll
@@ -363,13 +393,13 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttnArgs a
                     const int key = key0 + 16 * t, off = key & (page - 1);
                     limit[t] = id < 0 ? 0 : min(16, k1 - key);
                     const size_t at = ((size_t)max(id, 0) * a.c.kv_heads + kvh) * page_bytes;
-                    const char *kp = K + at + off * 16, *vp = V + at + (size_t)off * DH * ES;
+                    const __amdgpu_buffer_rsrc_t kp = page_buffer(K, at, page_bytes), vp = page_buffer(V, at, page_bytes);
 #pragma unroll
                     for (int j = 0; j < NK; ++j)
-                        kr[t][j] = *reinterpret_cast<const u32x4 *>(kp + (uint32_t)(((4 * j + c) * page + r) * 16));
+                        kr[t][j] = __builtin_amdgcn_raw_buffer_load_b128(kp, k_lane, off * 16 + j * 64 * page, 0);
 #pragma unroll
                     for (int j = 0; j < NV; ++j)
-                        vr[t][j] = *reinterpret_cast<const u32x4 *>(vp + (uint32_t)(c * DH * 4 * ES + (16 * j + r) * 16));
+                        vr[t][j] = __builtin_amdgcn_raw_buffer_load_b128(vp, v_lane, off * DH * ES + j * 256, 0);
                 }
                 float p[8];
                 float mx = m;
@@ -447,14 +477,15 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttnArgs a
         }
         // join the waves.  Lane (r, c) holds of head r the columns 16 W j + 4 W c + W e + w
         l = across_rows_sum(l);
-        if (r < n_heads) {
-            if (c == 0) {
-                m_lds[wave][r] = m;
-                l_lds[wave][r] = l;
+        const int late = opaque_lane(), head = late & 15, quad = late >> 4;
+        if (head < n_heads) {
+            if (quad == 0) {
+                m_lds[wave][head] = m;
+                l_lds[wave][head] = l;
             }
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
-                float *dst = &o_lds[wave][r][16 * W * j + 4 * W * c];
+                float *dst = &o_lds[wave][head][16 * W * j + 4 * W * quad];
                 float flat[4 * W];
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
@@ -467,17 +498,17 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attention_kernel(AttnArgs a
             }
         }
         __syncthreads();
-        const bool whole = part_count(it.keys, a.max_parts) == 1;
-        for (int i = tid; i < n_heads * (DH / 4); i += kThreads) {
+        const bool whole = it.keys <= 1 << part_log2;
+        for (int i = wave * 64 + late; i < n_heads * (DH / 4); i += 64 * WAVES) {
             const int h = i / (DH / 4), d = (i - h * (DH / 4)) * 4;
             float top = m_lds[0][h];
 #pragma unroll
-            for (int w = 1; w < kWaves; ++w) top = fmaxf(top, m_lds[w][h]);
+            for (int w = 1; w < WAVES; ++w) top = fmaxf(top, m_lds[w][h]);
             const float ref = top == -INFINITY ? 0.f : top;
             float sum = 0.f;
             f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
+            for (int w = 0; w < WAVES; ++w) {
                 const float f = __builtin_amdgcn_exp2f(m_lds[w][h] - ref);
                 sum += f * l_lds[w][h];
                 acc += f * *reinterpret_cast<const f32x4 *>(&o_lds[w][h][d]);
@@ -506,7 +537,7 @@ __global__ __launch_bounds__(kThreads) void paged_join_kernel(AttnArgs a) {
     __shared__ __attribute__((aligned(16))) f32x4 acc_lds[PAR][TPP];
     __shared__ float sum_lds[PAR];
     const int bh = blockIdx.x, b = bh / a.heads;
-    const int parts = part_count(min(max(a.lens[b], 0), a.max_keys), a.max_parts);
+    const int parts = paged_parts(min(max(a.lens[b], 0), a.max_keys), a.split);
     if (parts == 1) return;
     const float *ml = a.part_ml + (size_t)bh * a.slots * 2;
     const int lane = threadIdx.x & 63;
@@ -539,10 +570,11 @@ __global__ __launch_bounds__(kThreads) void paged_join_kernel(AttnArgs a) {
         u32x2{pack2(acc[0] * inv, acc[1] * inv), pack2(acc[2] * inv, acc[3] * inv)};
 }
 
-template <int DH>
-hipError_t launch_attention_dh(const AttnArgs &a, bool e4m3, dim3 grid, hipStream_t stream) {
-    const hipError_t e = e4m3 ? launch_kernel(paged_attention_kernel<DH, true>, grid, dim3(kThreads), stream, a)
-                              : launch_kernel(paged_attention_kernel<DH, false>, grid, dim3(kThreads), stream, a);
+template <int DH, bool E4M3>
+hipError_t launch_attention(const AttnArgs &a, dim3 grid, hipStream_t stream) {
+    const hipError_t e = a.split.waves == 8
+                             ? launch_kernel(paged_attention_kernel<DH, E4M3, 8>, grid, dim3(512), stream, a)
+                             : launch_kernel(paged_attention_kernel<DH, E4M3, 4>, grid, dim3(256), stream, a);
     if (e != hipSuccess || a.slots == 1) return e;     // no request can have a second part
     return launch_kernel(paged_join_kernel<DH>, dim3(a.batch * a.heads), dim3(kThreads), stream, a);
 }
@@ -566,8 +598,8 @@ hipError_t launch_paged_append(const PagedCache &c, const bf16_t *k, const bf16_
 }
 
 size_t paged_workspace_floats(int batch, int heads, int kv_heads, int head_dim, int max_keys) {
-    const size_t slots = paged_parts(max_keys, paged_max_parts(heads, kv_heads));
-    return slots <= 1 ? 0 : (size_t)batch * heads * slots * (head_dim + 2);
+    const size_t slots = paged_most_parts(max_keys, paged_split(batch, heads, kv_heads));
+    return slots == 1 ? 0 : (size_t)batch * heads * slots * (head_dim + 2);
 }
 
 hipError_t launch_paged_attention(const PagedCache &c, const bf16_t *q, int64_t q_stride, const int32_t *table,
@@ -584,18 +616,20 @@ hipError_t launch_paged_attention(const PagedCache &c, const bf16_t *q, int64_t 
     a.batch = batch;
     a.heads = heads;
     a.max_keys = max_pages << c.page_log2;
-    a.max_parts = paged_max_parts(heads, c.kv_heads);
-    a.slots = std::max(1, paged_parts(a.max_keys, a.max_parts));
+    a.split = paged_split(batch, heads, c.kv_heads);
+    a.slots = paged_most_parts(a.max_keys, a.split);
     a.scale_log2e = scale * 1.4426950408889634f;
     a.part_o = partials;
     a.part_ml = partials + (size_t)batch * heads * a.slots * c.head_dim;
-    // as many workgroups as the chip holds twice over, each going on to further items
-    const int y = c.kv_heads * paged_tiles(heads, c.kv_heads);
+    // The lengths are the device's: a workgroup for every part that there could be, up to 8 a CU, which then
+    // go on to further items.  (16 a CU: 64 x 4000 - 8192 keys 1.8% faster, but 96 x 5 - 12000 7% slower, most of
+    // whose workgroups find nothing to do.)
+    const int rows = c.kv_heads * paged_tiles(heads, c.kv_heads);
     const int64_t items = (int64_t)batch * a.slots;
-    const int64_t x = std::min<int64_t>(items, std::max(1, 2048 / y));
-    const dim3 grid((unsigned)x, (unsigned)y);
-    return c.head_dim == 64 ? launch_attention_dh<64>(a, c.e4m3, grid, stream)
-                            : launch_attention_dh<128>(a, c.e4m3, grid, stream);
+    const dim3 grid((unsigned)(std::min<int64_t>(items, std::max(1, 2048 / rows)) * rows));
+    if (c.head_dim == 64)
+        return c.e4m3 ? launch_attention<64, true>(a, grid, stream) : launch_attention<64, false>(a, grid, stream);
+    return c.e4m3 ? launch_attention<128, true>(a, grid, stream) : launch_attention<128, false>(a, grid, stream);
 }
 
 }  // namespace iefwd

@@ -1,34 +1,73 @@
-// How paged attention splits a request's keys: into parts of one length, a
-// multiple of 128 keys and at least 256, at most paged_max_parts() of them.
-// Host and device code share it (the workspace is sized by the same rule).
+// How paged attention splits a request's keys into parts, one workgroup each per
+// key-value head and 16 of its query heads.  Host and device code share it (the
+// workspace is sized by the same rule).
 #pragma once
 
 #include <hip/hip_runtime.h>
 
 namespace iefwd {
 
-constexpr int kPagedMinPart = 256;
-
 // Query heads of one key-value head are worked on in tiles of 16, the width
 // of one MFMA operand.
 inline __host__ __device__ int paged_tiles(int n_heads, int n_kv_heads) { return (n_heads / n_kv_heads + 15) / 16; }
 
-// The most parts a request is cut into: together with the key-value heads about two
-// workgroups a CU for a single request.  It depends on the head layout alone, never
-// on the batch, so that a request's result does not depend on its neighbours.
-inline __host__ __device__ int paged_max_parts(int n_heads, int n_kv_heads) {
-    const int per_part = n_kv_heads * paged_tiles(n_heads, n_kv_heads);
-    return per_part >= 16 ? 32 : 512 / per_part;
+// For `rows` = batch x key-value heads x tiles, in classes of a factor of two:
+//  - up to 256 rows (the CUs of the chip) a request is cut into up to 256 / rows
+//    parts (at most 64) of at least 256 keys, for workgroups of 8 waves, one a CU;
+//  - above, into 8 parts of at least 512, for workgroups of 4 waves.
+// A part has a power of two of keys, and at most 1024 up to 128 parts: one long
+// request among short ones must not be left to a few workgroups.
+// Measured (us, workgroups of 8 / 4 waves and parts of 256, 512, 1024 keys; 32 query and 8
+// key-value heads of 128 unless stated):
+//   1 x 4000 keys        11.1 11.6 14.0 / 11.5 12.8 16.8
+//   1 x 32001            35.3 35.3 30.9 / 31.9 32.0 31.9
+//   16 x 2000            41.5 35.2 31.3 / 32.9 31.5 31.8
+//   64 x 4000 - 8192      330  295  275 /  295  285  275
+//   96 x 5 - 12000, 16 / 4 heads of 64, e4m3   36.7 30.5 28.5 / 27.3 25.6 25.1
+struct PagedSplit {
+    int log2_parts;   // up to this many parts (log2)
+    int min_log2;     // of at least this many keys (log2)
+    int waves;        // of a workgroup
+};
+
+inline __host__ __device__ int log2_up(int n) { return n <= 1 ? 0 : 32 - __builtin_clz((unsigned)(n - 1)); }
+
+inline __host__ __device__ PagedSplit paged_split(int batch, int n_heads, int n_kv_heads) {
+    const long rows = (long)batch * n_kv_heads * paged_tiles(n_heads, n_kv_heads);
+    if (rows > 256) return {3, 9, 4};
+    const int spare = 8 - log2_up((int)rows);
+    return {spare < 6 ? spare : 6, 8, 8};
 }
 
-inline __host__ __device__ int paged_part_keys(int n_keys, int max_parts) {
-    const int even = (n_keys + max_parts - 1) / max_parts;
-    return even <= kPagedMinPart ? kPagedMinPart : (even + 127) / 128 * 128;
+// log2 of the keys in each part of a request of n_keys >= 0 (never falls as n_keys grows)
+inline __host__ __device__ int paged_part_log2(int n_keys, PagedSplit s) {
+    const int even = log2_up((n_keys + (1 << s.log2_parts) - 1) >> s.log2_parts);
+    const int most = log2_up((n_keys + 127) >> 7);      // for 128 parts
+    const int part = even < s.min_log2 ? s.min_log2 : even > 10 ? 10 : even;
+    return part < most ? most : part;
 }
 
-inline __host__ __device__ int paged_parts(int n_keys, int max_parts) {
-    const int part = paged_part_keys(n_keys, max_parts);
-    return (n_keys + part - 1) / part;
+inline __host__ __device__ int paged_parts(int n_keys, PagedSplit s) {
+    const int log2 = paged_part_log2(n_keys, s);
+    return n_keys <= 1 ? 1 : (n_keys + (1 << log2) - 1) >> log2;
+}
+
+// The most parts of any request of at most max_keys.  The count falls where the part
+// doubles, so the longest request need not have the most.
+inline int paged_most_parts(int max_keys, PagedSplit s) {
+    int most = 1;
+    for (int n = max_keys; n > 0;) {
+        const int log2 = paged_part_log2(n, s), parts = paged_parts(n, s);
+        if (parts > most) most = parts;
+        int lo = 0, hi = n - 1;                          // the longest with a smaller part, 0 if none
+        while (lo < hi) {
+            const int mid = lo + (hi - lo + 1) / 2;
+            if (paged_part_log2(mid, s) < log2) lo = mid;
+            else hi = mid - 1;
+        }
+        n = lo;
+    }
+    return most;
 }
 
 }  // namespace iefwd

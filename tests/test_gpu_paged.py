@@ -270,9 +270,12 @@ def test_attention_lengths(kind, heads, kv, dim, page):
 @pytest.mark.parametrize("kind,heads,kv,dim,page,lens", [
     ("bf16", 16, 16, 64, 16, [9000, 1, 8193]),            # parts longer than 256 keys
     ("bf16", 8, 8, 128, 64, [40000]),
-    ("e4m3", 4, 1, 128, 16, [131073, 3]),                 # 512 parts
+    ("e4m3", 4, 1, 128, 16, [131073, 3]),                 # parts longer than 1024 keys
     ("e4m3", 32, 32, 64, 128, [20001, 0, 300]),
     ("bf16", 24, 1, 64, 16, [70000]),                     # two tiles of query heads
+    ("e4m3", 2, 1, 64, 256, [1100000]),                   # each wave's steps looked up in two rounds
+    ("bf16", 64, 64, 64, 16, [2100, 513, 512, 511, 4097]),    # many rows: workgroups of 4 waves
+    ("bf16", 36, 36, 128, 32, [1025, 8200, 0, 31, 33, 600, 1024, 5]),
 ])
 def test_attention_long(kind, heads, kv, dim, page, lens):
     _check_attention(*_attention_case(kind, len(lens), heads, kv, dim, page, lens, 77))
@@ -320,17 +323,20 @@ def test_attention_of_scores_with_infinities():
     assert torch.isnan(_attend(ops)).all()
 
 
-def test_attention_result_depends_on_no_other_request():
-    lens = [700, 3, 0, 5000, 256, 900] * 20
-    ops, _ = _attention_case("bf16", len(lens), 8, 2, 128, 16, lens, 9)
+@pytest.mark.parametrize("batch", [3, 60, 400])
+def test_attention_result_depends_on_no_other_request(batch):
+    lens = ([700, 3, 0, 5000, 256, 900] * batch)[:batch]
+    ops, _ = _attention_case("bf16", batch, 8, 2, 128, 16, lens, 9)
     full = _attend(ops).clone()
     assert torch.equal(full, _attend(ops))
-    for b in (0, 3, 64, 117):
-        one = dict(ops, q=ops["q"][b:b + 1], table=ops["table"][b:b + 1], lens=ops["lens"][b:b + 1],
-                   out=torch.full((2, 8, 128), 9.0, dtype=torch.bfloat16, device=DEV))
-        assert torch.equal(_attend(one)[0], full[b])
+    # the others shorter, gone or in another order
+    keep = torch.arange(batch, device=DEV) % 3 == 0
+    assert torch.equal(_attend(dict(ops, lens=torch.where(keep, ops["lens"], ops["lens"] // 2)))[keep], full[keep])
+    assert torch.equal(_attend(dict(ops, lens=torch.where(keep, ops["lens"], 0)))[keep], full[keep])
+    order = torch.randperm(batch, generator=torch.Generator().manual_seed(1)).to(DEV)
+    assert torch.equal(_attend(dict(ops, q=ops["q"][order], table=ops["table"][order], lens=ops["lens"][order])), full[order])
     # columns of the table that no request uses
-    wide = torch.full((len(lens), 900), -1, dtype=torch.int32, device=DEV)
+    wide = torch.full((batch, 900), -1, dtype=torch.int32, device=DEV)
     wide[:, :ops["table"].shape[1]] = ops["table"]
     assert torch.equal(_attend(dict(ops, table=wide)), full)
 

@@ -42,7 +42,7 @@ def _append(cache, k=P, v=P, slots=P, n=5, ks=256, vs=256):
     return ie.lib().iefwd_paged_append(None if cache is None else ctypes.byref(cache), k, v, slots, n, ks, vs, None)
 
 
-def _attention(cache, q=P, qs=512, heads=8, table=P, stride=20, pages=20, lens=P, batch=3, scale=1.0, ctx=P, ws=P, bytes_=1 << 30):
+def _attention(cache, q=P, qs=512, heads=8, table=P, stride=200, pages=200, lens=P, batch=3, scale=1.0, ctx=P, ws=P, bytes_=1 << 30):
     return ie.lib().iefwd_paged_attention(None if cache is None else ctypes.byref(cache), q, qs, heads, table, stride, pages, lens,
                                           batch, scale, ctx, ws, bytes_, None)
 
@@ -73,21 +73,42 @@ def test_append_of_nothing_is_fine():
 
 
 @pytest.mark.parametrize("bad", [dict(q=None), dict(q=P + 4), dict(qs=511), dict(qs=516), dict(heads=0), dict(heads=6),
-                                 dict(heads=1028), dict(table=None), dict(lens=None), dict(ctx=None), dict(ctx=P + 2), dict(stride=19),
+                                 dict(heads=1028), dict(table=None), dict(lens=None), dict(ctx=None), dict(ctx=P + 2), dict(stride=199),
                                  dict(pages=0), dict(stride=2 ** 31), dict(stride=2 ** 27, pages=2 ** 27), dict(batch=0),
                                  dict(batch=65536), dict(scale=float("inf")), dict(scale=float("nan")), dict(ws=None),
-                                 dict(ws=P + 4), dict(bytes_=100)])
+                                 dict(ws=P + 4), dict(bytes_=100)])      # 3200 keys: more than a part
 def test_attention_refuses(bad):
     assert _attention(_desc(), **bad) == ie.EINVAL and ie.last_error()
 
 
-@pytest.mark.parametrize("heads,kv,pages,parts", [(4, 4, 16, 1), (4, 4, 17, 2), (4, 4, 1000, 63), (4, 4, 2048, 128), (4, 4, 5000, 125),
-                                                  (16, 16, 512, 32), (16, 16, 513, 22), (1, 1, 8192, 512), (40, 2, 4000, 125)])
-def test_workspace_holds_the_parts_of_the_longest_request(heads, kv, pages, parts):
-    n = ctypes.c_size_t()
-    assert ie.lib().iefwd_paged_attention_workspace(ctypes.byref(_desc(n_kv_heads=kv, head_dim=128)), 3, heads, pages,
-                                                    ctypes.byref(n)) == ie.OK
-    assert n.value == (0 if parts == 1 else 3 * heads * parts * (128 + 2) * 4)
+@pytest.mark.parametrize("batch,heads,kv", [(1, 4, 4), (1, 1, 1), (3, 32, 8), (16, 16, 16), (20, 16, 16), (1, 40, 2), (300, 64, 1),
+                                            (64, 32, 8)])
+def test_workspace_holds_the_parts_of_every_length(batch, heads, kv):
+    """The count of parts falls where a part doubles, so the longest request need not have the most."""
+    most, last, rng = 1, 0, list(range(0, 9000)) + list(range(9000, 300000, 37)) + [2 ** k + d for k in range(14, 20) for d in (0, 1)]
+    lengths = iter(sorted(rng))
+    seen = next(lengths)
+    for pages in (1, 2, 16, 17, 63, 64, 65, 128, 129, 500, 512, 513, 514, 1000, 5000, 16000, 18000):
+        while seen is not None and seen <= 16 * pages:
+            keys, waves = ie.test_paged_split(batch, heads, kv, seen)
+            assert keys >= last and keys & (keys - 1) == 0 and waves in (4, 8)
+            last, most = keys, max(most, -(-seen // keys))
+            seen = next(lengths, None)
+        n = ctypes.c_size_t()
+        assert ie.lib().iefwd_paged_attention_workspace(ctypes.byref(_desc(n_kv_heads=kv, head_dim=128)), batch, heads, pages,
+                                                        ctypes.byref(n)) == ie.OK
+        parts = n.value // (batch * heads * (128 + 2) * 4)
+        assert n.value == parts * batch * heads * (128 + 2) * 4
+        assert parts == 0 and most == 1 or parts >= most and parts <= most + 1      # the sample may miss the very most
+        assert parts <= 128
+
+
+@pytest.mark.parametrize("bad", [(0, 4, 4, 1), (65536, 4, 4, 1), (1, 0, 1, 1), (1, 6, 4, 1), (1, 4, 0, 1), (1, 1028, 1, 1),
+                                 (1, 4, 4, 2 ** 30 + 1)])
+def test_split_refuses(bad):
+    with pytest.raises(ie.IefwdError) as e:
+        ie.test_paged_split(*bad)
+    assert e.value.status == ie.EINVAL
 
 
 def _plan(batch=4, page=16, lens=P, new=2 * P, table=P, stride=10, pages=10, ring=P, size=50, counters=P, lens_out=3 * P,
