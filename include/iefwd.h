@@ -664,7 +664,7 @@ int iefwd_paged_plan(uint32_t batch, uint32_t page_size, const int32_t *lens, co
  * iefwd_paged_plan.  A token whose slot lies outside the pool is skipped.  No
  * two tokens may have the same slot.  IEFWD_KV_E4M3: x / scale rounded to the nearest
  * (ties to even), values beyond +-448 stored as +-448, NaN as NaN.
- * n_tokens = 0 does nothing. */
+ * n_tokens at most 2^28; 0 does nothing. */
 int iefwd_paged_append(const iefwd_paged_cache *cache, const void *k, const void *v, const int64_t *slots,
                        uint32_t n_tokens, uint64_t k_stride, uint64_t v_stride, void *stream);
 
@@ -684,7 +684,7 @@ int iefwd_paged_attention_workspace(const iefwd_paged_cache *cache, uint32_t bat
  * The keys of a long request are split and joined by a rule on its length, the head
  * counts and the batch size (iefwd_test_paged_split).  workspace: iefwd_paged_attention_workspace bytes, 16-byte aligned,
  * any contents; calls that may overlap need one each.  n_heads a multiple of
- * n_kv_heads, at most 1024; 1 <= batch <= 65535; max_pages >= 1 and
+ * n_kv_heads, at most 1024; 1 <= batch <= 65535, batch * n_heads <= 2^22; max_pages >= 1 and
  * max_pages * page_size <= 2^30; scale finite. */
 int iefwd_paged_attention(const iefwd_paged_cache *cache, const void *q, uint64_t q_stride, uint32_t n_heads,
                           const int32_t *table, uint32_t table_stride, uint32_t max_pages, const int32_t *lens,

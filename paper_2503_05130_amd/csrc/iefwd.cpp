@@ -1958,6 +1958,7 @@ void check_batch_heads(uint32_t batch, uint32_t n_heads, uint32_t n_kv_heads) {
     if (batch == 0 || batch > 65535) fail(IEFWD_EINVAL, "batch must be in [1, 65535]");
     if (n_heads == 0 || n_heads > 1024 || n_kv_heads == 0 || n_heads % n_kv_heads)
         fail(IEFWD_EINVAL, "n_heads must be a multiple of n_kv_heads, at most 1024");
+    if ((uint64_t)batch * n_heads > (1u << 22)) fail(IEFWD_EINVAL, "batch * n_heads must be at most 2^22");
 }
 
 // The workspace's size, with the argument checks that it shares with the launch.
@@ -2019,7 +2020,7 @@ int iefwd_paged_append(const iefwd_paged_cache *cache, const void *k, const void
         check_row_stride("k", k, k_stride, row);
         check_row_stride("v", v, v_stride, row);
         if (!slots) fail(IEFWD_EINVAL, "slots is NULL");
-        if (n_tokens > 0x7fffffffu || (uint64_t)n_tokens * row >= (1ull << 38)) fail(IEFWD_EINVAL, "too many tokens");
+        if (n_tokens > (1u << 28)) fail(IEFWD_EINVAL, "n_tokens must be at most 2^28");
         hip_check(launch_paged_append(c, (const bf16_t *)k, (const bf16_t *)v, slots, (int)n_tokens, (int64_t)k_stride,
                                       (int64_t)v_stride, (hipStream_t)stream),
                   "paged append launch");

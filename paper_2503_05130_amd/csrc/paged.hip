@@ -165,57 +165,124 @@ __global__ __launch_bounds__(kThreads) void paged_plan_kernel(PlanArgs p) {
 }
 
 // ------------------------------------------------------------------------------ append
+//
+// A workgroup copies `tile` following tokens of one key-value head.  K: a thread takes a
+// 16-byte piece of one token; neighbouring threads take neighbouring tokens, whose pieces
+// are neighbours in a page.  V holds 4 tokens of a column together, so a thread takes 16 bytes of
+// such quads (2 or 4 columns) from 4 rows and writes them at once.  The quads are found from the slots: a unit is a
+// run of tokens in following places of one quad, whole in the middle of a prompt, a single
+// token in a decode step; one that is not whole is written element by element.
+constexpr int kAppendTile = 32;      // most tokens of a workgroup
 
+// x / scale within e4m3's range; NaN stays
 __device__ inline float to_e4m3_range(float x, float scale) {
     const float y = x / scale;
     return y != y ? y : fminf(fmaxf(y, -448.f), 448.f);
 }
 
-// One thread: 8 columns of one token and head.
+__device__ inline float bf16_of(uint32_t w, int half) { return __uint_as_float(half ? w & 0xffff0000u : w << 16); }
+
+// Two 32-bit words of bf16 pairs as 4 e4m3 values
+__device__ inline uint32_t narrow(uint32_t a, uint32_t b, float scale) {
+    const int w = __builtin_amdgcn_cvt_pk_fp8_f32(to_e4m3_range(bf16_of(a, 0), scale), to_e4m3_range(bf16_of(a, 1), scale), 0,
+                                                  false);
+    return __builtin_amdgcn_cvt_pk_fp8_f32(to_e4m3_range(bf16_of(b, 0), scale), to_e4m3_range(bf16_of(b, 1), scale), w, true);
+}
+
 template <bool E4M3>
 __global__ __launch_bounds__(kThreads) void paged_append_kernel(PagedCache c, const bf16_t *__restrict__ k,
                                                                 const bf16_t *__restrict__ v,
-                                                                const int64_t *__restrict__ slots, int tokens,
+                                                                const int64_t *__restrict__ slots, int tokens, int tile,
                                                                 int64_t k_stride, int64_t v_stride) {
-    const int per_head = c.head_dim / 8, per_token = c.kv_heads * per_head;
-    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (i >= (int64_t)tokens * per_token) return;
-    const int64_t t = i / per_token;
-    const int part = (int)(i - t * per_token), head = part / per_head, d = (part - head * per_head) * 8;
-    const int64_t slot = slots[t];
-    if (slot < 0 || slot >= ((int64_t)c.n_pages << c.page_log2)) return;
-    const int page = 1 << c.page_log2, place = (int)(slot & (page - 1));
-    const u32x4 kw = *reinterpret_cast<const u32x4 *>(k + t * k_stride + part * 8);
-    const u32x4 vw = *reinterpret_cast<const u32x4 *>(v + t * v_stride + part * 8);
-    const size_t base = ((size_t)(slot >> c.page_log2) * c.kv_heads + head) * page * c.head_dim;
-    if constexpr (!E4M3) {
-        bf16_t *kp = static_cast<bf16_t *>(c.k) + base + ((size_t)(d / 8) * page + place) * 8;
-        *reinterpret_cast<u32x4 *>(kp) = kw;
-        bf16_t *vp = static_cast<bf16_t *>(c.v) + base + ((size_t)(place / 4) * c.head_dim + d) * 4 + place % 4;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) vp[4 * e] = (bf16_t)(vw[e / 2] >> (16 * (e % 2)));
-    } else {
-        const float ks = c.k_scale[head], vs = c.v_scale[head];
-        uint32_t kq[2], vq[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            float a[4], b[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const uint32_t x = kw[2 * h + e / 2], y = vw[2 * h + e / 2];
-                a[e] = to_e4m3_range(__uint_as_float(e % 2 ? x & 0xffff0000u : x << 16), ks);
-                b[e] = to_e4m3_range(__uint_as_float(e % 2 ? y & 0xffff0000u : y << 16), vs);
-            }
-            int w = __builtin_amdgcn_cvt_pk_fp8_f32(a[0], a[1], 0, false);
-            kq[h] = __builtin_amdgcn_cvt_pk_fp8_f32(a[2], a[3], w, true);
-            w = __builtin_amdgcn_cvt_pk_fp8_f32(b[0], b[1], 0, false);
-            vq[h] = __builtin_amdgcn_cvt_pk_fp8_f32(b[2], b[3], w, true);
+    constexpr int E = E4M3 ? 16 : 8, W = E4M3 ? 4 : 2;      // columns in 16 bytes of K and (of 4 tokens) of V
+    __shared__ int64_t slot_of[kAppendTile];                // -1: outside the pool
+    __shared__ int unit[kAppendTile];                       // first token in the tile, count << 8
+    __shared__ int n_units;
+    const int tid = threadIdx.x, head = blockIdx.y, dh = c.head_dim, page = 1 << c.page_log2;
+    const int64_t t0 = (int64_t)blockIdx.x * tile, limit = (int64_t)c.n_pages << c.page_log2;
+    const int n = (int)min((int64_t)tile, tokens - t0);
+    if (tid < 64) {
+        bool starts = false;
+        int count = 1;
+        if (tid < n) {
+            const int64_t i = t0 + tid, s = slots[i];
+            const bool in = s >= 0 && s < limit;
+            slot_of[tid] = in ? s : -1;
+            // a token that follows its predecessor within a quad belongs to that one's unit, whatever tile it is in
+            starts = in && !(i > 0 && (s & 3) != 0 && slots[i - 1] == s - 1);
+            while (starts && count < 4 - (s & 3) && i + count < tokens && slots[i + count] == s + count) ++count;
         }
-        uint8_t *kp = static_cast<uint8_t *>(c.k) + base + ((size_t)(d / 16) * page + place) * 16 + d % 16;
-        *reinterpret_cast<u32x2 *>(kp) = u32x2{kq[0], kq[1]};
-        uint8_t *vp = static_cast<uint8_t *>(c.v) + base + ((size_t)(place / 4) * c.head_dim + d) * 4 + place % 4;
+        const uint64_t all = __ballot(starts);
+        if (starts) unit[__popcll(all & ((1ull << tid) - 1))] = tid | count << 8;
+        if (tid == 0) n_units = __popcll(all);
+    }
+    __syncthreads();
+    const size_t head_elems = (size_t)page * dh;
+    auto base = [&](int64_t s) { return ((size_t)(s >> c.page_log2) * c.kv_heads + head) * head_elems; };
+    // K: 16 tokens x 16 bytes a step of 16 threads
+    const float ks = E4M3 ? c.k_scale[head] : 1.f, vs = E4M3 ? c.v_scale[head] : 1.f;
+    const bf16_t *kh = k + t0 * k_stride + head * dh, *vh = v + t0 * v_stride + head * dh;
+    for (int i = tid; i < tile * (dh / E); i += kThreads) {
+        const int t = i % tile, j = i / tile;
+        if (t >= n) continue;
+        const int64_t s = slot_of[t];
+        if (s < 0) continue;
+        const u32x4 *src = reinterpret_cast<const u32x4 *>(kh + t * k_stride + j * E);
+        u32x4 x = src[0];
+        if constexpr (E4M3) {
+            const u32x4 y = src[1];
+            x = u32x4{narrow(x[0], x[1], ks), narrow(x[2], x[3], ks), narrow(y[0], y[1], ks), narrow(y[2], y[3], ks)};
+        }
+        char *dst = static_cast<char *>(c.k) + base(s) * (16 / E) + ((size_t)j * page + (s & (page - 1))) * 16;
+        *reinterpret_cast<u32x4 *>(dst) = x;
+    }
+    // V: a unit's W columns a thread
+    const int per_unit = dh / W;
+    for (int i = tid; i < n_units * per_unit; i += kThreads) {
+        const int u = i / per_unit, d = (i - u * per_unit) * W, t = unit[u] & 255, count = unit[u] >> 8;
+        const int64_t s = slot_of[t];
+        uint32_t x[4][W / 2];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) vp[4 * e] = (uint8_t)(vq[e / 4] >> (8 * (e % 4)));
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int h = 0; h < W / 2; ++h)      // rows past the unit repeat its last one and are not stored
+                x[e][h] = reinterpret_cast<const uint32_t *>(vh + (t + min(e, count - 1)) * v_stride + d)[h];
+        const int place = (int)(s & (page - 1));
+        char *dst = static_cast<char *>(c.v) + (base(s) + ((size_t)(place >> 2) * dh + d) * 4) * (16 / E);
+        // column w of the 4 rows: 4 elements that lie together
+        u32x4 q;
+        if constexpr (E4M3) {
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                float f[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) f[e] = to_e4m3_range(bf16_of(x[e][w / 2], w % 2), vs);
+                const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
+                q[w] = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], lo, true);
+            }
+        } else {
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {        // rows 2 (w % 2) and the next of column w / 2
+                const uint32_t lo = x[2 * (w % 2)][0], hi = x[2 * (w % 2) + 1][0];
+                q[w] = w / 2 ? (lo >> 16) | (hi & 0xffff0000u) : (lo & 0xffffu) | (hi << 16);
+            }
+        }
+        if (count == 4) {
+            *reinterpret_cast<u32x4 *>(dst) = q;
+            continue;
+        }
+#pragma unroll
+        for (int e = 0; e < 3; ++e) {
+            if (e >= count) break;
+            const int at = (place & 3) + e;      // the element's place in the quad; the value is row e's
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                if constexpr (E4M3)
+                    reinterpret_cast<uint8_t *>(dst)[4 * w + at] = (uint8_t)(q[w] >> (8 * e));
+                else
+                    reinterpret_cast<bf16_t *>(dst)[4 * w + at] = (bf16_t)(x[e][0] >> (16 * w));
+            }
+        }
     }
 }
 
@@ -589,11 +656,12 @@ hipError_t launch_paged_plan(const PlanArgs &p, hipStream_t stream) {
 
 hipError_t launch_paged_append(const PagedCache &c, const bf16_t *k, const bf16_t *v, const int64_t *slots, int tokens,
                                int64_t k_stride, int64_t v_stride, hipStream_t stream) {
-    const int64_t threads = (int64_t)tokens * c.kv_heads * (c.head_dim / 8);
-    const dim3 grid((unsigned)((threads + kThreads - 1) / kThreads));
-    return c.e4m3 ? launch_kernel(paged_append_kernel<true>, grid, dim3(kThreads), stream, c, k, v, slots, tokens, k_stride,
-                                  v_stride)
-                  : launch_kernel(paged_append_kernel<false>, grid, dim3(kThreads), stream, c, k, v, slots, tokens,
+    // few tokens: more workgroups of fewer
+    const int tile = (int64_t)tokens * c.kv_heads <= 16 * 1024 ? 8 : kAppendTile;
+    const dim3 grid((unsigned)((tokens + tile - 1) / tile), (unsigned)c.kv_heads);
+    return c.e4m3 ? launch_kernel(paged_append_kernel<true>, grid, dim3(kThreads), stream, c, k, v, slots, tokens, tile,
+                                  k_stride, v_stride)
+                  : launch_kernel(paged_append_kernel<false>, grid, dim3(kThreads), stream, c, k, v, slots, tokens, tile,
                                   k_stride, v_stride);
 }
 

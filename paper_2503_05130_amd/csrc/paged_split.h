@@ -24,6 +24,10 @@ inline __host__ __device__ int paged_tiles(int n_heads, int n_kv_heads) { return
 //   16 x 2000            41.5 35.2 31.3 / 32.9 31.5 31.8
 //   64 x 4000 - 8192      330  295  275 /  295  285  275
 //   96 x 5 - 12000, 16 / 4 heads of 64, e4m3   36.7 30.5 28.5 / 27.3 25.6 25.1
+//   1 x 300              8.2 in parts of 256, 6.1 in one
+// so a request of up to 512 keys is never split: the launch that joins its parts would cost more.
+constexpr int kPagedWholeLog2 = 9;
+
 struct PagedSplit {
     int log2_parts;   // up to this many parts (log2)
     int min_log2;     // of at least this many keys (log2)
@@ -39,8 +43,9 @@ inline __host__ __device__ PagedSplit paged_split(int batch, int n_heads, int n_
     return {spare < 6 ? spare : 6, 8, 8};
 }
 
-// log2 of the keys in each part of a request of n_keys >= 0 (never falls as n_keys grows)
+// log2 of the keys in each part of a request of n_keys >= 0; from 513 keys on it never falls as n_keys grows
 inline __host__ __device__ int paged_part_log2(int n_keys, PagedSplit s) {
+    if (n_keys <= 1 << kPagedWholeLog2) return kPagedWholeLog2;
     const int even = log2_up((n_keys + (1 << s.log2_parts) - 1) >> s.log2_parts);
     const int most = log2_up((n_keys + 127) >> 7);      // for 128 parts
     const int part = even < s.min_log2 ? s.min_log2 : even > 10 ? 10 : even;
@@ -49,17 +54,17 @@ inline __host__ __device__ int paged_part_log2(int n_keys, PagedSplit s) {
 
 inline __host__ __device__ int paged_parts(int n_keys, PagedSplit s) {
     const int log2 = paged_part_log2(n_keys, s);
-    return n_keys <= 1 ? 1 : (n_keys + (1 << log2) - 1) >> log2;
+    return n_keys < 1 ? 1 : (n_keys + (1 << log2) - 1) >> log2;
 }
 
 // The most parts of any request of at most max_keys.  The count falls where the part
 // doubles, so the longest request need not have the most.
 inline int paged_most_parts(int max_keys, PagedSplit s) {
     int most = 1;
-    for (int n = max_keys; n > 0;) {
+    for (int n = max_keys; n > 1 << kPagedWholeLog2;) {
         const int log2 = paged_part_log2(n, s), parts = paged_parts(n, s);
         if (parts > most) most = parts;
-        int lo = 0, hi = n - 1;                          // the longest with a smaller part, 0 if none
+        int lo = 1 << kPagedWholeLog2, hi = n - 1;       // the longest with a smaller part
         while (lo < hi) {
             const int mid = lo + (hi - lo + 1) / 2;
             if (paged_part_log2(mid, s) < log2) lo = mid;

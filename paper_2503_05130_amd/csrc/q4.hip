@@ -16,7 +16,6 @@
 namespace iefwd {
 namespace {
 
-constexpr int kWaves = 8;
 constexpr int kChunk = 128;      // weights of a feature in one block: 4 K steps of 32
 
 struct Q4Params {
@@ -66,48 +65,43 @@ __global__ __launch_bounds__(256) void q4_pack_kernel(const uint8_t *codes, cons
     }
 }
 
-template <int N>
-__device__ inline bf16x8 rotate_rows(bf16x8 v) {     // lane i of each 16 gets lane (i - N) mod 16's value
-    if constexpr (N == 0) return v;
-    u32x4 w = __builtin_bit_cast(u32x4, v);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) w[e] = __builtin_amdgcn_update_dpp(0, w[e], 0x120 + N, 0xf, 0xf, false);
-    return __builtin_bit_cast(bf16x8, w);
-}
-
 __device__ inline bf16x8 widen(uint32_t x) {
     constexpr uint32_t mask = 0x00780078u, one = 0x41804180u;
     return __builtin_bit_cast(bf16x8, u32x4{((x << 3) & mask) | one, ((x >> 1) & mask) | one, ((x >> 5) & mask) | one,
                                             ((x >> 9) & mask) | one});
 }
 
-// MC: row class (4, 8 or 16 rows).  With at most 4 (8) rows a 16-byte load per lane
-// takes a chunk's 4 (2) steps of all rows at once: lane column s MC + m holds
-// row m's piece of step s, and a rotation within the 16 lanes brings it to
-// columns 0 .. MC - 1, the only ones that are stored.
+// NL: 16-byte activation loads a lane and chunk, 4 rows each (1, 2 or 4: up to 4, 8 or 16 rows).
+// A load takes 256 consecutive bytes of each of 4 rows, 16 lanes a row: only neighbouring
+// lanes' addresses are merged, and loading a matrix operand as it stands (neighbouring lanes in
+// different rows) reached 16 bytes a clock and CU where this reaches 50.  The pieces come to
+// their lanes through 1 KB of LDS a load, the wave's own; XORed with the row, a piece's place puts the
+// 16 lanes that read together into different banks.
+// The operand's 16 rows are the 4 NL rows of A, each 4 / NL times, so that a lane's results are
+// rows NL c .. NL c + NL - 1 of one feature and nothing is computed twice but by the matrix cores.
 // T: tiles of 16 features a workgroup works on together.  U: chunks a wave requests at once.
-template <int GROUP, int MC, int T, int U>
-__global__ __launch_bounds__(64 * kWaves) void q4_kernel(Q4Params p, Epi epi) {
+template <int GROUP, int NL, int T, int U, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void q4_kernel(Q4Params p, Epi epi) {
     constexpr int GPC = kChunk / GROUP, SPG = 4 / GPC;      // groups of a chunk, steps of a group
-    constexpr int NL = MC / 4, SPL = 4 / NL;                // activation loads per chunk, steps per load
-    __shared__ f32x4 part[kWaves * T][64];
+    constexpr int kStage = NL * 1024, kLds = WAVES * (kStage > T * NL * 256 ? kStage : T * NL * 256);
+    __shared__ __attribute__((aligned(16))) char lds[kLds];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, c = lane >> 4;
     const int tile0 = blockIdx.x * T;
-    f32x4 acc[T] = {};
+    float acc[T][NL] = {};
     const bf16x8 zero = {}, ones = __builtin_bit_cast(bf16x8, u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
-    const bf16_t *arow = p.a + (size_t)min(r % MC, p.M - 1) * p.K;
-    const int k_lane = 32 * (r / MC) + 8 * c;      // of this lane's piece in a chunk, plus 32 SPL per load
+    char *stage = lds + wave * kStage;
+    const int own = r * NL / 4;                             // the row of A that this lane's operand row is
+    const bf16_t *arow[NL];
+#pragma unroll
+    for (int i = 0; i < NL; ++i) arow[i] = p.a + (size_t)min(4 * i + c, p.M - 1) * p.K;
 
     bf16x8 af[U][NL];
     u32x4 wf[U][T];
     uint32_t mf[U][T][GPC];
     auto load = [&](int u, int j) {
 #pragma unroll
-        for (int i = 0; i < NL; ++i) {
-            const int k = j * kChunk + 32 * SPL * i + k_lane;
-            af[u][i] = *reinterpret_cast<const bf16x8 *>(arow + min(k, p.K - 8));
-        }
+        for (int i = 0; i < NL; ++i) af[u][i] = *reinterpret_cast<const bf16x8 *>(arow[i] + min(j * kChunk + 8 * r, p.K - 8));
 #pragma unroll
         for (int t = 0; t < T; ++t) {
             const size_t block = (size_t)min(tile0 + t, p.N / 16 - 1) * p.chunks + j;
@@ -127,24 +121,14 @@ __global__ __launch_bounds__(64 * kWaves) void q4_kernel(Q4Params p, Epi epi) {
         }
     };
     auto use = [&](int u, int j) {
+#pragma unroll
+        for (int i = 0; i < NL; ++i)      // past K (in the last chunk) zeros
+            *reinterpret_cast<bf16x8 *>(stage + (4 * i + c) * 256 + (r ^ (4 * i + c)) * 16) =
+                j * kChunk + 8 * r < p.K ? af[u][i] : zero;
         bf16x8 a[4];
 #pragma unroll
-        for (int i = 0; i < NL; ++i) {
-            bf16x8 x = af[u][i];
-            // the part of the last chunk past K
-            if (j * kChunk + 32 * SPL * i + k_lane >= p.K) x = zero;
-            if constexpr (MC == 4) {
-                a[0] = x;
-                a[1] = rotate_rows<12>(x);
-                a[2] = rotate_rows<8>(x);
-                a[3] = rotate_rows<4>(x);
-            } else if constexpr (MC == 8) {
-                a[2 * i] = x;
-                a[2 * i + 1] = rotate_rows<8>(x);
-            } else {
-                a[i] = x;
-            }
-        }
+        for (int s = 0; s < 4; ++s)
+            a[s] = *reinterpret_cast<const bf16x8 *>(stage + own * 256 + ((4 * s + c) ^ own) * 16);
 #pragma unroll
         for (int g = 0; g < GPC; ++g) {
             f32x4 sum = {0.f, 0.f, 0.f, 0.f};
@@ -159,34 +143,38 @@ __global__ __launch_bounds__(64 * kWaves) void q4_kernel(Q4Params p, Epi epi) {
                     d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[g * SPG + s], widen(wf[u][t][g * SPG + s]), d, 0, 0, 0);
                 const float scale = __uint_as_float(mf[u][t][g] << 16), off = __uint_as_float(mf[u][t][g] & 0xffff0000u);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) acc[t][e] = fmaf(scale, fmaf(-off, sum[e], d[e]), acc[t][e]);
+                for (int e = 0; e < NL; ++e)
+                    acc[t][e] = fmaf(scale, fmaf(-off, sum[e * 4 / NL], d[e * 4 / NL]), acc[t][e]);
             }
         }
     };
-    for (int j0 = wave; j0 < p.chunks; j0 += kWaves * U) {
+    for (int j0 = wave; j0 < p.chunks; j0 += WAVES * U) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) load(u, min(j0 + u * kWaves, p.chunks - 1));
+        for (int u = 0; u < U; ++u) load(u, min(j0 + u * WAVES, p.chunks - 1));
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (j0 + u * kWaves < p.chunks) use(u, j0 + u * kWaves);
+            if (j0 + u * WAVES < p.chunks) use(u, j0 + u * WAVES);
     }
     // the waves' sums in wave order, wave t for tile t
+    float (*part)[T][NL][64] = reinterpret_cast<float (*)[T][NL][64]>(lds);
+    __syncthreads();
 #pragma unroll
-    for (int t = 0; t < T; ++t) part[wave * T + t][lane] = acc[t];
+    for (int t = 0; t < T; ++t)
+#pragma unroll
+        for (int e = 0; e < NL; ++e) part[wave][t][e][lane] = acc[t][e];
     __syncthreads();
     const int n = (tile0 + wave) * 16 + r;
     if (wave >= T || n >= p.N) return;
-    f32x4 sum = part[wave][lane];
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) sum += part[w * T + wave][lane];
-    // this lane: feature n of rows 4 c .. 4 c + 3
     const float bias = p.bias ? __uint_as_float((uint32_t)p.bias[n] << 16) : 0.f;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const int row = 4 * c + e;
+    for (int e = 0; e < NL; ++e) {
+        const int row = NL * c + e;
         if (row >= p.M) break;
+        float v = part[0][wave][e][lane];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) v += part[w][wave][e][lane];
+        v += bias;
         const size_t i = (size_t)row * p.N + n;
-        const float v = sum[e] + bias;
         if (epi == Epi::BiasResidF32)
             static_cast<float *>(p.out)[i] = p.resid[i] + v;
         else
@@ -194,29 +182,34 @@ __global__ __launch_bounds__(64 * kWaves) void q4_kernel(Q4Params p, Epi epi) {
     }
 }
 
-template <int GROUP, int MC, int T>
-hipError_t launch_q4_t(Epi epi, const Q4Params &p, hipStream_t stream) {
-    const dim3 grid((p.N / 16 + T - 1) / T), block(64 * kWaves);
-    const int per_wave = (p.chunks + kWaves - 1) / kWaves;
-    if (per_wave == 1) return launch_kernel(q4_kernel<GROUP, MC, T, 1>, grid, block, stream, p, epi);
-    if (per_wave == 2) return launch_kernel(q4_kernel<GROUP, MC, T, 2>, grid, block, stream, p, epi);
-    return launch_kernel(q4_kernel<GROUP, MC, T, 4>, grid, block, stream, p, epi);
+template <int GROUP, int NL, int T, int U, int WAVES>
+hipError_t launch_q4_w(Epi epi, const Q4Params &p, hipStream_t stream) {
+    const dim3 grid((p.N / 16 + T - 1) / T), block(64 * WAVES);
+    return launch_kernel(q4_kernel<GROUP, NL, T, U, WAVES>, grid, block, stream, p, epi);
 }
 
-template <int GROUP, int MC>
+// Two tiles a workgroup halve the reads of the activations, which each CU takes in whole, and are taken
+// where the workgroups still fill the chip; 16 waves have all of a long row in flight at once where one
+// workgroup a CU is all there is.  The waves, and with them the order of the sums, follow from N and K alone.
+// us with 8 waves and 1 tile / 8 and 2 / 16 and 1 / 16 and 2, groups of 128:
+//   1 x 1024 -> 1024    3.7  3.7  3.8  4.0     16 x 4096 -> 4096    7.2  7.9  6.7  7.8
+//   1 x 8192 -> 2048    6.9  9.2  5.5  6.3     16 x 8192 -> 2048    9.5 12.9  8.3 10.7
+//   1 x 2048 -> 8192    4.1  3.9  4.2  4.1     16 x 2048 -> 8192    5.5  5.6  5.7  5.4
+//   1 x 4096 -> 16384   9.0  8.5  9.2  8.6     16 x 4096 -> 16384  12.0 10.8 12.3 11.3
+template <int GROUP, int NL>
 hipError_t launch_q4_m(Epi epi, const Q4Params &p, hipStream_t stream) {
-    // more tiles a workgroup read the activations fewer times, while enough workgroups are left for the chip
     const int tiles = p.N / 16;
-    if (tiles >= 1024) return launch_q4_t<GROUP, MC, 4>(epi, p, stream);
-    if (tiles >= 512) return launch_q4_t<GROUP, MC, 2>(epi, p, stream);
-    return launch_q4_t<GROUP, MC, 1>(epi, p, stream);
+    if (tiles > 512) return launch_q4_w<GROUP, NL, 2, 2, 8>(epi, p, stream);
+    if (p.chunks < 16) return launch_q4_w<GROUP, NL, 1, 1, 8>(epi, p, stream);
+    if (tiles > 256) return launch_q4_w<GROUP, NL, 2, 2, 16>(epi, p, stream);
+    return launch_q4_w<GROUP, NL, 1, 1, 16>(epi, p, stream);
 }
 
 template <int GROUP>
 hipError_t launch_q4_g(Epi epi, const Q4Params &p, hipStream_t stream) {
-    if (p.M <= 4) return launch_q4_m<GROUP, 4>(epi, p, stream);
-    if (p.M <= 8) return launch_q4_m<GROUP, 8>(epi, p, stream);
-    return launch_q4_m<GROUP, 16>(epi, p, stream);
+    if (p.M <= 4) return launch_q4_m<GROUP, 1>(epi, p, stream);
+    if (p.M <= 8) return launch_q4_m<GROUP, 2>(epi, p, stream);
+    return launch_q4_m<GROUP, 4>(epi, p, stream);
 }
 
 int q4_chunks(int K) { return (K + kChunk - 1) / kChunk; }
