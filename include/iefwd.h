@@ -664,7 +664,7 @@ int iefwd_paged_plan(uint32_t batch, uint32_t page_size, const int32_t *lens, co
  * iefwd_paged_plan.  A token whose slot lies outside the pool is skipped.  No
  * two tokens may have the same slot.  IEFWD_KV_E4M3: x / scale rounded to the nearest
  * (ties to even), values beyond +-448 stored as +-448, NaN as NaN.
- * n_tokens at most 2^28; 0 does nothing. */
+ * n_tokens * n_kv_heads at most 2^28; n_tokens = 0 does nothing. */
 int iefwd_paged_append(const iefwd_paged_cache *cache, const void *k, const void *v, const int64_t *slots,
                        uint32_t n_tokens, uint64_t k_stride, uint64_t v_stride, void *stream);
 

@@ -2020,7 +2020,7 @@ int iefwd_paged_append(const iefwd_paged_cache *cache, const void *k, const void
         check_row_stride("k", k, k_stride, row);
         check_row_stride("v", v, v_stride, row);
         if (!slots) fail(IEFWD_EINVAL, "slots is NULL");
-        if (n_tokens > (1u << 28)) fail(IEFWD_EINVAL, "n_tokens must be at most 2^28");
+        if ((uint64_t)n_tokens * c.kv_heads > (1u << 28)) fail(IEFWD_EINVAL, "n_tokens * n_kv_heads must be at most 2^28");
         hip_check(launch_paged_append(c, (const bf16_t *)k, (const bf16_t *)v, slots, (int)n_tokens, (int64_t)k_stride,
                                       (int64_t)v_stride, (hipStream_t)stream),
                   "paged append launch");

@@ -13,6 +13,19 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 
+// Inclusive scan over the wave's lanes: row shifts by 1, 2, 4, 8, then lane 15's row
+// result to the next row and lane 31's to the upper half.  0 is neutral to `add`.
+template <class T, class Add>
+__device__ inline T wave_scan(T v, Add add) {
+    v = add(v, (T)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, false));
+    v = add(v, (T)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, false));
+    v = add(v, (T)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, false));
+    v = add(v, (T)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, false));
+    v = add(v, (T)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false));
+    v = add(v, (T)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false));
+    return v;
+}
+
 // ------------------------------------------------------------------------------ plan
 //
 // For request b with o cached and n wanted tokens in pages of P: it holds
@@ -23,34 +36,26 @@ constexpr int kWaves = kThreads / 64;
 // spread over the workgroups whatever request they belong to (a binary search
 // in the sums finds it), so that one long prompt is as parallel as many short
 // ones; the slot that opens a page also writes the table's entry.  One launch, no
-// scratch, no atomics: what one workgroup writes none reads.
-constexpr int kPlanSlots = 1024;   // slots a workgroup makes per round
+// scratch, no atomics between workgroups: what one writes none reads.
+//
+// The sums saturate at 2^32 - 1, which is past everything they are compared with (below 2^31);
+// saturating sums of such numbers are the same in any order.
+constexpr int kPlanGiveBack = 16;      // requests a wave looks through for pages to give back
 
-struct PlanSums {
-    int64_t tokens, taken, given;
-};
-
-__device__ inline PlanSums operator+(PlanSums a, PlanSums b) {
-    return {a.tokens + b.tokens, a.taken + b.taken, a.given + b.given};
-}
-
-__device__ inline PlanSums shift_up(PlanSums a, int by) {
-    return {__shfl_up(a.tokens, by), __shfl_up(a.taken, by), __shfl_up(a.given, by)};
-}
+__device__ inline uint32_t add_sat(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
 
 struct PlanRequest {
-    int held, want, tokens;
+    int held, want;
+    uint32_t tokens;
     bool valid;
 };
 
-__device__ inline PlanRequest plan_request(const PlanArgs &p, int b) {
-    const int o = p.lens[b], n = p.new_lens[b];
-    const int64_t cap = (int64_t)p.max_pages << p.page_log2;
+__device__ inline PlanRequest plan_request(const PlanArgs &p, int o, int n) {
+    const int cap = p.max_pages << p.page_log2, up = (1 << p.page_log2) - 1;      // at most 2^30
     PlanRequest r{0, 0, 0, o >= 0 && n >= 0 && o <= cap && n <= cap};
     if (r.valid) {
-        const int up = (1 << p.page_log2) - 1;
-        r.held = (int)(((int64_t)o + up) >> p.page_log2);
-        r.want = (int)(((int64_t)n + up) >> p.page_log2);
+        r.held = (o + up) >> p.page_log2;
+        r.want = (n + up) >> p.page_log2;
         r.tokens = n > o ? n - o : 0;
     }
     return r;
@@ -59,58 +64,69 @@ __device__ inline PlanRequest plan_request(const PlanArgs &p, int b) {
 __global__ __launch_bounds__(kThreads) void paged_plan_kernel(PlanArgs p) {
     __shared__ int ends[kPlanMaxBatch];      // new tokens up to and with request b, at most room
     __shared__ int at[kPlanMaxBatch];        // the request's first entry of the ring (taken from or given to), -1: refused
-    __shared__ PlanSums wave_sum[kWaves];
+    __shared__ uint32_t wave_sum[2][kWaves][3];
     __shared__ int granted_total[2], refused_total;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    int o = tid < p.batch ? p.lens[tid] : 0, n = tid < p.batch ? p.new_lens[tid] : 0;
     const int64_t head = p.counters[0], tail = p.counters[1];
     const bool sane = head >= 0 && tail >= head && tail - head <= p.ring_size;
-    const int64_t avail = sane ? tail - head : 0, space = sane ? p.ring_size - avail : 0;
-    const int head_at = sane ? (int)(head % p.ring_size) : 0, tail_at = sane ? (int)(tail % p.ring_size) : 0;
-
-    // each thread sums a run of requests, then the runs are scanned
-    const int run = (p.batch + kThreads - 1) / kThreads;
-    const int first = min(tid * run, p.batch), last = min(first + run, p.batch);
-    PlanSums mine{0, 0, 0};
-    for (int b = first; b < last; ++b) {
-        const PlanRequest r = plan_request(p, b);
-        mine = mine + PlanSums{r.tokens, max(0, r.want - r.held), max(0, r.held - r.want)};
-    }
-    PlanSums incl = mine;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const PlanSums below = shift_up(incl, o);
-        if (lane >= o) incl = incl + below;
-    }
-    if (lane == 63) wave_sum[wave] = incl;
+    const uint32_t avail = sane ? (uint32_t)(tail - head) : 0, space = sane ? p.ring_size - avail : 0;
+    const uint32_t head_at = sane ? (uint32_t)(head % p.ring_size) : 0, tail_at = sane ? (uint32_t)(tail % p.ring_size) : 0;
     if (tid < 2) granted_total[tid] = 0;
     if (tid == 2) refused_total = 0;
-    __syncthreads();
-    PlanSums sum{incl.tokens - mine.tokens, incl.taken - mine.taken, incl.given - mine.given};
-    for (int w = 0; w < wave; ++w) sum = sum + wave_sum[w];
-    int taken = 0, given = 0, refused = 0;
-    for (int b = first; b < last; ++b) {
-        const PlanRequest r = plan_request(p, b);
-        const int take = max(0, r.want - r.held), give = max(0, r.held - r.want);
-        const PlanSums to = sum + PlanSums{r.tokens, take, give};
-        const bool ok = r.valid && (take == 0 || to.taken <= avail) && (r.tokens == 0 || to.tokens <= p.room) &&
-                        (give == 0 || to.given <= space);
-        ends[b] = (int)min(to.tokens, (int64_t)p.room);
-        // a granted request's sums are at most the ring's size
-        const int64_t place = !ok ? -1 : give ? tail_at + sum.given : take ? head_at + sum.taken : 0;
-        at[b] = (int)(place >= p.ring_size ? place - p.ring_size : place);
-        taken += ok ? take : 0;
-        given += ok ? give : 0;
-        refused += !ok;
-        if (blockIdx.x == 0) {
-            p.lens_out[b] = ok ? p.new_lens[b] : p.lens[b];
-            p.starts[b] = (int)min(sum.tokens, (int64_t)p.room);
-            if (b == p.batch - 1) p.starts[p.batch] = ends[b];
+
+    // kThreads requests at a time; sum: of all before them
+    uint32_t sum[3] = {0, 0, 0};
+    for (int b0 = 0; b0 < p.batch; b0 += kThreads) {
+        const int b = b0 + tid, next = b + kThreads;
+        const PlanRequest r = plan_request(p, o, n);
+        const int o_now = o, n_now = n;
+        if (next < p.batch) {
+            o = p.lens[next];
+            n = p.new_lens[next];
         }
-        sum = to;
+        const bool in = b < p.batch;
+        const uint32_t take = in ? max(0, r.want - r.held) : 0, give = in ? max(0, r.held - r.want) : 0;
+        const uint32_t mine[3] = {in ? r.tokens : 0, take, give};
+        uint32_t to[3];
+        uint32_t (*waves)[3] = wave_sum[(b0 / kThreads) & 1];      // the other half may still be read
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+            to[i] = wave_scan(mine[i], add_sat);
+            if (lane == 63) waves[wave][i] = to[i];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+            uint32_t below = sum[i];
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                if (w == wave) to[i] = add_sat(below, to[i]);
+                below = add_sat(below, waves[w][i]);
+            }
+            sum[i] = below;
+        }
+        const bool ok = in && r.valid && (take == 0 || to[1] <= avail) && (r.tokens == 0 || to[0] <= (uint32_t)p.room) &&
+                        (give == 0 || to[2] <= space);
+        if (in) {
+            // where the request's own pages begin in the ring: a granted request's sums are at most the ring's size
+            const int end = (int)min(to[0], (uint32_t)p.room);
+            uint32_t place = give ? tail_at + (to[2] - give) : take ? head_at + (to[1] - take) : 0;
+            if (place >= (uint32_t)p.ring_size) place -= p.ring_size;
+            ends[b] = end;
+            at[b] = ok ? (int)place : -1;
+            if (blockIdx.x == 0) {
+                p.lens_out[b] = ok ? n_now : o_now;
+                p.starts[b + 1] = end;
+                if (b == 0) p.starts[0] = 0;
+            }
+        }
+        if (blockIdx.x == 0) {      // whole numbers in LDS: any order gives the same
+            if (ok && take) atomicAdd(&granted_total[0], (int)take);
+            if (ok && give) atomicAdd(&granted_total[1], (int)give);
+            if (in && !ok) atomicAdd(&refused_total, 1);
+        }
     }
-    if (taken) atomicAdd(&granted_total[0], taken);     // whole numbers in LDS: any order gives the same
-    if (given) atomicAdd(&granted_total[1], given);
-    if (refused) atomicAdd(&refused_total, refused);
     __syncthreads();
     if (blockIdx.x == 0 && tid == 0) {
         p.counters_out[0] = head + granted_total[0];
@@ -119,47 +135,48 @@ __global__ __launch_bounds__(kThreads) void paged_plan_kernel(PlanArgs p) {
     }
 
     // slots and the table's new entries
-    const int page = 1 << p.page_log2;
-    const int total = p.batch ? ends[p.batch - 1] : 0;
-    for (int64_t i0 = (int64_t)blockIdx.x * kPlanSlots; i0 < p.room; i0 += (int64_t)gridDim.x * kPlanSlots) {
-        for (int j = tid; j < kPlanSlots; j += kThreads) {
-            const int64_t i = i0 + j;
-            if (i >= p.room) break;
-            int64_t slot = -1;
-            if (i < total) {
-                int lo = 0, hi = p.batch - 1;            // the first request whose tokens end past i
-                while (lo < hi) {
-                    const int mid = (lo + hi) >> 1;
-                    if (ends[mid] > i) hi = mid;
-                    else lo = mid + 1;
-                }
-                if (at[lo] >= 0) {
-                    const int o = p.lens[lo];
-                    const int pos = o + (int)(i - (lo ? ends[lo - 1] : 0));
-                    const int held = (int)(((int64_t)o + page - 1) >> p.page_log2);
-                    const int column = pos >> p.page_log2;
-                    int32_t *entry = p.table + (int64_t)lo * p.table_stride + column;
-                    int32_t id;
-                    if (column < held) {
-                        id = *entry;
-                    } else {
-                        int64_t place = (int64_t)at[lo] + column - held;
-                        id = p.ring[place >= p.ring_size ? place - p.ring_size : place];
-                        if ((pos & (page - 1)) == 0) *entry = id;
-                    }
-                    if (id >= 0 && id < p.ring_size) slot = ((int64_t)id << p.page_log2) + (pos & (page - 1));
-                }
+    const int page = 1 << p.page_log2, total = ends[p.batch - 1];
+    for (int64_t i = (int64_t)blockIdx.x * kThreads + tid; i < p.room; i += (int64_t)gridDim.x * kThreads) {
+        int64_t slot = -1;
+        if (i < total) {
+            int lo = 0, hi = p.batch - 1;            // the first request whose tokens end past i
+            while (lo < hi) {
+                const int mid = (lo + hi) >> 1;
+                if (ends[mid] > i) hi = mid;
+                else lo = mid + 1;
             }
-            p.slots[i] = slot;
+            if (at[lo] >= 0) {
+                const int cached = p.lens[lo], pos = cached + (int)(i - (lo ? ends[lo - 1] : 0));
+                const int held = (cached + page - 1) >> p.page_log2, column = pos >> p.page_log2;
+                int32_t *entry = p.table + (int64_t)lo * p.table_stride + column;
+                int32_t id;
+                if (column < held) {
+                    id = *entry;
+                } else {
+                    const uint32_t place = (uint32_t)at[lo] + column - held;
+                    id = p.ring[place >= (uint32_t)p.ring_size ? place - p.ring_size : place];
+                    if ((pos & (page - 1)) == 0) *entry = id;
+                }
+                if (id >= 0 && id < p.ring_size) slot = ((int64_t)id << p.page_log2) + (pos & (page - 1));
+            }
         }
+        p.slots[i] = slot;
     }
-    // pages given back, a wave a request
-    for (int b = blockIdx.x * kWaves + wave; b < p.batch; b += gridDim.x * kWaves) {
-        const PlanRequest r = plan_request(p, b);
-        if (r.want >= r.held || at[b] < 0) continue;
-        for (int c = r.want + lane; c < r.held; c += 64) {
-            const int64_t place = (int64_t)at[b] + c - r.want;
-            p.ring[place >= p.ring_size ? place - p.ring_size : place] = p.table[(int64_t)b * p.table_stride + c];
+    // pages given back: a wave finds them among some requests and copies them one request after the other
+    for (int b0 = (blockIdx.x * kWaves + wave) * kPlanGiveBack; b0 < p.batch; b0 += gridDim.x * kWaves * kPlanGiveBack) {
+        const int b = b0 + lane;
+        const bool in = lane < kPlanGiveBack && b < p.batch;
+        const PlanRequest r = plan_request(p, in ? p.lens[b] : 0, in ? p.new_lens[b] : 0);
+        const int to = in && r.want < r.held ? at[b] : -1;
+        for (uint64_t left = __ballot(to >= 0); left; left &= left - 1) {
+            const int src = __builtin_ctzll(left);
+            const int first = __builtin_amdgcn_readlane(r.want, src), count = __builtin_amdgcn_readlane(r.held, src) - first;
+            const uint32_t begin = (uint32_t)__builtin_amdgcn_readlane(to, src);
+            const int32_t *pages = p.table + (int64_t)(b0 + src) * p.table_stride + first;
+            for (int j = lane; j < count; j += 64) {
+                const uint32_t place = begin + j;
+                p.ring[place >= (uint32_t)p.ring_size ? place - p.ring_size : place] = pages[j];
+            }
         }
     }
 }
@@ -174,16 +191,36 @@ __global__ __launch_bounds__(kThreads) void paged_plan_kernel(PlanArgs p) {
 // token in a decode step; one that is not whole is written element by element.
 constexpr int kAppendTile = 32;      // most tokens of a workgroup
 
-// x / scale within e4m3's range; NaN stays
-__device__ inline float to_e4m3_range(float x, float scale) {
-    const float y = x / scale;
-    return y != y ? y : fminf(fmaxf(y, -448.f), 448.f);
+// x / scale, rounded as a division is, within e4m3's range; NaN stays NaN.  `inv` is the
+// rounded 1 / scale: one Newton step on the quotient by its remainder gives the correctly
+// rounded one (Markstein, IBM J. Res. Dev. 34, 1990), in 3 operations for the division's dozen.
+// That holds where neither leaves fp32's range, which `near` says of the scale; then a quotient of 2^-11
+// to 512 is exact so, a larger one is cut off and a smaller one is 0 in either form.
+struct E4m3Scale {
+    float scale, inv;
+    bool near;
+};
+
+__device__ inline E4m3Scale e4m3_scale(float scale) {
+    const float size = fabsf(scale);
+    return {scale, 1.f / scale, size >= 0x1p-60f && size <= 0x1p60f};
+}
+
+__device__ inline float to_e4m3_range(float x, const E4m3Scale &s) {
+    float y;
+    if (s.near) {
+        const float q = x * s.inv;
+        y = fabsf(q) < 512.f ? fmaf(-fmaf(q, s.scale, -x), s.inv, q) : q;      // in this form -0 stays -0
+    } else {
+        y = x / s.scale;
+    }
+    return __builtin_elementwise_minimum(__builtin_elementwise_maximum(y, -448.f), 448.f);
 }
 
 __device__ inline float bf16_of(uint32_t w, int half) { return __uint_as_float(half ? w & 0xffff0000u : w << 16); }
 
 // Two 32-bit words of bf16 pairs as 4 e4m3 values
-__device__ inline uint32_t narrow(uint32_t a, uint32_t b, float scale) {
+__device__ inline uint32_t narrow(uint32_t a, uint32_t b, const E4m3Scale &scale) {
     const int w = __builtin_amdgcn_cvt_pk_fp8_f32(to_e4m3_range(bf16_of(a, 0), scale), to_e4m3_range(bf16_of(a, 1), scale), 0,
                                                   false);
     return __builtin_amdgcn_cvt_pk_fp8_f32(to_e4m3_range(bf16_of(b, 0), scale), to_e4m3_range(bf16_of(b, 1), scale), w, true);
@@ -198,20 +235,22 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(PagedCache c, co
     __shared__ int64_t slot_of[kAppendTile];                // -1: outside the pool
     __shared__ int unit[kAppendTile];                       // first token in the tile, count << 8
     __shared__ int n_units;
-    const int tid = threadIdx.x, head = blockIdx.y, dh = c.head_dim, page = 1 << c.page_log2;
-    const int64_t t0 = (int64_t)blockIdx.x * tile, limit = (int64_t)c.n_pages << c.page_log2;
-    const int n = (int)min((int64_t)tile, tokens - t0);
+    const int tid = threadIdx.x, dh = c.head_dim, page = 1 << c.page_log2;
+    // the heads of a tile next to each other: their parts of a row are neighbours in memory
+    const int64_t tile_at = blockIdx.x / c.kv_heads, t0 = tile_at * tile, limit = (int64_t)c.n_pages << c.page_log2;
+    const int head = (int)(blockIdx.x - tile_at * c.kv_heads), n = (int)min((int64_t)tile, tokens - t0);
     if (tid < 64) {
-        bool starts = false;
-        int count = 1;
-        if (tid < n) {
-            const int64_t i = t0 + tid, s = slots[i];
-            const bool in = s >= 0 && s < limit;
-            slot_of[tid] = in ? s : -1;
-            // a token that follows its predecessor within a quad belongs to that one's unit, whatever tile it is in
-            starts = in && !(i > 0 && (s & 3) != 0 && slots[i - 1] == s - 1);
-            while (starts && count < 4 - (s & 3) && i + count < tokens && slots[i + count] == s + count) ++count;
-        }
+        // lane 63: the slot before the tile; lanes up to tile + 2: the tile's and the three after it
+        const int64_t i = tid == 63 ? t0 - 1 : t0 + tid;
+        const int64_t s = i >= 0 && i < tokens && (tid < tile + 3 || tid == 63) ? slots[i] : -2;
+        const bool in = tid < n && s >= 0 && s < limit;
+        if (tid < tile) slot_of[tid] = in ? s : -1;
+        // a token that follows its predecessor within a quad belongs to that one's unit, whatever tile it is in
+        const int64_t before = __shfl(s, (tid + 63) & 63);
+        const bool follows = (s & 3) != 0 && before == s - 1;
+        const bool starts = in && !follows;
+        const uint64_t chain = __ballot(s >= 0 && s < limit && follows) >> tid;      // bit j: token tid + j follows
+        const int count = chain & 2 ? (chain & 4 ? (chain & 8 ? 4 : 3) : 2) : 1;
         const uint64_t all = __ballot(starts);
         if (starts) unit[__popcll(all & ((1ull << tid) - 1))] = tid | count << 8;
         if (tid == 0) n_units = __popcll(all);
@@ -220,7 +259,7 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(PagedCache c, co
     const size_t head_elems = (size_t)page * dh;
     auto base = [&](int64_t s) { return ((size_t)(s >> c.page_log2) * c.kv_heads + head) * head_elems; };
     // K: 16 tokens x 16 bytes a step of 16 threads
-    const float ks = E4M3 ? c.k_scale[head] : 1.f, vs = E4M3 ? c.v_scale[head] : 1.f;
+    const E4m3Scale ks = e4m3_scale(E4M3 ? c.k_scale[head] : 1.f), vs = e4m3_scale(E4M3 ? c.v_scale[head] : 1.f);
     const bf16_t *kh = k + t0 * k_stride + head * dh, *vh = v + t0 * v_stride + head * dh;
     for (int i = tid; i < tile * (dh / E); i += kThreads) {
         const int t = i % tile, j = i / tile;
@@ -324,18 +363,6 @@ __device__ inline int opaque_lane() {
     return lane;
 }
 
-// Inclusive sum over the wave's lanes: row shifts by 1, 2, 4, 8, then lane 15's row
-// total to the next row and lane 31's to the upper half.
-__device__ inline int wave_scan(int v) {
-    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
-    return v;
-}
-
 struct AttnItem {
     int b, part, keys;
 };
@@ -349,7 +376,7 @@ __device__ inline bool find_item(const AttnArgs &a, int item, int &b0, int &befo
         const bool in = b0 + lane < a.batch;
         const int n = in ? min(max(a.lens[b0 + lane], 0), a.max_keys) : 0;
         const int parts = in ? paged_parts(n, a.split) : 0;
-        const int to = before + wave_scan(parts);
+        const int to = before + wave_scan(parts, [](int x, int y) { return x + y; });
         const int total = __builtin_amdgcn_readlane(to, 63);
         if (item < total) {
             const int src = __builtin_ctzll(__ballot(to > item));
@@ -649,8 +676,9 @@ hipError_t launch_attention(const AttnArgs &a, dim3 grid, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_paged_plan(const PlanArgs &p, hipStream_t stream) {
-    // a workgroup for every kPlanSlots slots and every 16 requests, whichever is more
-    const int64_t groups = std::max<int64_t>((p.room + (int64_t)kPlanSlots - 1) / kPlanSlots, (p.batch + 15) / 16);
+    // a thread a slot, and waves for the requests, up to 4 workgroups a CU
+    const int64_t groups = std::max<int64_t>((p.room + (int64_t)kThreads - 1) / kThreads,
+                                             (p.batch + kWaves * kPlanGiveBack - 1) / (kWaves * kPlanGiveBack));
     return launch_kernel(paged_plan_kernel, dim3((unsigned)std::min<int64_t>(groups, 1024)), dim3(kThreads), stream, p);
 }
 
@@ -658,7 +686,7 @@ hipError_t launch_paged_append(const PagedCache &c, const bf16_t *k, const bf16_
                                int64_t k_stride, int64_t v_stride, hipStream_t stream) {
     // few tokens: more workgroups of fewer
     const int tile = (int64_t)tokens * c.kv_heads <= 16 * 1024 ? 8 : kAppendTile;
-    const dim3 grid((unsigned)((tokens + tile - 1) / tile), (unsigned)c.kv_heads);
+    const dim3 grid((unsigned)((tokens + tile - 1) / tile * c.kv_heads));
     return c.e4m3 ? launch_kernel(paged_append_kernel<true>, grid, dim3(kThreads), stream, c, k, v, slots, tokens, tile,
                                   k_stride, v_stride)
                   : launch_kernel(paged_append_kernel<false>, grid, dim3(kThreads), stream, c, k, v, slots, tokens, tile,

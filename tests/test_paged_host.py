@@ -63,7 +63,7 @@ def test_null_cache_and_versions():
 
 
 @pytest.mark.parametrize("bad", [dict(k=None), dict(v=None), dict(slots=None), dict(k=P + 2), dict(v=P + 8), dict(ks=255),
-                                 dict(vs=248), dict(ks=260), dict(ks=2 ** 41), dict(n=2 ** 28 + 1)])
+                                 dict(vs=248), dict(ks=260), dict(ks=2 ** 41), dict(n=2 ** 26 + 1)])
 def test_append_refuses(bad):
     assert _append(_desc(), **bad) == ie.EINVAL and ie.last_error()
 
