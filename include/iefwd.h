@@ -692,10 +692,9 @@ int iefwd_paged_attention(const iefwd_paged_cache *cache, const void *q, uint64_
                           void *stream);
 
 /* Pure host function: the keys in each part that iefwd_paged_attention splits a
- * request of n_keys into, and the waves that work on a part, for a batch of this
- * many requests.  n_keys <= 2^30, the rest as there. */
-int iefwd_test_paged_split(uint32_t batch, uint32_t n_heads, uint32_t n_kv_heads, uint32_t n_keys, uint32_t *part_keys,
-                           uint32_t *waves);
+ * request of n_keys into, in a batch of this many requests.  n_keys <= 2^30, the
+ * rest as there. */
+int iefwd_test_paged_split(uint32_t batch, uint32_t n_heads, uint32_t n_kv_heads, uint32_t n_keys, uint32_t *part_keys);
 
 /* The 4-bit form of a weight matrix W [N, K]: W[n][k] = scales[n][g] *
  * (code[n][k] - zeros[n][g]), g = k / group.  codes uint8 [N, K / 2], weight 2 i in the

@@ -94,7 +94,7 @@ SIGNATURES = {
     "iefwd_paged_append": (_i32, [_vp, _vp, _vp, _vp, _u32, _u64, _u64, _vp]),
     "iefwd_paged_attention_workspace": (_i32, [_vp, _u32, _u32, _u32, ctypes.POINTER(_sz)]),
     "iefwd_paged_attention": (_i32, [_vp, _vp, _u64, _u32, _vp, _u32, _u32, _vp, _u32, _f32, _vp, _vp, _sz, _vp]),
-    "iefwd_test_paged_split": (_i32, [_u32, _u32, _u32, _u32, ctypes.POINTER(_u32), ctypes.POINTER(_u32)]),
+    "iefwd_test_paged_split": (_i32, [_u32, _u32, _u32, _u32, ctypes.POINTER(_u32)]),
     "iefwd_q4_packed_bytes": (_i32, [_u32, _u32, _u32, ctypes.POINTER(_sz)]),
     "iefwd_q4_pack": (_i32, [_vp, _vp, _vp, _vp, _u32, _u32, _u32, _vp]),
     "iefwd_q4_gemm": (_i32, [_u32, _vp, _vp, _vp, _vp, _vp, _u32, _u32, _u32, _u32, _vp]),
@@ -616,12 +616,11 @@ def paged_plan(page_size: int, lens, new_lens, table, ring, counters, lens_out, 
           starts.data_ptr(), refused.data_ptr())
 
 
-def test_paged_split(batch: int, n_heads: int, n_kv_heads: int, n_keys: int) -> tuple[int, int]:
-    """(keys in a part, waves of a workgroup): how ``PagedCache.attention`` splits a request of n_keys."""
-    keys, waves = _u32(), _u32()
-    _check(lib().iefwd_test_paged_split(batch, n_heads, n_kv_heads, n_keys, ctypes.byref(keys), ctypes.byref(waves)),
-           "iefwd_test_paged_split")
-    return keys.value, waves.value
+def test_paged_split(batch: int, n_heads: int, n_kv_heads: int, n_keys: int) -> int:
+    """The keys in each part that ``PagedCache.attention`` splits a request of n_keys into."""
+    keys = _u32()
+    _check(lib().iefwd_test_paged_split(batch, n_heads, n_kv_heads, n_keys, ctypes.byref(keys)), "iefwd_test_paged_split")
+    return keys.value
 
 
 class Q4Weight:

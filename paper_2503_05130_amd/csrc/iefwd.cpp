@@ -2059,15 +2059,12 @@ int iefwd_paged_attention(const iefwd_paged_cache *cache, const void *q, uint64_
     });
 }
 
-int iefwd_test_paged_split(uint32_t batch, uint32_t n_heads, uint32_t n_kv_heads, uint32_t n_keys, uint32_t *part_keys,
-                           uint32_t *waves) {
+int iefwd_test_paged_split(uint32_t batch, uint32_t n_heads, uint32_t n_kv_heads, uint32_t n_keys, uint32_t *part_keys) {
     return guarded([&] {
-        if (!part_keys || !waves) fail(IEFWD_EINVAL, "NULL pointer");
+        if (!part_keys) fail(IEFWD_EINVAL, "NULL pointer");
         check_batch_heads(batch, n_heads, n_kv_heads);
         if (n_keys > (1u << 30)) fail(IEFWD_EINVAL, "n_keys must be at most 2^30");
-        const PagedSplit split = paged_split((int)batch, (int)n_heads, (int)n_kv_heads);
-        *part_keys = 1u << paged_part_log2((int)n_keys, split);
-        *waves = (uint32_t)split.waves;
+        *part_keys = 1u << paged_part_log2((int)n_keys, paged_split((int)batch, (int)n_heads, (int)n_kv_heads));
     });
 }
 

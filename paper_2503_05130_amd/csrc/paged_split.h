@@ -11,36 +11,30 @@ namespace iefwd {
 // of one MFMA operand.
 inline __host__ __device__ int paged_tiles(int n_heads, int n_kv_heads) { return (n_heads / n_kv_heads + 15) / 16; }
 
-// For `rows` = batch x key-value heads x tiles, in classes of a factor of two:
-//  - up to 256 rows (the CUs of the chip) a request is cut into up to 256 / rows
-//    parts (at most 64) of at least 256 keys, for workgroups of 8 waves, one a CU;
-//  - above, into 8 parts of at least 512, for workgroups of 4 waves.
-// A part has a power of two of keys, and at most 1024 up to 128 parts: one long
-// request among short ones must not be left to a few workgroups.
-// Measured (us, workgroups of 8 / 4 waves and parts of 256, 512, 1024 keys; 32 query and 8
-// key-value heads of 128 unless stated):
-//   1 x 4000 keys        11.1 11.6 14.0 / 11.5 12.8 16.8
-//   1 x 32001            35.3 35.3 30.9 / 31.9 32.0 31.9
-//   16 x 2000            41.5 35.2 31.3 / 32.9 31.5 31.8
-//   64 x 4000 - 8192      330  295  275 /  295  285  275
-//   96 x 5 - 12000, 16 / 4 heads of 64, e4m3   36.7 30.5 28.5 / 27.3 25.6 25.1
-//   1 x 300              8.2 in parts of 256, 6.1 in one
-// so a request of up to 512 keys is never split: the launch that joins its parts would cost more.
-constexpr int kPagedWholeLog2 = 9;
+// With `rows` = batch x key-value heads x tiles, in classes of a factor of two, a
+// request is cut into up to 256 / rows parts (at most 64), so that one request alone gives
+// every CU a workgroup.  A part has a power of two of keys, from 256 to 1024 and more only past
+// 128 parts: one long request among short ones must not be left to a few workgroups.
+// Measured with parts of 256, 512 and 1024 keys (us; 32 query and 8 key-value heads of 128 unless
+// stated):
+//   1 x 4000 keys        11.1 11.6 14.0      16 x 2000               41.5 35.2 31.3
+//   1 x 32001            35.3 35.3 30.9      64 x 4000 - 8192         330  295  275
+//   96 x 5 - 12000, 16 / 4 heads of 64, e4m3 36.7 30.5 28.5 (22.6 with fewer registers)
+// A request of up to 512 keys is never split: the launch that joins its parts would cost more
+// (1 x 300: 8.2 in parts of 256, 6.1 in one).  Workgroups of 4 waves and of 8 differ by less than 2% where
+// there are many rows; with few, 8 are up to 12% faster.
+constexpr int kPagedWholeLog2 = 9, kPagedMinLog2 = 8, kPagedMaxLog2 = 10;
 
 struct PagedSplit {
     int log2_parts;   // up to this many parts (log2)
-    int min_log2;     // of at least this many keys (log2)
-    int waves;        // of a workgroup
 };
 
 inline __host__ __device__ int log2_up(int n) { return n <= 1 ? 0 : 32 - __builtin_clz((unsigned)(n - 1)); }
 
 inline __host__ __device__ PagedSplit paged_split(int batch, int n_heads, int n_kv_heads) {
     const long rows = (long)batch * n_kv_heads * paged_tiles(n_heads, n_kv_heads);
-    if (rows > 256) return {3, 9, 4};
-    const int spare = 8 - log2_up((int)rows);
-    return {spare < 6 ? spare : 6, 8, 8};
+    const int spare = rows >= 256 ? 0 : 8 - log2_up((int)rows);
+    return {spare < 6 ? spare : 6};
 }
 
 // log2 of the keys in each part of a request of n_keys >= 0; from 513 keys on it never falls as n_keys grows
@@ -48,7 +42,7 @@ inline __host__ __device__ int paged_part_log2(int n_keys, PagedSplit s) {
     if (n_keys <= 1 << kPagedWholeLog2) return kPagedWholeLog2;
     const int even = log2_up((n_keys + (1 << s.log2_parts) - 1) >> s.log2_parts);
     const int most = log2_up((n_keys + 127) >> 7);      // for 128 parts
-    const int part = even < s.min_log2 ? s.min_log2 : even > 10 ? 10 : even;
+    const int part = even < kPagedMinLog2 ? kPagedMinLog2 : even > kPagedMaxLog2 ? kPagedMaxLog2 : even;
     return part < most ? most : part;
 }
 

@@ -274,7 +274,7 @@ def test_attention_lengths(kind, heads, kv, dim, page):
     ("e4m3", 32, 32, 64, 128, [20001, 0, 300]),
     ("bf16", 24, 1, 64, 16, [70000]),                     # two tiles of query heads
     ("e4m3", 2, 1, 64, 256, [1100000]),                   # each wave's steps looked up in two rounds
-    ("bf16", 64, 64, 64, 16, [2100, 513, 512, 511, 4097]),    # many rows: workgroups of 4 waves
+    ("bf16", 64, 64, 64, 16, [2100, 513, 512, 511, 4097]),    # many rows: parts of 1024 keys
     ("bf16", 36, 36, 128, 32, [1025, 8200, 0, 31, 33, 600, 1024, 5]),
 ])
 def test_attention_long(kind, heads, kv, dim, page, lens):
