@@ -680,7 +680,8 @@ int iefwd_paged_attention_workspace(const iefwd_paged_cache *cache, uint32_t bat
  * table int32 [batch, table_stride], max_pages columns used; lens int32 [batch].
  * Lengths are cut to [0, max_pages * page_size]; a page id outside the pool drops
  * its tokens; a row with nothing to attend to becomes zeros.  fp32 scores, softmax and
- * sums; the probabilities enter the product with V in 16 bits.
+ * sums; the probabilities enter the product with V as a bf16 and its bf16 rest, 16
+ * bits in all (an infinite element of V gives NaN).
  * The keys of a long request are split and joined by a rule on its length, the head
  * counts and the batch size (iefwd_test_paged_split).  workspace: iefwd_paged_attention_workspace bytes, 16-byte aligned,
  * any contents; calls that may overlap need one each.  n_heads a multiple of
@@ -712,7 +713,8 @@ int iefwd_q4_pack(const void *codes, const void *scales, const void *zeros, void
  * M <= 16 rows, epilogues IEFWD_EPI_BIAS_BF16, _BIAS_GELU_BF16 and
  * _BIAS_RESID_F32 and operands as for iefwd_test_gemm_skinny (a 16-byte aligned; bias may be
  * NULL: none), packed from iefwd_q4_pack.  fp32 sums; out may be resid.  A row's
- * result depends neither on the other rows nor on M. */
+ * result depends neither on the other rows nor on M.  An infinite activation
+ * gives NaN. */
 int iefwd_q4_gemm(uint32_t epilogue, const void *a, const void *packed, const void *bias, const float *resid, void *out,
                   uint32_t M, uint32_t N, uint32_t K, uint32_t group, void *stream);
 

@@ -329,7 +329,7 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(PagedCache c, co
 //
 // One query per request and head, ctx = sum_j softmax_j(scale q . k_j) v_j over
 // the request's pages.  A workgroup takes one part of one request's keys for one
-// key-value head and up to 16 of its query heads; its 8 waves take steps
+// key-value head and up to 16 of its query heads; its waves take steps
 // of 32 keys in turn, each with its own running maximum, sum and context, and
 // join them through LDS.  A request of several parts is joined by a second kernel.
 //
@@ -426,17 +426,15 @@ __device__ inline __amdgpu_buffer_rsrc_t page_buffer(const char *base, size_t at
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base + ((uint64_t)hi << 32 | lo)), 0, bytes, 0x00027000);
 }
 
-constexpr int kAttnWaves = 8;
-
-template <int DH, bool E4M3>
-__global__ __launch_bounds__(64 * kAttnWaves, 2) void paged_attention_kernel(AttnArgs a) {
+template <int DH, bool E4M3, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void paged_attention_kernel(AttnArgs a) {
     constexpr int ES = E4M3 ? 1 : 2;             // bytes per element
     constexpr int NK = DH * ES / 64;             // 16-byte loads per lane and key tile: DH columns of 16 keys
     constexpr int W = E4M3 ? 4 : 2;              // columns of V in a 16-byte load
     constexpr int NV = DH / (16 * W);            // such loads per key tile
     constexpr int ROW = DH + 4;
-    __shared__ __attribute__((aligned(16))) float o_lds[kAttnWaves][16][ROW];
-    __shared__ float m_lds[kAttnWaves][16], l_lds[kAttnWaves][16];
+    __shared__ __attribute__((aligned(16))) float o_lds[WAVES][16][ROW];
+    __shared__ float m_lds[WAVES][16], l_lds[WAVES][16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, c = lane >> 4;
     const int group = a.heads / a.c.kv_heads, tiles = (group + 15) / 16;
@@ -471,16 +469,16 @@ __global__ __launch_bounds__(64 * kAttnWaves, 2) void paged_attention_kernel(Att
         float m = -INFINITY, l = 0.f;
         f32x4 o[NV][W] = {};
         const int steps = (k1 - k0 + 31) / 32;
-        for (int s0 = 0; s0 < steps; s0 += 32 * kAttnWaves) {
+        for (int s0 = 0; s0 < steps; s0 += 32 * WAVES) {
             // lane 2 i + t: the page of key tile t of this wave's i-th step from s0 on
             int pages;
             {
-                const int key = k0 + (s0 + wave + kAttnWaves * (lane >> 1)) * 32 + (lane & 1) * 16;
+                const int key = k0 + (s0 + wave + WAVES * (lane >> 1)) * 32 + (lane & 1) * 16;
                 pages = key < k1 ? ids[key >> a.c.page_log2] : -1;
                 if (pages >= a.c.n_pages) pages = -1;
             }
-            for (int i = 0; i < 32 && s0 + wave + kAttnWaves * i < steps; ++i) {
-                const int key0 = k0 + (s0 + wave + kAttnWaves * i) * 32;
+            for (int i = 0; i < 32 && s0 + wave + WAVES * i < steps; ++i) {
+                const int key0 = k0 + (s0 + wave + WAVES * i) * 32;
                 u32x4 kr[2][NK], vr[2][NV];
                 int limit[2];     // keys of each tile that take part
 #pragma unroll
@@ -595,16 +593,16 @@ __global__ __launch_bounds__(64 * kAttnWaves, 2) void paged_attention_kernel(Att
         }
         __syncthreads();
         const bool whole = it.keys <= 1 << part_log2;
-        for (int i = wave * 64 + late; i < n_heads * (DH / 4); i += 64 * kAttnWaves) {
+        for (int i = wave * 64 + late; i < n_heads * (DH / 4); i += 64 * WAVES) {
             const int h = i / (DH / 4), d = (i - h * (DH / 4)) * 4;
             float top = m_lds[0][h];
 #pragma unroll
-            for (int w = 1; w < kAttnWaves; ++w) top = fmaxf(top, m_lds[w][h]);
+            for (int w = 1; w < WAVES; ++w) top = fmaxf(top, m_lds[w][h]);
             const float ref = top == -INFINITY ? 0.f : top;
             float sum = 0.f;
             f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int w = 0; w < kAttnWaves; ++w) {
+            for (int w = 0; w < WAVES; ++w) {
                 const float f = __builtin_amdgcn_exp2f(m_lds[w][h] - ref);
                 sum += f * l_lds[w][h];
                 acc += f * *reinterpret_cast<const f32x4 *>(&o_lds[w][h][d]);
@@ -668,7 +666,9 @@ __global__ __launch_bounds__(kThreads) void paged_join_kernel(AttnArgs a) {
 
 template <int DH, bool E4M3>
 hipError_t launch_attention(const AttnArgs &a, dim3 grid, hipStream_t stream) {
-    const hipError_t e = launch_kernel(paged_attention_kernel<DH, E4M3>, grid, dim3(64 * kAttnWaves), stream, a);
+    const hipError_t e = a.split.waves == 8
+                             ? launch_kernel(paged_attention_kernel<DH, E4M3, 8>, grid, dim3(512), stream, a)
+                             : launch_kernel(paged_attention_kernel<DH, E4M3, 2>, grid, dim3(128), stream, a);
     if (e != hipSuccess || a.slots == 1) return e;     // no request can have a second part
     return launch_kernel(paged_join_kernel<DH>, dim3(a.batch * a.heads), dim3(kThreads), stream, a);
 }

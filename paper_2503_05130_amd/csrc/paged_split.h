@@ -21,12 +21,16 @@ inline __host__ __device__ int paged_tiles(int n_heads, int n_kv_heads) { return
 //   1 x 32001            35.3 35.3 30.9      64 x 4000 - 8192         330  295  275
 //   96 x 5 - 12000, 16 / 4 heads of 64, e4m3 36.7 30.5 28.5 (22.6 with fewer registers)
 // A request of up to 512 keys is never split: the launch that joins its parts would cost more
-// (1 x 300: 8.2 in parts of 256, 6.1 in one).  Workgroups of 4 waves and of 8 differ by less than 2% where
-// there are many rows; with few, 8 are up to 12% faster.
+// (1 x 300: 8.2 in parts of 256, 6.1 in one).  
+// A workgroup has 8 waves.  From 4096 rows on, more than the chip holds several times over, it has 2: a long
+// request's rows keep it busy all the same, and a short one's leave fewer waves idle (us with 8 / 4 / 2 waves:
+// 1024 x 20 - 60 keys, 8 heads of 64, 56 / 40 / 27; 1024 x 200 - 400, 32 / 8 heads of 128, 227 / 227 / 227; but
+// 256 x 800 - 1600 235 / 240 / 249; one request of 1000 up to 12% longer with 4).
 constexpr int kPagedWholeLog2 = 9, kPagedMinLog2 = 8, kPagedMaxLog2 = 10;
 
 struct PagedSplit {
     int log2_parts;   // up to this many parts (log2)
+    int waves;        // of a workgroup
 };
 
 inline __host__ __device__ int log2_up(int n) { return n <= 1 ? 0 : 32 - __builtin_clz((unsigned)(n - 1)); }
@@ -34,7 +38,7 @@ inline __host__ __device__ int log2_up(int n) { return n <= 1 ? 0 : 32 - __built
 inline __host__ __device__ PagedSplit paged_split(int batch, int n_heads, int n_kv_heads) {
     const long rows = (long)batch * n_kv_heads * paged_tiles(n_heads, n_kv_heads);
     const int spare = rows >= 256 ? 0 : 8 - log2_up((int)rows);
-    return {spare < 6 ? spare : 6};
+    return {spare < 6 ? spare : 6, rows >= 4096 ? 2 : 8};
 }
 
 // log2 of the keys in each part of a request of n_keys >= 0; from 513 keys on it never falls as n_keys grows

@@ -289,6 +289,16 @@ def test_attention_batches(batch):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+def test_attention_of_thousands_of_rows(kind):
+    """4096 rows and more: workgroups of 2 waves, and requests of several parts among them."""
+    rng = np.random.default_rng(3)
+    lens = rng.integers(0, 60, 520)
+    lens[[0, 77, 300, 519]] = 1100, 513, 2048, 300
+    _check_attention(*_attention_case(kind, 520, 8, 8, 64, 16, lens, 21))
+    _check_attention(*_attention_case(kind, 260, 16, 16, 128, 32, lens[-260:], 22))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
 def test_attention_drops_tokens_of_pages_outside_the_pool(kind):
     _check_attention(*_attention_case(kind, 4, 8, 2, 128, 16, [16, 300, 40, 700], 5, bad_pages=True))
 
