@@ -463,7 +463,10 @@ class PagedCacheDesc(ctypes.Structure):
 def _is(t, dtype, device: int, shape) -> bool:
     """Whether t is a contiguous tensor of this type, shape and GPU.  The calls of a decode step take a few
     microseconds on the GPU, so their checks are one expression here and explained only when they fail."""
-    return isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == device and t.shape == shape and t.is_contiguous()
+    try:
+        return t.dtype is dtype and t.get_device() == device and t.shape == shape and t.is_contiguous()
+    except AttributeError:
+        return False
 
 
 def _need(name: str, t, dtype, device: int | None = None, shape=None):
@@ -499,17 +502,17 @@ def _table(table, device: int, batch: int) -> tuple[int, int]:
     return (table.stride(0) if batch > 1 else cols), cols
 
 
-# The handle of torch's current stream of a device: torch.cuda.current_stream(device).cuda_stream without the object around
-# it, which takes longer (1.7 us) than a launch does.
-_current_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else (
-    lambda device: torch.cuda.current_stream(device).cuda_stream)
+# torch's current device, and the handle of its current stream of a device: torch.cuda.current_device() and
+# torch.cuda.current_stream(device).cuda_stream without the objects around them, which take longer (1.9 us) than a launch.
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
 def _call(device: int, stream, name: str, *args) -> None:
     """Calls a library function with `device` current, on `stream` or else torch's current stream of it."""
     handle = _current_stream(device) if stream is None else _stream(stream)
     fn = getattr(_lib or lib(), name)
-    if torch.cuda.current_device() == device:
+    if _current_device() == device:
         status = fn(*args, handle)
     else:
         with torch.cuda.device(device):
@@ -643,8 +646,9 @@ class Q4Weight:
         n = _sz()
         _check(lib().iefwd_q4_packed_bytes(self.N, self.K, self.group, ctypes.byref(n)), "iefwd_q4_packed_bytes")
         self.packed = torch.empty(n.value, dtype=torch.uint8, device=self.device)
-        _call(self._dev, stream, "iefwd_q4_pack", codes.data_ptr(), scales.data_ptr(), _ptr(zeros), self.packed.data_ptr(),
-              self.N, self.K, self.group)
+        self._at = self.packed.data_ptr()
+        _call(self._dev, stream, "iefwd_q4_pack", codes.data_ptr(), scales.data_ptr(), _ptr(zeros), self._at, self.N, self.K,
+              self.group)
 
     def product(self, a, out, epilogue: int = EPI_BIAS_BF16, bias=None, resid=None, stream=None) -> None:
         """out [M, N] = epilogue(a W^T + bias), a bf16 [M, K], M <= 16; out bf16, or fp32 (as resid) for
@@ -659,7 +663,7 @@ class Q4Weight:
             if bias is not None:
                 _need("bias", bias, torch.bfloat16, dev, (n,))
             _need("resid", resid, kind, dev, (m, n))
-        _call(dev, stream, "iefwd_q4_gemm", epilogue, a.data_ptr(), self.packed.data_ptr(),
+        _call(dev, stream, "iefwd_q4_gemm", epilogue, a.data_ptr(), self._at,
               None if bias is None else bias.data_ptr(), resid.data_ptr() if f32 else None, out.data_ptr(), m, n, k, self.group)
 
 
