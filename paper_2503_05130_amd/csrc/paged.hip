@@ -189,7 +189,12 @@ __global__ __launch_bounds__(kThreads) void paged_plan_kernel(PlanArgs p) {
 // such quads (2 or 4 columns) from 4 rows and writes them at once.  The quads are found from the slots: a unit is a
 // run of tokens in following places of one quad, whole in the middle of a prompt, a single
 // token in a decode step; one that is not whole is written element by element.
+//
+// Bound by its bytes for prompts: 24001 tokens of 8 x 128 in 8 bits 32 us, 16000 in bf16 25 us (4.5 and 5.3 TB/s of reads and
+// writes, where a large copy reaches 4.8).  Pages written by much are not read soon: from kAppendStream bytes on they are
+// stored with the non-temporal hint (36 -> 32 us and 33 -> 25; but 12 MB 8.5 -> 10.0).
 constexpr int kAppendTile = 32;      // most tokens of a workgroup
+constexpr int64_t kAppendStream = 32 << 20;
 
 // x / scale, rounded as a division is, within e4m3's range; NaN stays NaN.  `inv` is the
 // rounded 1 / scale: one Newton step on the quotient by its remainder gives the correctly
@@ -226,7 +231,8 @@ __device__ inline uint32_t narrow(uint32_t a, uint32_t b, const E4m3Scale &scale
     return __builtin_amdgcn_cvt_pk_fp8_f32(to_e4m3_range(bf16_of(b, 0), scale), to_e4m3_range(bf16_of(b, 1), scale), w, true);
 }
 
-template <bool E4M3>
+// STREAM: pages are stored with the non-temporal hint.
+template <bool E4M3, bool STREAM>
 __global__ __launch_bounds__(kThreads) void paged_append_kernel(PagedCache c, const bf16_t *__restrict__ k,
                                                                 const bf16_t *__restrict__ v,
                                                                 const int64_t *__restrict__ slots, int tokens, int tile,
@@ -258,7 +264,12 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(PagedCache c, co
     __syncthreads();
     const size_t head_elems = (size_t)page * dh;
     auto base = [&](int64_t s) { return ((size_t)(s >> c.page_log2) * c.kv_heads + head) * head_elems; };
-    // K: 16 tokens x 16 bytes a step of 16 threads
+    auto store = [&](char *dst, u32x4 x) {
+        if constexpr (STREAM)
+            __builtin_nontemporal_store(x, reinterpret_cast<u32x4 *>(dst));
+        else
+            *reinterpret_cast<u32x4 *>(dst) = x;
+    };
     const E4m3Scale ks = e4m3_scale(E4M3 ? c.k_scale[head] : 1.f), vs = e4m3_scale(E4M3 ? c.v_scale[head] : 1.f);
     const bf16_t *kh = k + t0 * k_stride + head * dh, *vh = v + t0 * v_stride + head * dh;
     for (int i = tid; i < tile * (dh / E); i += kThreads) {
@@ -273,7 +284,7 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(PagedCache c, co
             x = u32x4{narrow(x[0], x[1], ks), narrow(x[2], x[3], ks), narrow(y[0], y[1], ks), narrow(y[2], y[3], ks)};
         }
         char *dst = static_cast<char *>(c.k) + base(s) * (16 / E) + ((size_t)j * page + (s & (page - 1))) * 16;
-        *reinterpret_cast<u32x4 *>(dst) = x;
+        store(dst, x);
     }
     // V: a unit's W columns a thread
     const int per_unit = dh / W;
@@ -307,7 +318,7 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(PagedCache c, co
             }
         }
         if (count == 4) {
-            *reinterpret_cast<u32x4 *>(dst) = q;
+            store(dst, q);
             continue;
         }
 #pragma unroll
@@ -426,7 +437,8 @@ __device__ inline __amdgpu_buffer_rsrc_t page_buffer(const char *base, size_t at
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base + ((uint64_t)hi << 32 | lo)), 0, bytes, 0x00027000);
 }
 
-template <int DH, bool E4M3, int WAVES>
+// STREAM: pages are read with the non-temporal hint (see kStreamBytes).
+template <int DH, bool E4M3, int WAVES, bool STREAM>
 __global__ __launch_bounds__(64 * WAVES, 2) void paged_attention_kernel(AttnArgs a) {
     constexpr int ES = E4M3 ? 1 : 2;             // bytes per element
     constexpr int NK = DH * ES / 64;             // 16-byte loads per lane and key tile: DH columns of 16 keys
@@ -490,10 +502,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attention_kernel(AttnArgs
                     const __amdgpu_buffer_rsrc_t kp = page_buffer(K, at, page_bytes), vp = page_buffer(V, at, page_bytes);
 #pragma unroll
                     for (int j = 0; j < NK; ++j)
-                        kr[t][j] = __builtin_amdgcn_raw_buffer_load_b128(kp, k_lane, off * 16 + j * 64 * page, 0);
+                        kr[t][j] = __builtin_amdgcn_raw_buffer_load_b128(kp, k_lane, off * 16 + j * 64 * page,
+                                                                         STREAM ? 2 : 0);
 #pragma unroll
                     for (int j = 0; j < NV; ++j)
-                        vr[t][j] = __builtin_amdgcn_raw_buffer_load_b128(vp, v_lane, off * DH * ES + j * 256, 0);
+                        vr[t][j] = __builtin_amdgcn_raw_buffer_load_b128(vp, v_lane, off * DH * ES + j * 256,
+                                                                         STREAM ? 2 : 0);
                 }
                 float p[8];
                 float mx = m;
@@ -664,11 +678,25 @@ __global__ __launch_bounds__(kThreads) void paged_join_kernel(AttnArgs a) {
         u32x2{pack2(acc[0] * inv, acc[1] * inv), pack2(acc[2] * inv, acc[3] * inv)};
 }
 
+// A call that may read this much is taken to stream its pages past the chip's last cache (256 MiB, for which the other
+// layers' pages compete as well), and reads them with the non-temporal hint; what a smaller one reads may still be there at the
+// next call.  us without / with the hint, calls on three caches in turn: 1534 MB 275 / 250 (6.1 TB/s, what a plain read
+// of the memory reaches), 767 MB 152 / 135, 134 MB 30.6 / 26.9, 131 MB 30.2 / 26.7; but 72 MB 22.2 / 23.7, 17 MB 10.3 / 10.8.
+constexpr int64_t kStreamBytes = 96 << 20;
+
+template <int DH, bool E4M3, int WAVES>
+hipError_t launch_attention_w(const AttnArgs &a, bool stream_pages, dim3 grid, hipStream_t stream) {
+    return stream_pages ? launch_kernel(paged_attention_kernel<DH, E4M3, WAVES, true>, grid, dim3(64 * WAVES), stream, a)
+                        : launch_kernel(paged_attention_kernel<DH, E4M3, WAVES, false>, grid, dim3(64 * WAVES), stream, a);
+}
+
 template <int DH, bool E4M3>
 hipError_t launch_attention(const AttnArgs &a, dim3 grid, hipStream_t stream) {
-    const hipError_t e = a.split.waves == 8
-                             ? launch_kernel(paged_attention_kernel<DH, E4M3, 8>, grid, dim3(512), stream, a)
-                             : launch_kernel(paged_attention_kernel<DH, E4M3, 2>, grid, dim3(128), stream, a);
+    const int64_t row = (int64_t)a.c.kv_heads * DH * (E4M3 ? 2 : 4);      // of K and V for one token
+    const int64_t pool = ((int64_t)a.c.n_pages << a.c.page_log2) * row, most = (int64_t)a.batch * a.max_keys * row;
+    const bool stream_pages = std::min(pool, most) >= kStreamBytes;
+    const hipError_t e = a.split.waves == 8 ? launch_attention_w<DH, E4M3, 8>(a, stream_pages, grid, stream)
+                                            : launch_attention_w<DH, E4M3, 2>(a, stream_pages, grid, stream);
     if (e != hipSuccess || a.slots == 1) return e;     // no request can have a second part
     return launch_kernel(paged_join_kernel<DH>, dim3(a.batch * a.heads), dim3(kThreads), stream, a);
 }
@@ -684,13 +712,16 @@ hipError_t launch_paged_plan(const PlanArgs &p, hipStream_t stream) {
 
 hipError_t launch_paged_append(const PagedCache &c, const bf16_t *k, const bf16_t *v, const int64_t *slots, int tokens,
                                int64_t k_stride, int64_t v_stride, hipStream_t stream) {
-    // few tokens: more workgroups of fewer
+    // few tokens: more workgroups of fewer (48 tokens of 8 heads 3.6 us in tiles of 8, 4.4 of 16; 24001 34 us in tiles of 32, 39
+    // of 16, 45 of 8)
     const int tile = (int64_t)tokens * c.kv_heads <= 16 * 1024 ? 8 : kAppendTile;
     const dim3 grid((unsigned)((tokens + tile - 1) / tile * c.kv_heads));
-    return c.e4m3 ? launch_kernel(paged_append_kernel<true>, grid, dim3(kThreads), stream, c, k, v, slots, tokens, tile,
-                                  k_stride, v_stride)
-                  : launch_kernel(paged_append_kernel<false>, grid, dim3(kThreads), stream, c, k, v, slots, tokens, tile,
-                                  k_stride, v_stride);
+    const bool stream_out = (int64_t)tokens * c.kv_heads * c.head_dim * (c.e4m3 ? 2 : 4) >= kAppendStream;
+    auto launch = [&](auto kernel) {
+        return launch_kernel(kernel, grid, dim3(kThreads), stream, c, k, v, slots, tokens, tile, k_stride, v_stride);
+    };
+    if (c.e4m3) return stream_out ? launch(paged_append_kernel<true, true>) : launch(paged_append_kernel<true, false>);
+    return stream_out ? launch(paged_append_kernel<false, true>) : launch(paged_append_kernel<false, false>);
 }
 
 size_t paged_workspace_floats(int batch, int heads, int kv_heads, int head_dim, int max_keys) {

@@ -142,7 +142,8 @@ def _places(c):
 
 @pytest.mark.parametrize("kind", ["bf16", "e4m3"])
 @pytest.mark.parametrize("heads,dim,page,tokens,stride", [(1, 64, 16, 1, 0), (8, 128, 16, 33, 24), (3, 64, 64, 500, 8),
-                                                          (2, 128, 256, 1203, 0), (16, 64, 32, 70, 512)])
+                                                          (2, 128, 256, 1203, 0), (16, 64, 32, 70, 512),
+                                                          (16, 128, 16, 9001, 8)])
 def test_append(kind, heads, dim, page, tokens, stride):
     g = torch.Generator().manual_seed(tokens)
     pages = tokens // page + 12
@@ -272,6 +273,8 @@ def test_attention_lengths(kind, heads, kv, dim, page):
     ("bf16", 8, 8, 128, 64, [40000]),
     ("e4m3", 4, 1, 128, 16, [131073, 3]),                 # parts longer than 1024 keys
     ("e4m3", 32, 32, 64, 128, [20001, 0, 300]),
+    ("e4m3", 8, 8, 128, 64, [52000]),                     # more than the last cache is taken to hold
+    ("bf16", 8, 8, 64, 32, [52000]),
     ("bf16", 24, 1, 64, 16, [70000]),                     # two tiles of query heads
     ("e4m3", 2, 1, 64, 256, [1100000]),                   # each wave's steps looked up in two rounds
     ("bf16", 64, 64, 64, 16, [2100, 513, 512, 511, 4097]),    # many rows: parts of 1024 keys
@@ -295,7 +298,7 @@ def test_attention_of_thousands_of_rows(kind):
     lens = rng.integers(0, 60, 520)
     lens[[0, 77, 300, 519]] = 1100, 513, 2048, 300
     _check_attention(*_attention_case(kind, 520, 8, 8, 64, 16, lens, 21))
-    _check_attention(*_attention_case(kind, 260, 16, 16, 128, 32, lens[-260:], 22))
+    _check_attention(*_attention_case(kind, 260, 16, 16, 128, 32, lens[-260:] + 60, 22))
 
 
 @pytest.mark.parametrize("kind", ["bf16", "e4m3"])
