@@ -704,7 +704,7 @@ int iefwd_test_paged_split(uint32_t batch, uint32_t n_heads, uint32_t n_kv_heads
  * out once for iefwd_q4_gemm into dst (iefwd_q4_packed_bytes bytes, 16-byte aligned): blocks of
  * 1 KB, one wave load each, with the codes of 16 features x 128 weights, then a
  * 4-byte {scale, 16 + zero} per group.  group 32, 64 or 128; N a positive
- * multiple of 16, K of 32 and of group; N * K < 2^31. */
+ * multiple of 16, K of group and at most 2^24; N * K < 2^31. */
 int iefwd_q4_packed_bytes(uint32_t N, uint32_t K, uint32_t group, size_t *bytes);   /* host only */
 int iefwd_q4_pack(const void *codes, const void *scales, const void *zeros, void *dst, uint32_t N, uint32_t K,
                   uint32_t group, void *stream);

@@ -1970,7 +1970,7 @@ size_t paged_workspace(const PagedCache &c, uint32_t batch, uint32_t n_heads, ui
 void check_q4(uint32_t N, uint32_t K, uint32_t group) {
     if (group != 32 && group != 64 && group != 128) fail(IEFWD_EINVAL, "group must be 32, 64 or 128");
     if (N == 0 || N % 16 || K == 0 || K % group) fail(IEFWD_EINVAL, "N must be a positive multiple of 16, K of group");
-    if ((uint64_t)N * K >= (1ull << 31)) fail(IEFWD_EINVAL, "too large");
+    if ((uint64_t)N * K >= (1ull << 31) || K > (1u << 24)) fail(IEFWD_EINVAL, "too large");
 }
 
 }  // namespace

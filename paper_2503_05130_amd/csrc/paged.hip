@@ -431,7 +431,7 @@ __device__ inline u32x2 widen(uint32_t w) {
 __device__ inline bf16x8 operand(u32x2 a, u32x2 b) { return __builtin_bit_cast(bf16x8, u32x4{a[0], a[1], b[0], b[1]}); }
 
 // A page of one head as a buffer: its base in scalar registers, so that a load needs one
-// 32-bit offset a lane, and nothing past the page is read.
+// 32-bit offset a lane.
 __device__ inline __amdgpu_buffer_rsrc_t page_buffer(const char *base, size_t at, uint32_t bytes) {
     const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)at), hi = __builtin_amdgcn_readfirstlane((uint32_t)(at >> 32));
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base + ((uint64_t)hi << 32 | lo)), 0, bytes, 0x00027000);

@@ -9,6 +9,12 @@
 // the second sum from a matrix product with ones.  Both sums are fp32; the
 // subtraction cancels at most the five bits that 16 + code has over code, so
 // some 19 bits of the result are left.
+//
+// Measured (us; a plain read of the same bytes, launch included, takes 7.6 for the last two): 1 x 1024 -> 1024 2.9,
+// 1 x 2048 -> 8192 3.8, 1 x 4096 -> 16384 8.4, 16 x 4096 -> 16384 10.2 and, in groups of 32, 11.1, where the vector
+// units have some 5 us of work (7 operations for 8 weights; 10 for the 4 results of a lane and group).  Short rows are bound by the
+// latency of a launch and two loads in a row.  Moving the offsets' part to a product of fp32 matrices took as many registers as it
+// saved operations (12.0); loading the next chunk before using this one made no difference at best.
 #include "q4.h"
 
 #include "gemm_device.h"
@@ -29,8 +35,8 @@ struct Q4Params {
 };
 
 // Lane l of a block holds of feature l % 16 the weights 32 s + 8 (l / 16) + e in
-// word s, e = 0 .. 7; the even ones lie in the word's low half, the odd ones in
-// its high half, so that a pair comes out as the two halves of a register.
+// word s, e = 0 .. 7; of each pair the even one lies 16 bits below the odd one, so that
+// they come out as the two halves of a register (widen).
 template <int GROUP>
 __global__ __launch_bounds__(256) void q4_pack_kernel(const uint8_t *codes, const bf16_t *scales, const uint8_t *zeros,
                                                       u32x4 *dst, uint32_t *meta, int N, int K, int chunks) {
@@ -48,8 +54,8 @@ __global__ __launch_bounds__(256) void q4_pack_kernel(const uint8_t *codes, cons
         if (k < K)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const uint32_t byte = codes[((size_t)n * K + k) / 2 + e];
-                out[s] |= (byte & 15) << (4 * e) | (byte >> 4) << (16 + 4 * e);
+                const uint32_t byte = codes[((size_t)n * K + k) / 2 + e], pair = (byte & 15) | (byte >> 4) << 16;
+                out[s] |= __builtin_rotateleft32(pair, e < 3 ? 3 + 4 * e : 31);
             }
     }
     dst[i] = out;
@@ -65,10 +71,16 @@ __global__ __launch_bounds__(256) void q4_pack_kernel(const uint8_t *codes, cons
     }
 }
 
+__device__ inline __amdgpu_buffer_rsrc_t buffer(const void *p, uint32_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, bytes, 0x00027000);
+}
+
+// The eight weights of a word: pair e sits at bits 3 + 4 e of each half (the last one
+// wrapped round the word), so that only three of the four need a shift.
 __device__ inline bf16x8 widen(uint32_t x) {
-    constexpr uint32_t mask = 0x00780078u, one = 0x41804180u;
-    return __builtin_bit_cast(bf16x8, u32x4{((x << 3) & mask) | one, ((x >> 1) & mask) | one, ((x >> 5) & mask) | one,
-                                            ((x >> 9) & mask) | one});
+    constexpr uint32_t mask = 0x00780078u, base = 0x41804180u;
+    return __builtin_bit_cast(bf16x8, u32x4{(x & mask) | base, ((x >> 4) & mask) | base, ((x >> 8) & mask) | base,
+                                            (__builtin_rotateleft32(x, 4) & mask) | base});
 }
 
 // NL: 16-byte activation loads a lane and chunk, 4 rows each (1, 2 or 4: up to 4, 8 or 16 rows).
@@ -79,8 +91,8 @@ __device__ inline bf16x8 widen(uint32_t x) {
 // 16 lanes that read together into different banks.
 // The operand's 16 rows are the 4 NL rows of A, each 4 / NL times, so that a lane's results are
 // rows NL c .. NL c + NL - 1 of one feature and nothing is computed twice but by the matrix cores.
-// T: tiles of 16 features a workgroup works on together.  U: chunks a wave requests at once.
-template <int GROUP, int NL, int T, int U, int WAVES>
+// T: tiles of 16 features a workgroup works on together.
+template <int GROUP, int NL, int T, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void q4_kernel(Q4Params p, Epi epi) {
     constexpr int GPC = kChunk / GROUP, SPG = 4 / GPC;      // groups of a chunk, steps of a group
     constexpr int kStage = NL * 1024, kLds = WAVES * (kStage > T * NL * 256 ? kStage : T * NL * 256);
@@ -88,43 +100,56 @@ __global__ __launch_bounds__(64 * WAVES) void q4_kernel(Q4Params p, Epi epi) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, c = lane >> 4;
     const int tile0 = blockIdx.x * T;
-    float acc[T][NL] = {};
-    const bf16x8 zero = {}, ones = __builtin_bit_cast(bf16x8, u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
+    f32x4 acc[T] = {};
+    const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
     char *stage = lds + wave * kStage;
     const int own = r * NL / 4;                             // the row of A that this lane's operand row is
-    const bf16_t *arow[NL];
+    // Operands as buffers: a scalar base and step, one 32-bit offset a lane.  Every offset lies inside
+    // them by itself: a tile past N reads the last one's operands and is not stored.
+    const int n_tiles = min(T, p.N / 16 - tile0);
+    const size_t block0 = (size_t)tile0 * p.chunks;
+    const __amdgpu_buffer_rsrc_t a_buf = buffer(p.a, (uint32_t)p.M * p.K * 2);
+    const __amdgpu_buffer_rsrc_t code_buf = buffer(p.codes + block0 * 64, (uint32_t)n_tiles * p.chunks * 1024);
+    const __amdgpu_buffer_rsrc_t meta_buf = buffer(p.meta + block0 * 16 * GPC, (uint32_t)n_tiles * p.chunks * 64 * GPC);
+    uint32_t a_lane[NL];
 #pragma unroll
-    for (int i = 0; i < NL; ++i) arow[i] = p.a + (size_t)min(4 * i + c, p.M - 1) * p.K;
+    for (int i = 0; i < NL; ++i) a_lane[i] = (uint32_t)min(4 * i + c, p.M - 1) * p.K * 2 + r * 16;
 
-    bf16x8 af[U][NL];
-    u32x4 wf[U][T];
-    uint32_t mf[U][T][GPC];
-    auto load = [&](int u, int j) {
+    // this lane's piece of chunk j lies past K: the chunk's first is read in its place and not used
+    auto past = [&](int j) { return (j + 1) * kChunk > p.K && j * kChunk + 8 * r >= p.K; };
+
+    u32x4 af[NL], wf[T];
+    uint32_t mf[T][GPC];
+    auto load = [&](int j) {
 #pragma unroll
-        for (int i = 0; i < NL; ++i) af[u][i] = *reinterpret_cast<const bf16x8 *>(arow[i] + min(j * kChunk + 8 * r, p.K - 8));
+        for (int i = 0; i < NL; ++i)
+            af[i] = __builtin_amdgcn_raw_buffer_load_b128(a_buf, a_lane[i] - (past(j) ? r * 16 : 0), j * 256, 0);
 #pragma unroll
         for (int t = 0; t < T; ++t) {
-            const size_t block = (size_t)min(tile0 + t, p.N / 16 - 1) * p.chunks + j;
-            wf[u][t] = p.codes[block * 64 + lane];
-            const uint32_t *m = p.meta + (block * 16 + r) * GPC;
+            const int block = min(t, n_tiles - 1) * p.chunks + j;
+            wf[t] = __builtin_amdgcn_raw_buffer_load_b128(code_buf, lane * 16, block * 1024, 0);
             if constexpr (GPC == 4) {
-                const u32x4 x = *reinterpret_cast<const u32x4 *>(m);
+                const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(meta_buf, r * 16, block * 256, 0);
 #pragma unroll
-                for (int g = 0; g < 4; ++g) mf[u][t][g] = x[g];
+                for (int g = 0; g < 4; ++g) mf[t][g] = x[g];
             } else if constexpr (GPC == 2) {
-                const u32x2 x = *reinterpret_cast<const u32x2 *>(m);
-                mf[u][t][0] = x[0];
-                mf[u][t][1] = x[1];
+                const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(meta_buf, r * 8, block * 128, 0);
+                mf[t][0] = x[0];
+                mf[t][1] = x[1];
             } else {
-                mf[u][t][0] = *m;
+                mf[t][0] = __builtin_amdgcn_raw_buffer_load_b32(meta_buf, r * 4, block * 64, 0);
             }
         }
     };
-    auto use = [&](int u, int j) {
+    auto use = [&](int j) {
+        if ((j + 1) * kChunk > p.K) {
 #pragma unroll
-        for (int i = 0; i < NL; ++i)      // past K (in the last chunk) zeros
-            *reinterpret_cast<bf16x8 *>(stage + (4 * i + c) * 256 + (r ^ (4 * i + c)) * 16) =
-                j * kChunk + 8 * r < p.K ? af[u][i] : zero;
+            for (int i = 0; i < NL; ++i)
+                if (past(j)) af[i] = u32x4{0, 0, 0, 0};
+        }
+#pragma unroll
+        for (int i = 0; i < NL; ++i)
+            *reinterpret_cast<u32x4 *>(stage + (4 * i + c) * 256 + (r ^ (4 * i + c)) * 16) = af[i];
         bf16x8 a[4];
 #pragma unroll
         for (int s = 0; s < 4; ++s)
@@ -140,20 +165,17 @@ __global__ __launch_bounds__(64 * WAVES) void q4_kernel(Q4Params p, Epi epi) {
                 f32x4 d = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int s = 0; s < SPG; ++s)
-                    d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[g * SPG + s], widen(wf[u][t][g * SPG + s]), d, 0, 0, 0);
-                const float scale = __uint_as_float(mf[u][t][g] << 16), off = __uint_as_float(mf[u][t][g] & 0xffff0000u);
+                    d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[g * SPG + s], widen(wf[t][g * SPG + s]), d, 0, 0, 0);
+                const float scale = __uint_as_float(mf[t][g] << 16), off = __uint_as_float(mf[t][g] & 0xffff0000u);
 #pragma unroll
                 for (int e = 0; e < NL; ++e)
-                    acc[t][e] = fmaf(scale, fmaf(-off, sum[e * 4 / NL], d[e * 4 / NL]), acc[t][e]);
+                    acc[t][e * 4 / NL] = fmaf(scale, fmaf(-off, sum[e * 4 / NL], d[e * 4 / NL]), acc[t][e * 4 / NL]);
             }
         }
     };
-    for (int j0 = wave; j0 < p.chunks; j0 += WAVES * U) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) load(u, min(j0 + u * WAVES, p.chunks - 1));
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (j0 + u * WAVES < p.chunks) use(u, j0 + u * WAVES);
+    for (int j = wave; j < p.chunks; j += WAVES) {
+        load(j);
+        use(j);
     }
     // the waves' sums in wave order, wave t for tile t
     float (*part)[T][NL][64] = reinterpret_cast<float (*)[T][NL][64]>(lds);
@@ -161,7 +183,7 @@ __global__ __launch_bounds__(64 * WAVES) void q4_kernel(Q4Params p, Epi epi) {
 #pragma unroll
     for (int t = 0; t < T; ++t)
 #pragma unroll
-        for (int e = 0; e < NL; ++e) part[wave][t][e][lane] = acc[t][e];
+        for (int e = 0; e < NL; ++e) part[wave][t][e][lane] = acc[t][e * 4 / NL];
     __syncthreads();
     const int n = (tile0 + wave) * 16 + r;
     if (wave >= T || n >= p.N) return;
@@ -182,16 +204,16 @@ __global__ __launch_bounds__(64 * WAVES) void q4_kernel(Q4Params p, Epi epi) {
     }
 }
 
-template <int GROUP, int NL, int T, int U, int WAVES>
+template <int GROUP, int NL, int T, int WAVES>
 hipError_t launch_q4_w(Epi epi, const Q4Params &p, hipStream_t stream) {
     const dim3 grid((p.N / 16 + T - 1) / T), block(64 * WAVES);
-    return launch_kernel(q4_kernel<GROUP, NL, T, U, WAVES>, grid, block, stream, p, epi);
+    return launch_kernel(q4_kernel<GROUP, NL, T, WAVES>, grid, block, stream, p, epi);
 }
 
 // Two tiles a workgroup halve the reads of the activations, which each CU takes in whole, and are taken
-// where the workgroups still fill the chip; 16 waves have all of a long row in flight at once where one
-// workgroup a CU is all there is.  The waves, and with them the order of the sums, follow from N and K alone.
-// us with 8 waves and 1 tile / 8 and 2 / 16 and 1 / 16 and 2, groups of 128:
+// where the workgroups still fill the chip; 16 waves have more of a long row in flight where one workgroup a
+// CU is all there is.  The waves, and with them the order of the sums, follow from N and K alone.
+// us with 8 waves and 1 tile / 8 and 2 / 16 and 1 / 16 and 2, groups of 128 (a form with addresses in vector registers):
 //   1 x 1024 -> 1024    3.7  3.7  3.8  4.0     16 x 4096 -> 4096    7.2  7.9  6.7  7.8
 //   1 x 8192 -> 2048    6.9  9.2  5.5  6.3     16 x 8192 -> 2048    9.5 12.9  8.3 10.7
 //   1 x 2048 -> 8192    4.1  3.9  4.2  4.1     16 x 2048 -> 8192    5.5  5.6  5.7  5.4
@@ -199,10 +221,10 @@ hipError_t launch_q4_w(Epi epi, const Q4Params &p, hipStream_t stream) {
 template <int GROUP, int NL>
 hipError_t launch_q4_m(Epi epi, const Q4Params &p, hipStream_t stream) {
     const int tiles = p.N / 16;
-    if (tiles > 512) return launch_q4_w<GROUP, NL, 2, 2, 8>(epi, p, stream);
-    if (p.chunks < 16) return launch_q4_w<GROUP, NL, 1, 1, 8>(epi, p, stream);
-    if (tiles > 256) return launch_q4_w<GROUP, NL, 2, 2, 16>(epi, p, stream);
-    return launch_q4_w<GROUP, NL, 1, 1, 16>(epi, p, stream);
+    if (tiles > 512) return launch_q4_w<GROUP, NL, 2, 8>(epi, p, stream);
+    if (p.chunks < 16) return launch_q4_w<GROUP, NL, 1, 8>(epi, p, stream);
+    if (tiles > 256) return launch_q4_w<GROUP, NL, 2, 16>(epi, p, stream);
+    return launch_q4_w<GROUP, NL, 1, 16>(epi, p, stream);
 }
 
 template <int GROUP>

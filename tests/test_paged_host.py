@@ -126,7 +126,7 @@ def test_plan_refuses(bad):
     assert _plan(**bad) == ie.EINVAL and ie.last_error()
 
 
-SHAPES = [dict(N=0), dict(N=24), dict(K=0), dict(K=96), dict(group=16), dict(group=256), dict(group=0), dict(N=2 ** 20, K=2 ** 12)]
+SHAPES = [dict(N=0), dict(N=24), dict(K=0), dict(K=96), dict(group=16), dict(group=256), dict(group=0), dict(N=2 ** 20, K=2 ** 12), dict(N=16, K=2 ** 24 + 128)]
 
 
 def _bytes(N=32, K=128, group=64):
