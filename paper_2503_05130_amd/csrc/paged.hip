@@ -38,6 +38,9 @@ __device__ inline T wave_scan(T v, Add add) {
 // ones; the slot that opens a page also writes the table's entry.  One launch, no
 // scratch, no atomics between workgroups: what one writes none reads.
 //
+// Bound by latency, a launch and four loads that depend on each other (lengths, LDS sums, ring or table entry): 4 requests 3.0 us,
+// 512 of which 16 end 5.4, 192 prompts with 90000 slots 4.8.
+//
 // The sums saturate at 2^32 - 1, which is past everything they are compared with (below 2^31);
 // saturating sums of such numbers are the same in any order.
 constexpr int kPlanGiveBack = 16;      // requests a wave looks through for pages to give back
@@ -190,9 +193,10 @@ __global__ __launch_bounds__(kThreads) void paged_plan_kernel(PlanArgs p) {
 // run of tokens in following places of one quad, whole in the middle of a prompt, a single
 // token in a decode step; one that is not whole is written element by element.
 //
-// Bound by its bytes for prompts: 24001 tokens of 8 x 128 in 8 bits 32 us, 16000 in bf16 25 us (4.5 and 5.3 TB/s of reads and
+// Bound by its bytes for prompts: 24001 tokens of 8 x 128 in 8 bits 31 us, 16000 in bf16 23 us (4.8 and 5.7 TB/s of reads and
 // writes, where a large copy reaches 4.8).  Pages written by much are not read soon: from kAppendStream bytes on they are
-// stored with the non-temporal hint (36 -> 32 us and 33 -> 25; but 12 MB 8.5 -> 10.0).
+// stored with the non-temporal hint (36 -> 32 us and 33 -> 23; but 12 MB 8.5 -> 10.0).  48 tokens of a decode step take 3.6 us,
+// a launch and two loads in a row.
 constexpr int kAppendTile = 32;      // most tokens of a workgroup
 constexpr int64_t kAppendStream = 32 << 20;
 
@@ -351,7 +355,14 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(PagedCache c, co
 // operand, so the probabilities never leave the lane's registers; the
 // pages are laid out so that K's and V's operands are 16-byte loads in the
 // same sense.  P goes in as two bf16 numbers, the rounded value and the rounded
-// rest, which keeps 16 bits of it for two products where there is ample room.
+// rest, which keeps 16 bits of it for two products where there is ample room (the matrix cores
+// are busy for 7% of the time).
+//
+// Bound by reading the pages once: 64 requests of 4000 - 8192 keys, 32 / 8 heads of 128, 246 us with the joining kernel (6.2
+// TB/s, what a plain read reaches), in 8 bits 135 us; one request of 32001 keys 26 us (5.0 TB/s); 96 of 5 - 12000, 16 / 4 heads
+// of 64 in 8 bits, 22 us (3.3 TB/s: 784 workgroups in one round, whose longest have 4 steps in a row, and 4 us of joining).
+// Not kept: K of the next step requested before this step's V is used, and 2 or 4 steps at once (249 registers and 18% slower
+// in bf16, no faster in 8 bits).
 struct AttnArgs {
     PagedCache c;
     const bf16_t *q;

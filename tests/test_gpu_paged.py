@@ -506,3 +506,76 @@ def test_runs_on_the_current_or_given_stream():
             ops["cache"].attention(late, ops["table"], ops["lens"], ops["out"][:2], ws, stream=s)
         sync()
         assert torch.equal(ops["out"][:2], want)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+def test_a_decoder_block_of_4_bit_products_over_the_cache(kind):
+    """The QKV product, plan, append, attention and the out-projection with its residual, a token after the other for
+    requests of different lengths; each product and context against 64 bits on the inputs that it had."""
+    batch, d, heads, kv, dim, page = 5, 256, 4, 2, 64, 16
+    s = _Server(kind, batch, heads, kv, dim, page, 80, 25, 6)
+    g = torch.Generator().manual_seed(17)
+
+    def weight(n, k, group):
+        codes = torch.randint(0, 256, (n, k // 2), generator=g, dtype=torch.uint8)
+        scales = (0.02 * (0.5 + torch.rand(n, k // group, generator=g))).bfloat16()
+        w = P.q4_weight(codes.numpy(), f64(scales), None)
+        return ie.Q4Weight(codes.to(DEV), scales.to(DEV)), w, f64(scales), group
+
+    def bound(a, scales, group, y):       # as in the product's own tests
+        mag = np.abs(a).reshape(len(a), -1, group).sum(-1) @ np.abs(scales).T
+        return 2.0 ** -24 * (62 * (group + 4) + 16 * scales.shape[1]) * mag + 2.0 ** -22 * np.abs(y)
+
+    qkv_w, out_w = weight((heads + 2 * kv) * dim, d, 64), weight(d, heads * dim, 128)
+    bias = torch.randn((heads + 2 * kv) * dim, generator=g).bfloat16().to(DEV)
+    lens = [0, 250, 16, 31, 256]                                     # prompts first, with keys and values as they come
+    n = sum(lens)
+    pk, pv = (torch.randn(n, kv, dim, generator=g).bfloat16().to(DEV) for _ in range(2))
+    s.new.copy_(torch.tensor(lens, dtype=torch.int32))
+    out = torch.empty(batch, heads * dim, dtype=torch.bfloat16, device=DEV)
+    s.step(torch.zeros_like(out), pk, pv, torch.empty(n, dtype=torch.int64, device=DEV), out)
+    s.swap()
+    qkv = torch.empty(batch, (heads + 2 * kv) * dim, dtype=torch.bfloat16, device=DEV)
+    slots = torch.empty(batch, dtype=torch.int64, device=DEV)
+    x, h = torch.empty(batch, d, dtype=torch.bfloat16, device=DEV), torch.empty(batch, d, device=DEV)
+    sync()
+
+    def block():
+        s.new.copy_(s.lens + 1)
+        qkv_w[0].product(x, qkv, bias=bias)
+        q, k, v = qkv.split([heads * dim, kv * dim, kv * dim], 1)
+        s.step(q, k, v, slots, out)
+        out_w[0].product(out, h, ie.EPI_BIAS_RESID_F32, resid=h)
+        s.swap()
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        block()
+    rounds = []
+    for step in range(4):
+        x.copy_(torch.randn(batch, d, generator=g).bfloat16())
+        h.copy_(torch.randn(batch, d, generator=g))
+        before = f64(h)
+        graph.replay() if step % 2 else block()
+        sync()
+        y = f64(x) @ qkv_w[1].T + f64(bias)
+        assert (np.abs(f64(qkv) - y) <= bound(f64(x), *qkv_w[2:], y) + 2.0 ** -8 * np.abs(y)).all()
+        rounds.append(f64(qkv))
+        assert s.lens.tolist() == [m + step + 1 for m in lens] and int(s.refused) == 0
+        at = 0
+        for b, m in enumerate(lens):
+            dense = []
+            for old, lo, scale in ((pk, heads * dim, s.c.k_scale), (pv, (heads + kv) * dim, s.c.v_scale)):
+                t = np.concatenate([f64(old)[at:at + m]] + [r[b, lo:lo + kv * dim].reshape(1, kv, dim) for r in rounds])
+                if kind == "e4m3":
+                    sc = scale.cpu().view(1, -1, 1)
+                    t = ((torch.from_numpy(t).float() / sc).clamp(-448, 448).to(torch.float8_e4m3fn).double() * sc.double()).numpy()
+                dense.append(t[None])
+            at += m
+            keys = m + step + 1
+            ref, mag, dots = P.attention(rounds[-1][b, :heads * dim].reshape(1, heads, dim), *dense, np.zeros((1, 1), int), [keys],
+                                         dim ** -0.5)
+            tol = P.attention_tolerance(ref, mag, dots, keys, dim, dim ** -0.5)
+            assert (np.abs(f64(out[b]).reshape(1, heads, dim) - ref) <= tol).all()
+        y = f64(out) @ out_w[1].T
+        assert (np.abs(f64(h) - before - y) <= bound(f64(out), *out_w[2:], y) + 2.0 ** -23 * (np.abs(before) + np.abs(y))).all()
