@@ -23,7 +23,7 @@ LIB = os.path.join(HERE, "libiefwd.so")
 ARCH = "gfx950"
 
 SOURCES = ["gemm.hip", "attention.hip", "decode.hip", "layernorm.hip", "train.hip", "paged.hip", "q4.hip", "quota.cpp", "controller.cpp", "init_weights.cpp",
-           "iefwd.cpp"]
+           "iefwd.cpp", "paged_abi.cpp"]
 
 COMMON = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Werror",
