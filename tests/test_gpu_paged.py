@@ -579,3 +579,48 @@ def test_a_decoder_block_of_4_bit_products_over_the_cache(kind):
             assert (np.abs(f64(out[b]).reshape(1, heads, dim) - ref) <= tol).all()
         y = f64(out) @ out_w[1].T
         assert (np.abs(f64(h) - before - y) <= bound(f64(out), *out_w[2:], y) + 2.0 ** -23 * (np.abs(before) + np.abs(y))).all()
+
+
+def test_two_calls_at_once_on_streams_of_their_own():
+    ops, _ = _attention_case("bf16", 6, 8, 2, 128, 16, [5000, 40, 700, 0, 2049, 513], 31)
+    want = _attend(ops).clone()
+    c, streams = ops["cache"], [torch.cuda.Stream() for _ in range(2)]
+    outs = [torch.zeros(6, 8, 128, dtype=torch.bfloat16, device=DEV) for _ in streams]
+    spaces = [c.workspace(6, 8, ops["table"].shape[1]) for _ in streams]
+    sync()
+    for _ in range(5):
+        for s, o, w in zip(streams, outs, spaces):
+            c.attention(ops["q"], ops["table"], ops["lens"], o, w, stream=s)
+    sync()
+    assert all(torch.equal(o, want) for o in outs)
+
+
+def test_the_binding_refuses_other_types_shapes_and_sizes():
+    ops, _ = _attention_case("bf16", 2, 4, 2, 64, 16, [2000, 30], 13)
+    c, q, table, lens = (ops[k] for k in ("cache", "q", "table", "lens"))
+    out, ws = torch.full((2, 4, 64), 9.0, dtype=torch.bfloat16, device=DEV), c.workspace(2, 4, table.shape[1])
+    bad = [dict(q=q.float()), dict(q=q[:1]), dict(q=q.cpu()), dict(q=q[:, ::2]), dict(table=table.long()), dict(table=table[:1]),
+           dict(table=table.t().contiguous().t()), dict(lens=lens.long()), dict(lens=lens[::2]), dict(lens=lens[:, None]),
+           dict(out=out.float()), dict(out=out[:, :, ::2]), dict(out=out[:1]), dict(workspace=ws.float())]
+    for b in bad:
+        args = dict(dict(q=q, table=table, lens=lens, out=out, workspace=ws), **b)
+        with pytest.raises(ValueError):
+            c.attention(**args)
+    with pytest.raises(ie.IefwdError) as e:
+        c.attention(q, table, lens, out, ws[:-16])
+    assert e.value.status == ie.EINVAL and "workspace" in str(e.value)
+    with pytest.raises(ie.IefwdError):
+        c.attention(q, table, lens, out, ws, scale=float("nan"))
+    k = torch.zeros(3, 2, 64, dtype=torch.bfloat16, device=DEV)
+    slots = torch.zeros(3, dtype=torch.int64, device=DEV)
+    for b in (dict(k=k.half()), dict(k=k[:2]), dict(v=k.transpose(1, 2)), dict(slots=slots.int()), dict(slots=slots[::2])):
+        with pytest.raises(ValueError):
+            c.append(**dict(dict(k=k, v=k, slots=slots), **b))
+    with pytest.raises(ValueError):
+        ie.PagedCache(c.k, c.v[:1])
+    with pytest.raises(ValueError):
+        ie.PagedCache(c.k, c.v, torch.ones(2, device=DEV), torch.ones(2, device=DEV))
+    with pytest.raises(ValueError):
+        ie.PagedCache(c.k.view(torch.float8_e4m3fn), c.v.view(torch.float8_e4m3fn))
+    sync()
+    assert (out == 9.0).all()
