@@ -647,8 +647,10 @@ typedef struct iefwd_paged_cache {
  *   refused   int32 [1]: number of refused requests
  * Requests are served in order.  One that needs pages is refused when the free
  * pages do not suffice for it and all before it together, one with new tokens
- * when its slots end past max_new, and one whose lengths lie outside [0, max_pages *
- * page_size]; it keeps its length and pages.  lens_out must not be lens or new_lens and
+ * when its slots end past max_new, one that gives pages back when the ring has no room
+ * for them, and one whose lengths lie outside [0, max_pages * page_size]; it keeps its
+ * length and pages.  With counters that are not 0 <= head <= tail <= head + ring_size
+ * nothing is taken or given back.  lens_out must not be lens or new_lens and
  * counters_out not counters (they swap roles from call to call); a call on
  * the same inputs again gives the same outputs.  A page in the table belongs to one
  * request.  1 <= batch <= 4096; page_size as above; max_pages * page_size <= 2^30;
@@ -683,8 +685,8 @@ int iefwd_paged_attention_workspace(const iefwd_paged_cache *cache, uint32_t bat
  * sums; the probabilities enter the product with V as a bf16 and its bf16 rest, 16
  * bits in all (an infinite element of V gives NaN).
  * The keys of a long request are split and joined by a rule on its length, the head
- * counts and the batch size (iefwd_test_paged_split).  workspace: iefwd_paged_attention_workspace bytes, 16-byte aligned,
- * any contents; calls that may overlap need one each.  n_heads a multiple of
+ * counts and the batch size (iefwd_test_paged_split).  workspace:
+ * iefwd_paged_attention_workspace bytes, 16-byte aligned, any contents; calls that may overlap need one each.  n_heads a multiple of
  * n_kv_heads, at most 1024; 1 <= batch <= 65535, batch * n_heads <= 2^22; max_pages >= 1 and
  * max_pages * page_size <= 2^30; scale finite. */
 int iefwd_paged_attention(const iefwd_paged_cache *cache, const void *q, uint64_t q_stride, uint32_t n_heads,
@@ -712,7 +714,7 @@ int iefwd_q4_pack(const void *codes, const void *scales, const void *zeros, void
 /* The decode-step product with 4-bit weights: out = epilogue(A W^T + b) for
  * M <= 16 rows, epilogues IEFWD_EPI_BIAS_BF16, _BIAS_GELU_BF16 and
  * _BIAS_RESID_F32 and operands as for iefwd_test_gemm_skinny (a 16-byte aligned; bias may be
- * NULL: none), packed from iefwd_q4_pack.  fp32 sums; out may be resid.  A row's
+ * NULL: none), packed from iefwd_q4_pack for the same N, K and group.  fp32 sums; out may be resid.  A row's
  * result depends neither on the other rows nor on M.  An infinite activation
  * gives NaN. */
 int iefwd_q4_gemm(uint32_t epilogue, const void *a, const void *packed, const void *bias, const float *resid, void *out,
