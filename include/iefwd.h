@@ -705,7 +705,7 @@ int iefwd_test_paged_split(uint32_t batch, uint32_t n_heads, uint32_t n_kv_heads
  * uint8 [N, K / group] in 0 .. 15, or NULL for 8 everywhere.  iefwd_q4_pack lays it
  * out once for iefwd_q4_gemm into dst (iefwd_q4_packed_bytes bytes, 16-byte aligned): blocks of
  * 1 KB, one wave load each, with the codes of 16 features x 128 weights, then a
- * 4-byte {scale, 16 + zero} per group.  group 32, 64 or 128; N a positive
+ * 4-byte {scale, -zero} per group.  group 32, 64 or 128; N a positive
  * multiple of 16, K of group and at most 2^24; N * K < 2^31. */
 int iefwd_q4_packed_bytes(uint32_t N, uint32_t K, uint32_t group, size_t *bytes);   /* host only */
 int iefwd_q4_pack(const void *codes, const void *scales, const void *zeros, void *dst, uint32_t N, uint32_t K,
@@ -714,9 +714,10 @@ int iefwd_q4_pack(const void *codes, const void *scales, const void *zeros, void
 /* The decode-step product with 4-bit weights: out = epilogue(A W^T + b) for
  * M <= 16 rows, epilogues IEFWD_EPI_BIAS_BF16, _BIAS_GELU_BF16 and
  * _BIAS_RESID_F32 and operands as for iefwd_test_gemm_skinny (a 16-byte aligned; bias may be
- * NULL: none), packed from iefwd_q4_pack for the same N, K and group.  fp32 sums; out may be resid.  A row's
- * result depends neither on the other rows nor on M.  An infinite activation
- * gives NaN. */
+ * NULL: none), packed from iefwd_q4_pack for the same N, K and group.  out may be resid.  The terms
+ * a (code - zero) are exact and summed in fp32, a group's sum times its scale: weights that
+ * equal their zero point add exactly 0, infinities and NaN of A give what the formula gives (for
+ * finite scales).  A row's result depends neither on the other rows nor on M. */
 int iefwd_q4_gemm(uint32_t epilogue, const void *a, const void *packed, const void *bias, const float *resid, void *out,
                   uint32_t M, uint32_t N, uint32_t K, uint32_t group, void *stream);
 

@@ -2,19 +2,20 @@
 // out = epilogue(A W^T + b), W[n][k] = s[n][g] (code[n][k] - z[n][g]), g = k / group,
 // for at most 16 rows of A.  Bound by reading the codes once.
 //
-// The codes go to the matrix cores as bf16 numbers 16 + code: the four bits are
-// set into the mantissa of 16.0 (16 (1 + code / 16) = 16 + code), which is exact and
-// takes a shift and one and-or for two weights.  Per group g the product then is
-//   s_g (sum_k a_k (16 + code_k) - (16 + z_g) sum_k a_k),
-// the second sum from a matrix product with ones.  Both sums are fp32; the
-// subtraction cancels at most the five bits that 16 + code has over code, so
-// some 19 bits of the result are left.
+// code - z, a whole number from -15 to 15, is exact in bf16 and goes to the matrix cores as such: a weight
+// that equals its zero point adds nothing, an infinite activation gives what the definition gives. The sums
+// are fp32, the scale is applied to a group's sum.  Relative to 64 bits the fp32 result is off by 8.5e-8 in
+// the mean (16 x 4096 -> 1024, groups of 128, activations of either or of one sign; sums of a (16 + code) less
+// (16 + z) sum a, which need no subtraction a weight, were off by 1.3e-7 and 3.9e-7 at the same times).
+// The matrix cores subtract: as an e4m3 bit pattern a byte 0 .. 15 is the number 2^-9 code, and an 8-bit product
+// with a matrix that has 2^9 in the right places and with -z as its addend leaves each lane its own eight code - z
+// in fp32 (exact), four to a product, whose upper halves are the bf16 operand.
 //
 // Measured (us; a plain read of the same bytes, launch included, takes 7.6 for the last two): 1 x 1024 -> 1024 2.9,
-// 1 x 2048 -> 8192 3.8, 1 x 4096 -> 16384 8.4, 16 x 4096 -> 16384 10.2 and, in groups of 32, 11.1, where the vector
-// units have some 5 us of work (7 operations for 8 weights; 10 for the 4 results of a lane and group).  Short rows are bound by the
-// latency of a launch and two loads in a row.  Moving the offsets' part to a product of fp32 matrices took as many registers as it
-// saved operations (12.0); loading the next chunk before using this one made no difference at best.
+// 1 x 2048 -> 8192 3.9, 1 x 4096 -> 16384 8.7, 16 x 4096 -> 16384 10.6 and, in groups of 32, 11.5, where the vector
+// units have some 3.4 us of work (16 operations for 8 weights of a lane: 3 to part and 4 to pack the codes, 4 for
+// the addend, 5 for the scale) and the matrix cores 2.6.  Short rows are bound by the latency of a launch and two loads in a row.
+// Loading the next chunk before using this one made no difference at best.
 #include "q4.h"
 
 #include "gemm_device.h"
@@ -35,8 +36,7 @@ struct Q4Params {
 };
 
 // Lane l of a block holds of feature l % 16 the weights 32 s + 8 (l / 16) + e in
-// word s, e = 0 .. 7; of each pair the even one lies 16 bits below the odd one, so that
-// they come out as the two halves of a register (widen).
+// word s: e = 0 .. 3 in the low and e = 4 .. 7 in the high halves of its bytes, in order.
 template <int GROUP>
 __global__ __launch_bounds__(256) void q4_pack_kernel(const uint8_t *codes, const bf16_t *scales, const uint8_t *zeros,
                                                       u32x4 *dst, uint32_t *meta, int N, int K, int chunks) {
@@ -53,9 +53,9 @@ __global__ __launch_bounds__(256) void q4_pack_kernel(const uint8_t *codes, cons
         const int k = chunk * kChunk + 32 * s + 8 * (l / 16);
         if (k < K)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const uint32_t byte = codes[((size_t)n * K + k) / 2 + e], pair = (byte & 15) | (byte >> 4) << 16;
-                out[s] |= __builtin_rotateleft32(pair, e < 3 ? 3 + 4 * e : 31);
+            for (int e = 0; e < 4; ++e) {      // the pair 2 e, 2 e + 1
+                const uint32_t byte = codes[((size_t)n * K + k) / 2 + e], pair = (byte & 15) | (byte >> 4) << 8;
+                out[s] |= pair << (e < 2 ? 16 * e : 16 * e - 28);
             }
     }
     dst[i] = out;
@@ -64,7 +64,7 @@ __global__ __launch_bounds__(256) void q4_pack_kernel(const uint8_t *codes, cons
         uint32_t w = 0;      // past K: scale 0
         if (at < groups) {
             const size_t j = (size_t)n * groups + at;
-            const float off = 16.f + (zeros ? (float)(zeros[j] & 15) : 8.f);
+            const float off = zeros ? -(float)(zeros[j] & 15) : -8.f;
             w = scales[j] | (__float_as_uint(off) & 0xffff0000u);
         }
         meta[(block * 16 + l % 16) * GPC + g] = w;
@@ -75,12 +75,15 @@ __device__ inline __amdgpu_buffer_rsrc_t buffer(const void *p, uint32_t bytes) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, bytes, 0x00027000);
 }
 
-// The eight weights of a word: pair e sits at bits 3 + 4 e of each half (the last one
-// wrapped round the word), so that only three of the four need a shift.
-__device__ inline bf16x8 widen(uint32_t x) {
-    constexpr uint32_t mask = 0x00780078u, base = 0x41804180u;
-    return __builtin_bit_cast(bf16x8, u32x4{(x & mask) | base, ((x >> 4) & mask) | base, ((x >> 8) & mask) | base,
-                                            (__builtin_rotateleft32(x, 4) & mask) | base});
+// The lane's eight codes of a word, each less the zero point: off holds -z four times.  pick, this lane's part of the
+// product's first operand (e5m2), is 2^9 at its row's weight: row 4 c + e takes weight 8 c + e with it in the
+// lower word and 8 c + 4 + e in the upper one.
+__device__ inline bf16x8 widen(uint32_t x, uint32_t pick, f32x4 off) {
+    const long bytes = (long)((uint64_t)((x >> 4) & 0x0f0f0f0fu) << 32 | (x & 0x0f0f0f0fu));
+    const f32x4 lo = __builtin_amdgcn_mfma_f32_16x16x32_bf8_fp8((long)pick, bytes, off, 0, 0, 0);
+    const f32x4 hi = __builtin_amdgcn_mfma_f32_16x16x32_bf8_fp8((long)((uint64_t)pick << 32), bytes, off, 0, 0, 0);
+    auto pair = [](float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u); };
+    return __builtin_bit_cast(bf16x8, u32x4{pair(lo[0], lo[1]), pair(lo[2], lo[3]), pair(hi[0], hi[1]), pair(hi[2], hi[3])});
 }
 
 // NL: 16-byte activation loads a lane and chunk, 4 rows each (1, 2 or 4: up to 4, 8 or 16 rows).
@@ -101,7 +104,7 @@ __global__ __launch_bounds__(64 * WAVES) void q4_kernel(Q4Params p, Epi epi) {
     const int r = lane & 15, c = lane >> 4;
     const int tile0 = blockIdx.x * T;
     f32x4 acc[T] = {};
-    const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
+    const uint32_t pick = r >> 2 == c ? 0x60u << (8 * (r & 3)) : 0u;
     char *stage = lds + wave * kStage;
     const int own = r * NL / 4;                             // the row of A that this lane's operand row is
     // Operands as buffers: a scalar base and step, one 32-bit offset a lane.  Every offset lies inside
@@ -156,20 +159,16 @@ __global__ __launch_bounds__(64 * WAVES) void q4_kernel(Q4Params p, Epi epi) {
             a[s] = *reinterpret_cast<const bf16x8 *>(stage + own * 256 + ((4 * s + c) ^ own) * 16);
 #pragma unroll
         for (int g = 0; g < GPC; ++g) {
-            f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int s = 0; s < SPG; ++s)
-                sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[g * SPG + s], ones, sum, 0, 0, 0);
 #pragma unroll
             for (int t = 0; t < T; ++t) {
+                const float scale = __uint_as_float(mf[t][g] << 16), z = __uint_as_float(mf[t][g] & 0xffff0000u);
                 f32x4 d = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int s = 0; s < SPG; ++s)
-                    d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[g * SPG + s], widen(wf[t][g * SPG + s]), d, 0, 0, 0);
-                const float scale = __uint_as_float(mf[t][g] << 16), off = __uint_as_float(mf[t][g] & 0xffff0000u);
+                    d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                        a[g * SPG + s], widen(wf[t][g * SPG + s], pick, f32x4{z, z, z, z}), d, 0, 0, 0);
 #pragma unroll
-                for (int e = 0; e < NL; ++e)
-                    acc[t][e * 4 / NL] = fmaf(scale, fmaf(-off, sum[e * 4 / NL], d[e * 4 / NL]), acc[t][e * 4 / NL]);
+                for (int e = 0; e < NL; ++e) acc[t][e * 4 / NL] = fmaf(scale, d[e * 4 / NL], acc[t][e * 4 / NL]);
             }
         }
     };
