@@ -683,7 +683,8 @@ int iefwd_paged_attention_workspace(const iefwd_paged_cache *cache, uint32_t bat
  * Lengths are cut to [0, max_pages * page_size]; a page id outside the pool drops
  * its tokens; a row with nothing to attend to becomes zeros.  fp32 scores, softmax and
  * sums; the probabilities enter the product with V as a bf16 and its bf16 rest, 16
- * bits in all (an infinite element of V gives NaN).
+ * bits in all.  Infinities and NaN of V give what the formula gives (an infinite element whose
+ * probability is below 2^-100 of the row's largest may give NaN).
  * The keys of a long request are split and joined by a rule on its length, the head
  * counts and the batch size (iefwd_test_paged_split).  workspace:
  * iefwd_paged_attention_workspace bytes, 16-byte aligned, any contents; calls that may overlap need one each.  n_heads a multiple of
