@@ -526,7 +526,7 @@ class PagedCache:
     k [n_pages, n_kv_heads, head_dim // E, page_size, E] and v [n_pages, n_kv_heads, page_size // 4,
     head_dim, 4], bfloat16 (E = 8) or float8_e4m3fn (E = 16; then with fp32 k_scale and v_scale
     [n_kv_heads]).  ``PagedCache.empty`` makes them.  Calls run on `stream`, by default torch's
-    current stream of the cache's GPU."""
+    current stream of the cache's GPU; they neither wait for another stream nor keep the tensors given alive."""
 
     def __init__(self, k, v, k_scale=None, v_scale=None):
         e4m3 = isinstance(k, torch.Tensor) and k.dtype == torch.float8_e4m3fn
@@ -570,7 +570,8 @@ class PagedCache:
         _call(dev, stream, "iefwd_paged_append", self._ref, k.data_ptr(), v.data_ptr(), slots.data_ptr(), n, ks, vs)
 
     def workspace(self, batch: int, n_heads: int, max_pages: int) -> torch.Tensor:
-        """A workspace for ``attention`` on a batch and a table of max_pages columns."""
+        """A workspace for ``attention`` on a batch and a table of max_pages columns, in memory of torch's current
+        stream: calls on another one have to be ordered behind it, and the workspace to live until they have run."""
         n = _sz()
         _check(lib().iefwd_paged_attention_workspace(self._ref, batch, n_heads, max_pages, ctypes.byref(n)),
                "iefwd_paged_attention_workspace")
@@ -629,8 +630,10 @@ def test_paged_split(batch: int, n_heads: int, n_kv_heads: int, n_keys: int) -> 
 class Q4Weight:
     """A weight matrix [N, K] in 4 bits, laid out for ``product`` once: codes uint8 [N, K / 2] (weight 2 i in
     the low half of byte i), scales bf16 [N, K / group], zeros uint8 [N, K / group] or None (8 everywhere);
-    W = scales (codes - zeros).  The tensors given are not kept.  Calls run on `stream`, by default torch's
-    current stream of the weight's GPU."""
+    W = scales (codes - zeros).  Calls run on `stream`, by default torch's current stream of the weight's GPU.
+    The constructor allocates on the current stream and packs on `stream`: the one waits for the other before and
+    after, so that the tensors given, which are not kept, may be freed or overwritten at once on the current stream,
+    and the weight used there.  A weight that is used on another stream lives until its last call there has run."""
 
     def __init__(self, codes, scales, zeros=None, stream=None):
         _need("codes", codes, torch.uint8)
@@ -645,10 +648,20 @@ class Q4Weight:
             _need("zeros", zeros, torch.uint8, self._dev, shape)
         n = _sz()
         _check(lib().iefwd_q4_packed_bytes(self.N, self.K, self.group, ctypes.byref(n)), "iefwd_q4_packed_bytes")
+        home = torch.cuda.current_stream(self._dev)
         self.packed = torch.empty(n.value, dtype=torch.uint8, device=self.device)
         self._at = self.packed.data_ptr()
-        _call(self._dev, stream, "iefwd_q4_pack", codes.data_ptr(), scales.data_ptr(), _ptr(zeros), self._at, self.N, self.K,
+        side = home if stream is None else torch.cuda.ExternalStream(_stream(stream), device=self.device)
+        apart = side.cuda_stream != home.cuda_stream
+        if apart:      # home's earlier work may still use the memory of `packed`
+            side.wait_stream(home)
+        _call(self._dev, side, "iefwd_q4_pack", codes.data_ptr(), scales.data_ptr(), _ptr(zeros), self._at, self.N, self.K,
               self.group)
+        if apart:
+            home.wait_stream(side)
+        for t in (codes, scales, zeros):      # of a third stream, perhaps: not handed out again before they are read
+            if t is not None:
+                t.record_stream(home)
 
     def product(self, a, out, epilogue: int = EPI_BIAS_BF16, bias=None, resid=None, stream=None) -> None:
         """out [M, N] = epilogue(a W^T + bias), a bf16 [M, K], M <= 16; out bf16, or fp32 (as resid) for
