@@ -689,7 +689,7 @@ int iefwd_paged_attention_workspace(const iefwd_paged_cache *cache, uint32_t bat
  * counts and the batch size (iefwd_test_paged_split).  workspace:
  * iefwd_paged_attention_workspace bytes, 16-byte aligned, any contents; calls that may overlap need one each.  n_heads a multiple of
  * n_kv_heads, at most 1024; 1 <= batch <= 65535, batch * n_heads <= 2^22; max_pages >= 1 and
- * max_pages * page_size <= 2^30; scale finite. */
+ * max_pages * page_size <= 2^30; scale * log2(e) finite. */
 int iefwd_paged_attention(const iefwd_paged_cache *cache, const void *q, uint64_t q_stride, uint32_t n_heads,
                           const int32_t *table, uint32_t table_stride, uint32_t max_pages, const int32_t *lens,
                           uint32_t batch, float scale, void *ctx, void *workspace, size_t workspace_bytes,

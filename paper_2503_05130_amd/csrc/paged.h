@@ -16,6 +16,7 @@ struct PagedCache {
 };
 
 constexpr int kPlanMaxBatch = 4096;
+constexpr float kLog2e = 1.4426950408889634f;
 
 struct PlanArgs {
     const int32_t *lens, *new_lens;

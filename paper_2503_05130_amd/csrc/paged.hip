@@ -759,7 +759,7 @@ hipError_t launch_paged_attention(const PagedCache &c, const bf16_t *q, int64_t 
     a.max_keys = max_pages << c.page_log2;
     a.split = paged_split(batch, heads, c.kv_heads);
     a.slots = paged_most_parts(a.max_keys, a.split);
-    a.scale_log2e = scale * 1.4426950408889634f;
+    a.scale_log2e = scale * kLog2e;
     a.part_o = partials;
     a.part_ml = partials + (size_t)batch * heads * a.slots * c.head_dim;
     // The lengths are the device's: a workgroup for every part that there could be, up to 8 a CU, which then

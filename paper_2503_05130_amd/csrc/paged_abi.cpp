@@ -145,7 +145,8 @@ int iefwd_paged_attention(const iefwd_paged_cache *cache, const void *q, uint64_
         check_row_stride("q", q, q_stride, (uint64_t)n_heads * c.head_dim);
         if (!table || !lens || !ctx) fail(IEFWD_EINVAL, "NULL pointer");
         if (!aligned16(ctx)) fail(IEFWD_EINVAL, "ctx must be 16-byte aligned");
-        if (!std::isfinite(scale)) fail(IEFWD_EINVAL, "scale must be finite");
+        // the kernel's exponent is in powers of two; infinity times a product of 0 would be NaN
+        if (!std::isfinite(scale * kLog2e)) fail(IEFWD_EINVAL, "scale * log2(e) must be finite");
         if (workspace_bytes < need || (need && (!workspace || !aligned16(workspace))))
             fail(IEFWD_EINVAL, "workspace of " + std::to_string(need) + " bytes (16-byte aligned) needed, " +
                                    std::to_string(workspace_bytes) + " given");
