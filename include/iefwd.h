@@ -687,8 +687,9 @@ int iefwd_paged_attention_workspace(const iefwd_paged_cache *cache, uint32_t bat
  * probability is below 2^-100 of the row's largest may give NaN).
  * The keys of a long request are split and joined by a rule on its length, the head
  * counts and the batch size (iefwd_test_paged_split).  workspace:
- * iefwd_paged_attention_workspace bytes, 16-byte aligned, any contents; calls that may overlap need one each.  n_heads a multiple of
- * n_kv_heads, at most 1024; 1 <= batch <= 65535, batch * n_heads <= 2^22; max_pages >= 1 and
+ * iefwd_paged_attention_workspace bytes, 16-byte aligned, any contents; calls that may
+ * overlap need one each.  n_heads a multiple of n_kv_heads, at most 1024;
+ * 1 <= batch <= 65535, batch * n_heads <= 2^22; max_pages >= 1 and
  * max_pages * page_size <= 2^30; scale * log2(e) finite. */
 int iefwd_paged_attention(const iefwd_paged_cache *cache, const void *q, uint64_t q_stride, uint32_t n_heads,
                           const int32_t *table, uint32_t table_stride, uint32_t max_pages, const int32_t *lens,

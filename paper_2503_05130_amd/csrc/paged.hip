@@ -39,7 +39,7 @@ __device__ inline T wave_scan(T v, Add add) {
 // scratch, no atomics between workgroups: what one writes none reads.
 //
 // Bound by latency, a launch and four loads that depend on each other (lengths, LDS sums, ring or table entry): 4 requests 3.0 us,
-// 512 of which 16 end 5.4, 192 prompts with 90000 slots 4.8.
+// 512 of which 16 end 5.4, 192 prompts with 90000 slots 4.7.
 //
 // The sums saturate at 2^32 - 1, which is past everything they are compared with (below 2^31);
 // saturating sums of such numbers are the same in any order.
@@ -193,16 +193,18 @@ __global__ __launch_bounds__(kThreads) void paged_plan_kernel(PlanArgs p) {
 // run of tokens in following places of one quad, whole in the middle of a prompt, a single
 // token in a decode step; one that is not whole is written element by element.
 //
-// Bound by its bytes for prompts: 24001 tokens of 8 x 128 in 8 bits 31 us, 16000 in bf16 23 us (4.8 and 5.7 TB/s of reads and
-// writes, where a large copy reaches 4.8).  Pages written by much are not read soon: from kAppendStream bytes on they are
-// stored with the non-temporal hint (36 -> 32 us and 33 -> 23; but 12 MB 8.5 -> 10.0).  48 tokens of a decode step take 3.6 us,
-// a launch and two loads in a row.
+// Bound by its bytes for prompts: 24001 tokens of 8 x 128 in 8 bits 30 - 33 us, 16000 in bf16 22 - 28 us, by where the memory
+// lies (4.5 - 4.9 and 4.7 - 5.9 TB/s of reads and writes; a copy of 4 GiB reaches 4.8, but a plain kernel that reads and writes
+// the same amounts in a row and leaves them in the last cache in part takes 21 and 16 us).  Pages written by much are not read
+// soon: from kAppendStream bytes on they are stored with the non-temporal hint (34.6 -> 32.6 us and 30.7 -> 23.4; but 12 MB
+// 7.3 -> 7.5).  48 tokens of a decode step take 3.5 us, a launch and two loads in a row.
 constexpr int kAppendTile = 32;      // most tokens of a workgroup
 constexpr int64_t kAppendStream = 32 << 20;
 
 // x / scale, rounded as a division is, within e4m3's range; NaN stays NaN.  `inv` is the
 // rounded 1 / scale: one Newton step on the quotient by its remainder gives the correctly
-// rounded one (Markstein, IBM J. Res. Dev. 34, 1990), in 3 operations for the division's dozen.
+// rounded one (Markstein, IBM J. Res. Dev. 34, 1990; checked for every scale's with every bf16's mantissa), in 3
+// operations for the division's dozen.
 // That holds where neither leaves fp32's range, which `near` says of the scale; then a quotient of 2^-11
 // to 512 is exact so, a larger one is cut off and a smaller one is 0 in either form.
 struct E4m3Scale {
@@ -359,9 +361,11 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(PagedCache c, co
 // are busy for 6% of the time).  Neither part is ever negative, nor the rest zero, for which it gets 2^-22 of P more: both
 // times an infinite element of V are infinities of its sign, and so is their sum.
 //
-// Bound by reading the pages once: 64 requests of 4000 - 8192 keys, 32 / 8 heads of 128, 246 us with the joining kernel (6.2
-// TB/s, what a plain read reaches), in 8 bits 135 us; one request of 32001 keys 26 us (5.0 TB/s); 96 of 5 - 12000, 16 / 4 heads
+// Bound by reading the pages once: 64 requests of 4000 - 8192 keys, 32 / 8 heads of 128, 250 us with the joining kernel (6.1
+// TB/s, what a plain read reaches), in 8 bits 134 us; one request of 32001 keys 26 us (5.0 TB/s); 96 of 5 - 12000, 16 / 4 heads
 // of 64 in 8 bits, 22 us (3.3 TB/s: 784 workgroups in one round, whose longest have 4 steps in a row, and 4 us of joining).
+// Each 16 query heads of a key-value head read the pages for themselves: 64 x 6000 keys with 40 / 2 heads of 128 take 141 us, with
+// 32 / 2 (one tile) 74; 64 / 1 145, 16 / 1 41.
 // Not kept: K of the next step requested before this step's V is used, and 2 or 4 steps at once (249 registers and 18% slower
 // in bf16, no faster in 8 bits).
 struct AttnArgs {
@@ -694,8 +698,12 @@ __global__ __launch_bounds__(kThreads) void paged_join_kernel(AttnArgs a) {
 
 // A call that may read this much is taken to stream its pages past the chip's last cache (256 MiB, for which the other
 // layers' pages compete as well), and reads them with the non-temporal hint; what a smaller one reads may still be there at the
-// next call.  us without / with the hint, calls on three caches in turn: 1534 MB 275 / 250 (6.1 TB/s, what a plain read
-// of the memory reaches), 767 MB 152 / 135, 134 MB 30.6 / 26.9, 131 MB 30.2 / 26.7; but 72 MB 22.2 / 23.7, 17 MB 10.3 / 10.8.
+// next call.  us without / with the hint, calls on three caches in turn: 1534 MB 269 / 250 (6.1 TB/s, what a plain read
+// of the memory reaches), 767 MB 145 / 134, 135 MB 27.3 / 24.5, 131 MB 30.7 / 27.1; but 72 MB 22.4 / 23.1, 44 MB in short requests
+// 14.7 / 15.9 (and 74 MB in long ones 15.3 / 15.3, 16 MB 10.3 / 10.1).
+// The host knows the table's width and the pool's size, not the lengths: short requests under a wide table of a large pool count as
+// long ones (96 x 5 - 500 keys, 16 heads of 128: 14.4 us under their own table, 17.0 under one of 12000 keys, by the
+// joining launch, and 18.8 with 24000 pages, by the hint).
 constexpr int64_t kStreamBytes = 96 << 20;
 
 template <int DH, bool E4M3, int WAVES>
@@ -726,8 +734,8 @@ hipError_t launch_paged_plan(const PlanArgs &p, hipStream_t stream) {
 
 hipError_t launch_paged_append(const PagedCache &c, const bf16_t *k, const bf16_t *v, const int64_t *slots, int tokens,
                                int64_t k_stride, int64_t v_stride, hipStream_t stream) {
-    // few tokens: more workgroups of fewer (48 tokens of 8 heads 3.6 us in tiles of 8, 4.4 of 16; 24001 34 us in tiles of 32, 39
-    // of 16, 45 of 8)
+    // few tokens: more workgroups of fewer (48 tokens of 8 heads 3.6 us in tiles of 8, 4.3 of 16, 5.7 of 32; 24001 in 8 bits
+    // 31.7 us in tiles of 32, 32.4 of 16, 40 of 8; 16000 in bf16 22.2, 22.7 and 27)
     const int tile = (int64_t)tokens * c.kv_heads <= 16 * 1024 ? 8 : kAppendTile;
     const dim3 grid((unsigned)((tokens + tile - 1) / tile * c.kv_heads));
     const bool stream_out = (int64_t)tokens * c.kv_heads * c.head_dim * (c.e4m3 ? 2 : 4) >= kAppendStream;
@@ -763,8 +771,8 @@ hipError_t launch_paged_attention(const PagedCache &c, const bf16_t *q, int64_t 
     a.part_o = partials;
     a.part_ml = partials + (size_t)batch * heads * a.slots * c.head_dim;
     // The lengths are the device's: a workgroup for every part that there could be, up to 8 a CU, which then
-    // go on to further items.  (4, 8 and 16 a CU, us: 64 x 4000 - 8192 keys 281, 275 and 275; 96 x 5 - 12000 keys,
-    // where most workgroups find nothing to do, 22.4, 22.7 and 26.2.)
+    // go on to further items.  (4, 8 and 16 a CU, us: 64 x 4000 - 8192 keys 255, 250 and 250; 96 x 5 - 12000 keys,
+    // where most workgroups find nothing to do, 21.6, 21.6 and 26.3.)
     const int rows = c.kv_heads * paged_tiles(heads, c.kv_heads);
     const int64_t items = (int64_t)batch * a.slots;
     const dim3 grid((unsigned)(std::min<int64_t>(items, std::max(1, 2048 / rows)) * rows));

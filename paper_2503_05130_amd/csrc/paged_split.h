@@ -17,15 +17,15 @@ inline __host__ __device__ int paged_tiles(int n_heads, int n_kv_heads) { return
 // 128 parts: one long request among short ones must not be left to a few workgroups.
 // Measured with parts of 256, 512 and 1024 keys (us; 32 query and 8 key-value heads of 128 unless
 // stated):
-//   1 x 4000 keys        11.1 11.6 14.0      16 x 2000               41.5 35.2 31.3
-//   1 x 32001            35.3 35.3 30.9      64 x 4000 - 8192         330  295  275
-//   96 x 5 - 12000, 16 / 4 heads of 64, e4m3 36.7 30.5 28.5 (22.6 with fewer registers)
+//   1 x 4000 keys        10.6 11.0 13.4      16 x 2000               27.7 26.9 26.4
+//   1 x 32001            29.3 27.5 26.1      64 x 4000 - 8192         275  260  250
+//   96 x 5 - 12000, 16 / 4 heads of 64, e4m3 26.6 23.5 22.2
 // A request of up to 512 keys is never split: the launch that joins its parts would cost more
-// (1 x 300: 8.2 in parts of 256, 6.1 in one).  
+// (1 x 300: 8.2 in parts of 256, 5.7 in one).
 // A workgroup has 8 waves.  From 4096 rows on, more than the chip holds several times over, it has 2: a long
 // request's rows keep it busy all the same, and a short one's leave fewer waves idle (us with 8 / 4 / 2 waves:
-// 1024 x 20 - 60 keys, 8 heads of 64, 56 / 40 / 27; 1024 x 200 - 400, 32 / 8 heads of 128, 227 / 227 / 227; but
-// 256 x 800 - 1600 235 / 240 / 249; one request of 1000 up to 12% longer with 4).
+// 1024 x 20 - 60 keys, 8 heads of 64, 57 / 40 / 26; 1024 x 200 - 400, 32 / 8 heads of 128, 203 / 202 / 202; but
+// 256 x 800 - 1600 211 / 215 / 223; one request of 1000 8.3 / 8.5 with 8 / 4).
 constexpr int kPagedWholeLog2 = 9, kPagedMinLog2 = 8, kPagedMaxLog2 = 10;
 
 struct PagedSplit {

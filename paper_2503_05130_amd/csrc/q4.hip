@@ -12,10 +12,11 @@
 // in fp32 (exact), four to a product, whose upper halves are the bf16 operand.
 //
 // Measured (us; a plain read of the same bytes, launch included, takes 7.6 for the last two): 1 x 1024 -> 1024 2.9,
-// 1 x 2048 -> 8192 3.9, 1 x 4096 -> 16384 8.7, 16 x 4096 -> 16384 10.6 and, in groups of 32, 11.5, where the vector
-// units have some 3.4 us of work (16 operations for 8 weights of a lane: 3 to part and 4 to pack the codes, 4 for
-// the addend, 5 for the scale) and the matrix cores 2.6.  Short rows are bound by the latency of a launch and two loads in a row.
-// Loading the next chunk before using this one made no difference at best.
+// 1 x 2048 -> 8192 3.8, 1 x 4096 -> 16384 8.8, 16 x 4096 -> 16384 10.0 and, in groups of 32, 11.3, where the vector
+// units have 4.2 us of work (for 8 weights of a lane 16 operations, 3 to part and 4 to pack the codes, 4 for the
+// addend, 5 for the scale; and 4 of other work) and the matrix cores 2.6.  With weights that are not in the last cache (430 MB read in turn)
+// the last three take 9.8, 12.8 and 14.0.  Short rows are bound by the latency of a launch and two loads in a row.
+// Loading the next chunk before using this one: 8.9, 10.4, 12.1, and 10.9, 12.8, 13.8 from memory; not kept.
 #include "q4.h"
 
 #include "gemm_device.h"
@@ -212,11 +213,11 @@ hipError_t launch_q4_w(Epi epi, const Q4Params &p, hipStream_t stream) {
 // Two tiles a workgroup halve the reads of the activations, which each CU takes in whole, and are taken
 // where the workgroups still fill the chip; 16 waves have more of a long row in flight where one workgroup a
 // CU is all there is.  The waves, and with them the order of the sums, follow from N and K alone.
-// us with 8 waves and 1 tile / 8 and 2 / 16 and 1 / 16 and 2, groups of 128 (a form with addresses in vector registers):
-//   1 x 1024 -> 1024    3.7  3.7  3.8  4.0     16 x 4096 -> 4096    7.2  7.9  6.7  7.8
-//   1 x 8192 -> 2048    6.9  9.2  5.5  6.3     16 x 8192 -> 2048    9.5 12.9  8.3 10.7
-//   1 x 2048 -> 8192    4.1  3.9  4.2  4.1     16 x 2048 -> 8192    5.5  5.6  5.7  5.4
-//   1 x 4096 -> 16384   9.0  8.5  9.2  8.6     16 x 4096 -> 16384  12.0 10.8 12.3 11.3
+// us with 8 waves and 1 tile / 8 and 2 / 16 and 1 / 16 and 2, groups of 128:
+//   1 x 1024 -> 1024    2.8  3.1  2.9  3.1     16 x 4096 -> 4096    5.6  6.5  5.4  6.1
+//   1 x 8192 -> 2048    7.1  8.5  5.4  7.2     16 x 8192 -> 2048    7.9  9.6  6.9  8.3
+//   1 x 2048 -> 8192    4.0  4.0  4.1  4.0     16 x 2048 -> 8192    5.4  5.0  5.4  5.1
+//   1 x 4096 -> 16384   8.7  8.6  9.5  8.7     16 x 4096 -> 16384  11.4 10.0 12.3 11.4
 template <int GROUP, int NL>
 hipError_t launch_q4_m(Epi epi, const Q4Params &p, hipStream_t stream) {
     const int tiles = p.N / 16;
