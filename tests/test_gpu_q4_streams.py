@@ -90,3 +90,22 @@ def test_products_beside_the_default_stream():
     with torch.cuda.stream(side):
         inner = ie.Q4Weight(*w)
         assert torch.equal(_product(inner, a), want)
+
+
+@pytest.mark.parametrize("apart", [False, True])
+def test_a_weight_packed_in_a_captured_graph(apart):
+    """Codes that change between the replays are packed again by each, on the capturing stream or on one beside it."""
+    w, a = _weights(5), torch.randn(4, K, device=DEV).bfloat16()
+    out = torch.zeros(4, N, dtype=torch.bfloat16, device=DEV)
+    side = torch.cuda.Stream() if apart else None
+    sync()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        weight = ie.Q4Weight(*w, stream=side)
+        weight.product(a, out)
+    for i in range(4):
+        for t, new in zip(w, _weights(6 + i)):
+            t.copy_(new)
+        graph.replay()
+        sync()
+        assert torch.equal(out, _product(ie.Q4Weight(*w), a)), i
