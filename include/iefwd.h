@@ -723,6 +723,49 @@ int iefwd_q4_pack(const void *codes, const void *scales, const void *zeros, void
 int iefwd_q4_gemm(uint32_t epilogue, const void *a, const void *packed, const void *bias, const float *resid, void *out,
                   uint32_t M, uint32_t N, uint32_t K, uint32_t group, void *stream);
 
+/* ---- matrices in microscaled 4 bits ---------------------------------------------------------
+ * 32 neighbours of a row share a scale 2^(s - 127), s a byte, and are each one of 0, 0.5, 1, 1.5,
+ * 2, 3, 4 and 6 with a sign in 4 bits (the OCP microscaling format MXFP4): code = sign * 8 + index.
+ * Quantising a block: scale = 2^(floor(log2(largest magnitude)) - 2), at least 2^-127, values / scale
+ * rounded to the nearest (ties to the even code) and cut off at +-6; a block with an infinity or a NaN gets s =
+ * 255, which stands for NaN in all of its values.  The last block of a row may be short.  gfx950's
+ * matrix cores multiply such operands as they are: the terms are exact and summed in fp32.
+ *
+ * A matrix [rows, K] is kept in the operands' own order (iefwd_mx4_bytes bytes, 16-byte aligned): for each
+ * 16 rows, blocks of 1 KB with the codes of 16 rows x 128 columns (16 bytes from l * 16 on: row l % 16,
+ * columns 32 (l / 16) to 32 (l / 16) + 31, the first in the low half of the first byte), then for each 4 such
+ * blocks 256 bytes with the 4 scales of each l in block order.  What lies past the last row of 16 or the
+ * last column is 0.  The layout of the first rows does not depend on how many there are.
+ *
+ * Calls launch on `stream` of the current device, return without synchronising, allocate
+ * nothing and may be captured.  1 <= rows <= 2^24, 1 <= K <= 2^20, rows * K <= 2^36. */
+#define IEFWD_BF16  0u
+#define IEFWD_F32   1u
+
+int iefwd_mx4_bytes(uint32_t rows, uint32_t K, size_t *bytes);   /* host only */
+
+/* dst = x [rows, K], IEFWD_BF16 or IEFWD_F32, rows x_stride >= K elements apart (at most 2^40).  Whole tiles of 16 rows
+ * are written. */
+int iefwd_mx4_quantize(uint32_t type, const void *x, uint64_t x_stride, void *dst, uint32_t rows, uint32_t K, void *stream);
+
+/* dst = the matrix of codes uint8 [rows, K / 2] (column 2 i in the low half of byte i; 16-byte aligned) and scale bytes
+ * uint8 [rows, K / 32], as checkpoints hold them; K a multiple of 32. */
+int iefwd_mx4_pack(const void *codes, const void *scales, void *dst, uint32_t rows, uint32_t K, void *stream);
+
+/* out [rows, K], rows out_stride >= K elements apart = the values that src stands for (exact in both types). */
+int iefwd_mx4_values(const void *src, uint32_t type, void *out, uint64_t out_stride, uint32_t rows, uint32_t K, void *stream);
+
+/* out [M, N] = epilogue(A W^T + b) of a [M, K] and w [N, K] in this form: epilogues IEFWD_EPI_BIAS_BF16, _BIAS_GELU_BF16 and
+ * _BIAS_RESID_F32, bias bf16 [N] or NULL, resid f32 [M, N]; out may be resid.  A row's result does not depend on
+ * the other rows; the order of its sums follows from M, N and K.  M and N as rows, M * N <= 2^36. */
+int iefwd_mx4_gemm(uint32_t epilogue, const void *a, const void *w, const void *bias, const float *resid, void *out,
+                   uint32_t M, uint32_t N, uint32_t K, void *stream);
+
+/* The same of a bf16 [M, K] (16-byte aligned), quantised on the way: M <= 16, K a multiple of 8.  The terms are those
+ * of iefwd_mx4_quantize followed by iefwd_mx4_gemm. */
+int iefwd_mx4_gemm_bf16(uint32_t epilogue, const void *a, const void *w, const void *bias, const float *resid, void *out,
+                        uint32_t M, uint32_t N, uint32_t K, void *stream);
+
 /* CU residency probe: launches n_groups workgroups of 64 threads on `stream`;
  * workgroup g writes out[2g] = XCC id, out[2g+1] = the hardware id register
  * (CU, SIMD, shader-array and shader-engine fields).  out: device uint32

@@ -26,6 +26,7 @@ K_QKV, K_ATTN, K_OUTPROJ, K_FFN1, K_FFN2, K_LN, K_BWD_GEMM, K_BWD, K_OPTIM = ran
 TRAIN_MASTER, TRAIN_GRAD, TRAIN_MOMENT1, TRAIN_MOMENT2 = range(4)
 EPI_BIAS_BF16, EPI_BIAS_GELU_BF16, EPI_BIAS_RESID_F32 = 0, 1, 2
 KV_BF16, KV_E4M3 = 0, 1
+BF16, F32 = 0, 1
 EPI_LN_RESID_F32, EPI_F32, EPI_GELU_BWD_BF16, EPI_GELU2_BF16 = 4, 5, 6, 7
 
 _u32, _u64, _i32, _f32, _vp, _sz = (ctypes.c_uint32, ctypes.c_uint64, ctypes.c_int, ctypes.c_float,
@@ -98,6 +99,12 @@ SIGNATURES = {
     "iefwd_q4_packed_bytes": (_i32, [_u32, _u32, _u32, ctypes.POINTER(_sz)]),
     "iefwd_q4_pack": (_i32, [_vp, _vp, _vp, _vp, _u32, _u32, _u32, _vp]),
     "iefwd_q4_gemm": (_i32, [_u32, _vp, _vp, _vp, _vp, _vp, _u32, _u32, _u32, _u32, _vp]),
+    "iefwd_mx4_bytes": (_i32, [_u32, _u32, ctypes.POINTER(_sz)]),
+    "iefwd_mx4_quantize": (_i32, [_u32, _vp, _u64, _vp, _u32, _u32, _vp]),
+    "iefwd_mx4_pack": (_i32, [_vp, _vp, _vp, _u32, _u32, _vp]),
+    "iefwd_mx4_values": (_i32, [_vp, _u32, _vp, _u64, _u32, _u32, _vp]),
+    "iefwd_mx4_gemm": (_i32, [_u32, _vp, _vp, _vp, _vp, _vp, _u32, _u32, _u32, _vp]),
+    "iefwd_mx4_gemm_bf16": (_i32, [_u32, _vp, _vp, _vp, _vp, _vp, _u32, _u32, _u32, _vp]),
     "iefwd_decode_attention_noalloc": (_i32, [_vp, _vp, _vp, _vp, _u32, _u32, _u32, _u32, _u32, _u32, _vp]),
 }
 
@@ -678,6 +685,84 @@ class Q4Weight:
             _need("resid", resid, kind, dev, (m, n))
         _call(dev, stream, "iefwd_q4_gemm", epilogue, a.data_ptr(), self._at,
               None if bias is None else bias.data_ptr(), resid.data_ptr() if f32 else None, out.data_ptr(), m, n, k, self.group)
+
+
+# ------------------------------------------------------------------ matrices in microscaled 4 bits
+_FLOATS = {torch.bfloat16: BF16, torch.float32: F32}
+
+
+def _float_rows(name: str, t, device: int, rows: int | None, cols: int) -> tuple[int, int, int]:
+    """Checks bf16 or fp32 [rows, cols] (any number of rows for None) whose rows are contiguous and may lie apart; returns its
+    type, the rows' stride in elements and the number of rows."""
+    if not isinstance(t, torch.Tensor) or t.dtype not in _FLOATS or t.get_device() != device or not t.is_cuda:
+        raise ValueError(f"{name} must be a bfloat16 or float32 tensor on cuda:{device}")
+    if t.dim() != 2 or t.shape[1] != cols or (rows is not None and t.shape[0] != rows) or (cols > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be [{'rows' if rows is None else rows}, {cols}] with each row contiguous")
+    n = t.shape[0]
+    return _FLOATS[t.dtype], (t.stride(0) if n > 1 else cols), n
+
+
+class Mx4Matrix:
+    """A matrix [rows, K] in microscaled 4 bits (``iefwd_mx4_*``), in new, unset memory of torch's current stream: weights, or
+    activations for a product.  Calls run on `stream`, by default torch's current stream of the matrix's GPU; they neither
+    wait for another stream nor keep the tensors given alive."""
+
+    def __init__(self, rows: int, K: int, device="cuda:0"):
+        n = _sz()
+        _check(lib().iefwd_mx4_bytes(rows, K, ctypes.byref(n)), "iefwd_mx4_bytes")
+        self.rows, self.K = rows, K
+        self.packed = torch.empty(n.value, dtype=torch.uint8, device=device)
+        if not self.packed.is_cuda:
+            raise ValueError("device must be a GPU")
+        self.device, self._dev, self._at = self.packed.device, self.packed.get_device(), self.packed.data_ptr()
+
+    def quantize(self, x, stream=None) -> None:
+        """The first len(x) rows (and the rest of their 16 as zeros) = x, bf16 or fp32 [at most rows, K], whose rows may lie
+        apart."""
+        kind, stride, n = _float_rows("x", x, self._dev, None, self.K)
+        if n > self.rows:
+            raise ValueError(f"x has {n} rows, the matrix {self.rows}")
+        _call(self._dev, stream, "iefwd_mx4_quantize", kind, x.data_ptr(), stride, self._at, n, self.K)
+
+    def load(self, codes, scales, stream=None) -> None:
+        """All rows from codes uint8 [rows, K / 2] (column 2 i in the low half of byte i) and scale bytes uint8
+        [rows, K / 32], as checkpoints hold them; K a multiple of 32."""
+        if self.K % 32:
+            raise ValueError("K must be a multiple of 32")
+        _need("codes", codes, torch.uint8, self._dev, (self.rows, self.K // 2))
+        _need("scales", scales, torch.uint8, self._dev, (self.rows, self.K // 32))
+        _call(self._dev, stream, "iefwd_mx4_pack", codes.data_ptr(), scales.data_ptr(), self._at, self.rows, self.K)
+
+    def values(self, out, stream=None) -> None:
+        """out, bf16 or fp32 [at most rows, K], whose rows may lie apart, = the values of the first rows."""
+        kind, stride, n = _float_rows("out", out, self._dev, None, self.K)
+        if n > self.rows:
+            raise ValueError(f"out has {n} rows, the matrix {self.rows}")
+        _call(self._dev, stream, "iefwd_mx4_values", self._at, kind, out.data_ptr(), stride, n, self.K)
+
+    def product(self, a, out, epilogue: int = EPI_BIAS_BF16, bias=None, resid=None, stream=None) -> None:
+        """out [M, N] = epilogue(a W^T + bias) with this matrix as W [N, K]: a another Mx4Matrix, of which the first M
+        rows are taken, or bf16 [M, K], M <= 16 and K a multiple of 8, which is quantised on the way; out bf16, or fp32 (as resid)
+        for EPI_BIAS_RESID_F32; bias bf16 [N] or None."""
+        dev, m, n, k = self._dev, len(out), self.rows, self.K
+        f32 = epilogue == EPI_BIAS_RESID_F32
+        kind = torch.float32 if f32 else torch.bfloat16
+        if not (_is(out, kind, dev, (m, n)) and (bias is None or _is(bias, torch.bfloat16, dev, (n,))) and
+                (not f32 or _is(resid, kind, dev, (m, n)))):
+            _need("out", out, kind, dev, (m, n))
+            if bias is not None:
+                _need("bias", bias, torch.bfloat16, dev, (n,))
+            _need("resid", resid, kind, dev, (m, n))
+        if isinstance(a, Mx4Matrix):
+            if a.K != k or a.rows < m or a._dev != dev:
+                raise ValueError(f"a must have at least {m} rows, {k} columns and be on cuda:{dev}")
+            name, at = "iefwd_mx4_gemm", a._at
+        else:
+            if not _is(a, torch.bfloat16, dev, (m, k)):
+                _need("a", a, torch.bfloat16, dev, (m, k))
+            name, at = "iefwd_mx4_gemm_bf16", a.data_ptr()
+        _call(dev, stream, name, epilogue, at, self._at, None if bias is None else bias.data_ptr(),
+              resid.data_ptr() if f32 else None, out.data_ptr(), m, n, k)
 
 
 # ------------------------------------------------------------------ quota controller

@@ -4,6 +4,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <cstdint>
 #include <new>
 #include <string>
 
@@ -24,6 +25,8 @@ struct Error {
 inline void hip_check(hipError_t e, const char *what) {
     if (e != hipSuccess) fail(IEFWD_EHIP, std::string(what) + ": " + hipGetErrorString(e));
 }
+
+inline bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
 
 template <class F>
 int guarded(F &&f) {

@@ -13,8 +13,6 @@ using namespace iefwd;
 
 namespace {
 
-bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
-
 int log2_page(uint32_t page_size) {
     for (int i = 4; i <= 8; ++i)
         if (page_size == 1u << i) return i;

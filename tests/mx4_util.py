@@ -1,0 +1,70 @@
+"""Plain 64-bit forms of microscaled 4-bit matrices and of a cache in this form, on the CPU, for the tests."""
+from __future__ import annotations
+
+import numpy as np
+
+VALUES = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0, -0.0, -0.5, -1.0, -1.5, -2.0, -3.0, -4.0, -6.0])
+
+
+def quantize(x):
+    """codes uint8 [..., K'] and scale bytes uint8 [..., K' / 32] of fp64 rows, K' = the length rounded up to 32."""
+    x = np.asarray(x, np.float64)
+    k = -(-x.shape[-1] // 32) * 32
+    padded = np.zeros((*x.shape[:-1], k))
+    padded[..., :x.shape[-1]] = x
+    b = padded.reshape(*x.shape[:-1], k // 32, 32)
+    top = np.abs(b).max(-1)
+    bad = ~np.isfinite(b).all(-1)
+    safe = np.where(bad | (top == 0), 1.0, top)
+    exponent = np.floor(np.log2(safe)).astype(int)
+    exponent -= 2.0 ** exponent > safe          # log2 may round up to the next whole number
+    e = np.where(top == 0, -127, np.maximum(exponent - 2, -127))
+    y = np.where(bad[..., None], 0.0, b) / np.exp2(e.astype(float))[..., None]
+    size = np.abs(y)
+    # the nearest value, ties to the even code: the sum of the borders passed, a border itself passed where that leads to an even code
+    codes = np.zeros(size.shape, np.uint8)
+    for i, border in enumerate([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0]):
+        codes += (size >= border) if i % 2 else (size > border)
+    codes += 8 * np.signbit(y).astype(np.uint8)
+    codes[bad] = 0
+    return codes.reshape(*x.shape[:-1], k), np.where(bad, 255, e + 127).astype(np.uint8)
+
+
+def values(codes, scales):
+    """fp64 values of codes (one a byte) under scale bytes."""
+    v = VALUES[codes].reshape(*codes.shape[:-1], -1, 32)
+    s = np.where(scales == 255, np.nan, np.exp2(scales.astype(float) - 127.0))
+    return (v * s[..., None]).reshape(codes.shape)
+
+
+def pairs(codes):
+    """Two codes a byte, the first in the low half."""
+    return codes[..., 0::2] | codes[..., 1::2] << 4
+
+
+def packed(codes, scales, rows, cols):
+    """The library's layout of a matrix, all bytes of it."""
+    tiles, chunks = -(-rows // 16), -(-cols // 128)
+    c = np.zeros((tiles * 16, chunks * 128), np.uint8)
+    c[:rows, :codes.shape[1]] = codes
+    s = np.zeros((tiles * 16, -(-chunks // 4) * 16), np.uint8)
+    s[:rows, :scales.shape[1]] = scales
+    c = pairs(c).reshape(tiles, 16, chunks, 4, 16).transpose(0, 2, 3, 1, 4).reshape(tiles, -1)
+    s = s.reshape(tiles, 16, -1, 4, 4).transpose(0, 2, 4, 1, 3).reshape(tiles, -1)      # tile, group, block, row, chunk of the group
+    return np.concatenate([c, s], 1).reshape(-1)
+
+
+def k_pages(codes, scales):
+    """The cache's bytes [pages, heads, 17, d / 32, page] of keys given as [pages, place, head, column]."""
+    p, page, h, d = codes.shape
+    c = pairs(codes).reshape(p, page, h, d // 32, 16).transpose(0, 2, 3, 1, 4).reshape(p, h, -1)
+    s = scales.transpose(0, 2, 3, 1).reshape(p, h, -1)
+    return np.ascontiguousarray(np.concatenate([c, s], -1).reshape(p, h, 17, d // 32, page))
+
+
+def v_pages(codes, scales):
+    """The cache's bytes [pages, heads, 17, page / 4, d / 8] of values given as [pages, place, head, column]."""
+    p, page, h, d = codes.shape
+    c = pairs(codes).reshape(p, page // 4, 4, h, d // 8, 4).transpose(0, 3, 1, 4, 2, 5).reshape(p, h, -1)
+    s = scales.reshape(p, page // 4, 4, h, d // 32).transpose(0, 3, 1, 4, 2).reshape(p, h, -1)
+    return np.ascontiguousarray(np.concatenate([c, s], -1).reshape(p, h, 17, page // 4, d // 8))
