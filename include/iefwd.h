@@ -609,12 +609,19 @@ int iefwd_decode_attention_noalloc(const void *q, const void *k, const void *vt,
 #define IEFWD_KV_BF16  0u
 #define IEFWD_KV_E4M3  1u   /* 8-bit floating point (1-4-3 bits, largest value 448) with a scale per key-value head */
 
+#define IEFWD_KV_MX4   3u   /* microscaled 4 bits (see iefwd_mx4_quantize) in blocks of 32 columns of one token; 2 is no type */
+
 /* A pool of pages.  With E = 16 / bytes per element (8 or 16), both 16-byte aligned:
  *   k  [n_pages][n_kv_heads][head_dim / E][page_size][E]
  *   v  [n_pages][n_kv_heads][page_size / 4][head_dim][4]
  * i.e. K in 16-byte pieces of one token, V in pieces of 4 consecutive tokens of one
  * column, the orders in which the attention's matrix operands read them.  A slot
- * is page * page_size + place.  Places that no token was written to may hold any bits. */
+ * is page * page_size + place.  Places that no token was written to may hold any bits.
+ * IEFWD_KV_MX4: each head's part of a page is page_size * head_dim * 17 / 32 bytes, the codes and behind them the scales:
+ *   k  [head_dim / 32][page_size] pieces of 16 bytes (32 columns of a token), then [head_dim / 32][page_size] scale bytes
+ *   v  [page_size / 4][head_dim / 8] pieces of 16 bytes (4 tokens, of each 4 bytes of 8 columns), then
+ *      [page_size / 4][head_dim / 32][4] scale bytes (4 tokens)
+ * two columns a byte, the first in the low half. */
 typedef struct iefwd_paged_cache {
     uint32_t abi_version;   /* must be IEFWD_ABI_VERSION */
     uint32_t kv_type;       /* IEFWD_KV_* */
@@ -666,9 +673,16 @@ int iefwd_paged_plan(uint32_t batch, uint32_t page_size, const int32_t *lens, co
  * iefwd_paged_plan.  A token whose slot lies outside the pool is skipped.  No
  * two tokens may have the same slot.  IEFWD_KV_E4M3: x / scale rounded to the nearest
  * (ties to even), values beyond +-448 stored as +-448, NaN as NaN.
+ * IEFWD_KV_MX4: each 32 columns of a token and head as by iefwd_mx4_quantize.
  * n_tokens * n_kv_heads at most 2^28; n_tokens = 0 does nothing. */
 int iefwd_paged_append(const iefwd_paged_cache *cache, const void *k, const void *v, const int64_t *slots,
                        uint32_t n_tokens, uint64_t k_stride, uint64_t v_stride, void *stream);
+
+/* The inverse: the keys and values of n_tokens slots, in bf16 (an 8-bit cache's scale * stored rounded to it, the others' values
+ * exactly), to rows of k and v as for iefwd_paged_append.  A slot may occur more than once; one outside the pool gives
+ * zeros. */
+int iefwd_paged_read(const iefwd_paged_cache *cache, const int64_t *slots, void *k, void *v, uint32_t n_tokens,
+                     uint64_t k_stride, uint64_t v_stride, void *stream);
 
 /* Bytes of workspace that iefwd_paged_attention needs for a batch and a table of
  * max_pages columns (0 where no request can be long enough to be split). Host only. */
@@ -695,6 +709,16 @@ int iefwd_paged_attention(const iefwd_paged_cache *cache, const void *q, uint64_
                           const int32_t *table, uint32_t table_stride, uint32_t max_pages, const int32_t *lens,
                           uint32_t batch, float scale, void *ctx, void *workspace, size_t workspace_bytes,
                           void *stream);
+
+/* The same with other scores: with s_j = scale * q . k_j, cap tanh(s_j / cap) in its place (cap 0: s_j itself), less slopes[h] (f32
+ * [n_heads], finite, or NULL: 0) times the distance lens[b] - 1 - j of the key from the newest one.  cap 0 or in [2^-60, 2^60].
+ * Over a cache of IEFWD_KV_MX4, here and above, q enters the product as two e4m3 numbers, under scales for 32 columns each:
+ * exact down to 2^-13 of the largest of these, and off by 2^-21 of it below; an infinity or NaN of q makes its head's row NaN,
+ * and a block of a key or value that is NaN does what the formula says. */
+int iefwd_paged_attention_scored(const iefwd_paged_cache *cache, const void *q, uint64_t q_stride, uint32_t n_heads,
+                                 const int32_t *table, uint32_t table_stride, uint32_t max_pages, const int32_t *lens,
+                                 uint32_t batch, float scale, float cap, const float *slopes, void *ctx, void *workspace,
+                                 size_t workspace_bytes, void *stream);
 
 /* Pure host function: the keys in each part that iefwd_paged_attention splits a
  * request of n_keys into, in a batch of this many requests.  n_keys <= 2^30, the

@@ -25,7 +25,7 @@ OK, EINVAL, ENODEV, ENOMEM, EHIP, ESTATE, EVERSION = 0, -1, -2, -3, -4, -5, -6
 K_QKV, K_ATTN, K_OUTPROJ, K_FFN1, K_FFN2, K_LN, K_BWD_GEMM, K_BWD, K_OPTIM = range(9)
 TRAIN_MASTER, TRAIN_GRAD, TRAIN_MOMENT1, TRAIN_MOMENT2 = range(4)
 EPI_BIAS_BF16, EPI_BIAS_GELU_BF16, EPI_BIAS_RESID_F32 = 0, 1, 2
-KV_BF16, KV_E4M3 = 0, 1
+KV_BF16, KV_E4M3, KV_MX4 = 0, 1, 3
 BF16, F32 = 0, 1
 EPI_LN_RESID_F32, EPI_F32, EPI_GELU_BWD_BF16, EPI_GELU2_BF16 = 4, 5, 6, 7
 
@@ -95,6 +95,8 @@ SIGNATURES = {
     "iefwd_paged_append": (_i32, [_vp, _vp, _vp, _vp, _u32, _u64, _u64, _vp]),
     "iefwd_paged_attention_workspace": (_i32, [_vp, _u32, _u32, _u32, ctypes.POINTER(_sz)]),
     "iefwd_paged_attention": (_i32, [_vp, _vp, _u64, _u32, _vp, _u32, _u32, _vp, _u32, _f32, _vp, _vp, _sz, _vp]),
+    "iefwd_paged_attention_scored": (_i32, [_vp, _vp, _u64, _u32, _vp, _u32, _u32, _vp, _u32, _f32, _f32, _vp, _vp, _vp, _sz, _vp]),
+    "iefwd_paged_read": (_i32, [_vp, _vp, _vp, _vp, _u32, _u64, _u64, _vp]),
     "iefwd_test_paged_split": (_i32, [_u32, _u32, _u32, _u32, ctypes.POINTER(_u32)]),
     "iefwd_q4_packed_bytes": (_i32, [_u32, _u32, _u32, ctypes.POINTER(_sz)]),
     "iefwd_q4_pack": (_i32, [_vp, _vp, _vp, _vp, _u32, _u32, _u32, _vp]),
@@ -532,34 +534,47 @@ class PagedCache:
     """A pool of pages of keys and values (``iefwd_paged_cache``) in the caller's tensors:
     k [n_pages, n_kv_heads, head_dim // E, page_size, E] and v [n_pages, n_kv_heads, page_size // 4,
     head_dim, 4], bfloat16 (E = 8) or float8_e4m3fn (E = 16; then with fp32 k_scale and v_scale
-    [n_kv_heads]).  ``PagedCache.empty`` makes them.  Calls run on `stream`, by default torch's
+    [n_kv_heads]); or, in microscaled 4 bits, uint8 k [n_pages, n_kv_heads, 17, head_dim // 32, page_size] and v
+    [n_pages, n_kv_heads, 17, page_size // 4, head_dim // 8], per head of a page 16 parts codes and one of scales.
+    ``PagedCache.empty`` makes them.  Calls run on `stream`, by default torch's
     current stream of the cache's GPU; they neither wait for another stream nor keep the tensors given alive."""
 
     def __init__(self, k, v, k_scale=None, v_scale=None):
-        e4m3 = isinstance(k, torch.Tensor) and k.dtype == torch.float8_e4m3fn
-        dtype, e = (torch.float8_e4m3fn, 16) if e4m3 else (torch.bfloat16, 8)
+        dtype = k.dtype if isinstance(k, torch.Tensor) and k.dtype in (torch.float8_e4m3fn, torch.uint8) else torch.bfloat16
+        e4m3, mx4, e = dtype is torch.float8_e4m3fn, dtype is torch.uint8, 16 if dtype is torch.float8_e4m3fn else 8
         _need("k", k, dtype)
-        if k.dim() != 5 or k.shape[4] != e:
-            raise ValueError(f"k must be [n_pages, n_kv_heads, head_dim // {e}, page_size, {e}]")
+        if k.dim() != 5 or (k.shape[2] != 17 if mx4 else k.shape[4] != e):
+            raise ValueError("k must be [n_pages, n_kv_heads, 17, head_dim // 32, page_size]" if mx4 else
+                             f"k must be [n_pages, n_kv_heads, head_dim // {e}, page_size, {e}]")
         n_pages, heads, pieces, page, _ = k.shape
+        if mx4:
+            pieces, page = k.shape[3:]
         self.device, self._dev = k.device, k.get_device()
-        self.page_size, self.n_kv_heads, self.head_dim = page, heads, pieces * e
+        self.page_size, self.n_kv_heads, self.head_dim = page, heads, pieces * (32 if mx4 else e)
         _need("k", k, dtype, shape=k.shape)
-        _need("v", v, dtype, self._dev, (n_pages, heads, page // 4, self.head_dim, 4))
+        _need("v", v, dtype, self._dev, (n_pages, heads, 17, page // 4, self.head_dim // 8) if mx4 else
+              (n_pages, heads, page // 4, self.head_dim, 4))
         if e4m3:
             _need("k_scale", k_scale, torch.float32, self._dev, (heads,))
             _need("v_scale", v_scale, torch.float32, self._dev, (heads,))
         elif k_scale is not None or v_scale is not None:
             raise ValueError("scales belong to a float8_e4m3fn cache")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self.desc = PagedCacheDesc(ABI_VERSION, KV_E4M3 if e4m3 else KV_BF16, n_pages, page, heads, self.head_dim, _ptr(k),
-                                   _ptr(v), _ptr(k_scale), _ptr(v_scale))
+        kind = KV_E4M3 if e4m3 else KV_MX4 if mx4 else KV_BF16
+        self.desc = PagedCacheDesc(ABI_VERSION, kind, n_pages, page, heads, self.head_dim, _ptr(k), _ptr(v), _ptr(k_scale),
+                                   _ptr(v_scale))
         self._ref = ctypes.byref(self.desc)
 
     @classmethod
     def empty(cls, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, k_scale=None, v_scale=None,
-              device="cuda:0") -> "PagedCache":
-        """A pool in new, unset memory; 8-bit if scales are given."""
+              device="cuda:0", mx4: bool = False) -> "PagedCache":
+        """A pool in new, unset memory; 8-bit if scales are given, in microscaled 4 bits with mx4."""
+        if mx4:
+            if page_size % 4 or head_dim % 32:
+                raise ValueError("page_size must be a multiple of 4 and head_dim of 32")
+            return cls(torch.empty((n_pages, n_kv_heads, 17, head_dim // 32, page_size), dtype=torch.uint8, device=device),
+                       torch.empty((n_pages, n_kv_heads, 17, page_size // 4, head_dim // 8), dtype=torch.uint8, device=device),
+                       k_scale, v_scale)
         dtype, e = (torch.bfloat16, 8) if k_scale is None else (torch.float8_e4m3fn, 16)
         return cls(torch.empty((n_pages, n_kv_heads, head_dim // e, page_size, e), dtype=dtype, device=device),
                    torch.empty((n_pages, n_kv_heads, page_size // 4, head_dim, 4), dtype=dtype, device=device), k_scale,
@@ -576,6 +591,17 @@ class PagedCache:
         vs = _rows("v", v, dev, n, self.n_kv_heads, self.head_dim)
         _call(dev, stream, "iefwd_paged_append", self._ref, k.data_ptr(), v.data_ptr(), slots.data_ptr(), n, ks, vs)
 
+    def read(self, slots, k, v, stream=None) -> None:
+        """k and v, bf16 [tokens, n_kv_heads, head_dim] (rows may lie apart) = what the cache holds at slots (int64 [tokens];
+        outside the pool: zeros)."""
+        dev = self._dev
+        n = len(slots)
+        if not _is(slots, torch.int64, dev, (n,)):
+            _need("slots", slots, torch.int64, dev, (n,))
+        ks = _rows("k", k, dev, n, self.n_kv_heads, self.head_dim)
+        vs = _rows("v", v, dev, n, self.n_kv_heads, self.head_dim)
+        _call(dev, stream, "iefwd_paged_read", self._ref, slots.data_ptr(), k.data_ptr(), v.data_ptr(), n, ks, vs)
+
     def workspace(self, batch: int, n_heads: int, max_pages: int) -> torch.Tensor:
         """A workspace for ``attention`` on a batch and a table of max_pages columns, in memory of torch's current
         stream: calls on another one have to be ordered behind it, and the workspace to live until they have run."""
@@ -584,10 +610,12 @@ class PagedCache:
                "iefwd_paged_attention_workspace")
         return torch.empty(n.value, dtype=torch.uint8, device=self.device)
 
-    def attention(self, q, table, lens, out, workspace, scale: float | None = None, stream=None) -> None:
+    def attention(self, q, table, lens, out, workspace, scale: float | None = None, stream=None, cap: float = 0.0,
+                  slopes=None) -> None:
         """out bf16 [batch, n_heads, head_dim] = attention of one query per request and head, q of that
         shape (rows may lie apart), over the pages in `table` (int32 [batch, max_pages], rows may lie apart) of
-        lens (int32 [batch]) cached tokens.  scale: 1 / sqrt(head_dim) by default."""
+        lens (int32 [batch]) cached tokens.  scale: 1 / sqrt(head_dim) by default.  A score s becomes cap tanh(s / cap) unless
+        cap is 0, and loses slopes[head] (fp32 [n_heads]) times the key's distance from the newest one."""
         dev, d = self._dev, self.head_dim
         batch = len(lens)
         if not _is(lens, torch.int32, dev, (batch,)):
@@ -599,9 +627,16 @@ class PagedCache:
         qs = _rows("q", q, dev, batch, heads, d)
         if workspace.dtype is not torch.uint8 or workspace.get_device() != dev or not workspace.is_contiguous():
             _need("workspace", workspace, torch.uint8, dev, (workspace.numel(),))
-        _call(dev, stream, "iefwd_paged_attention", self._ref, q.data_ptr(), qs, heads, table.data_ptr(), stride, cols,
-              lens.data_ptr(), batch, d ** -0.5 if scale is None else scale, out.data_ptr(), workspace.data_ptr(),
-              workspace.numel())
+        scale = d ** -0.5 if scale is None else scale
+        if cap == 0.0 and slopes is None:
+            _call(dev, stream, "iefwd_paged_attention", self._ref, q.data_ptr(), qs, heads, table.data_ptr(), stride, cols,
+                  lens.data_ptr(), batch, scale, out.data_ptr(), workspace.data_ptr(), workspace.numel())
+            return
+        if slopes is not None and not _is(slopes, torch.float32, dev, (heads,)):
+            _need("slopes", slopes, torch.float32, dev, (heads,))
+        _call(dev, stream, "iefwd_paged_attention_scored", self._ref, q.data_ptr(), qs, heads, table.data_ptr(), stride, cols,
+              lens.data_ptr(), batch, scale, cap, None if slopes is None else slopes.data_ptr(), out.data_ptr(),
+              workspace.data_ptr(), workspace.numel())
 
 
 def paged_plan(page_size: int, lens, new_lens, table, ring, counters, lens_out, counters_out, slots, starts, refused,

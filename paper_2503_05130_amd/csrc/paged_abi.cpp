@@ -23,15 +23,15 @@ int log2_page(uint32_t page_size) {
 PagedCache paged_cache(const iefwd_paged_cache *c) {
     if (!c) fail(IEFWD_EINVAL, "cache is NULL");
     if (c->abi_version != IEFWD_ABI_VERSION) fail(IEFWD_EVERSION, "cache: ABI version mismatch");
-    if (c->kv_type > IEFWD_KV_E4M3) fail(IEFWD_EINVAL, "unknown kv_type");
+    if (c->kv_type != IEFWD_KV_BF16 && c->kv_type != IEFWD_KV_E4M3 && c->kv_type != IEFWD_KV_MX4) fail(IEFWD_EINVAL, "unknown kv_type");
     if (c->n_pages == 0 || c->n_pages > 0x7fffffffu) fail(IEFWD_EINVAL, "n_pages must be in [1, 2^31 - 1]");
     if (c->n_kv_heads == 0 || c->n_kv_heads > 1024) fail(IEFWD_EINVAL, "n_kv_heads must be in [1, 1024]");
     if (c->head_dim != 64 && c->head_dim != 128) fail(IEFWD_EINVAL, "head_dim must be 64 or 128");
     const int log2 = log2_page(c->page_size);
     if (!c->k || !c->v || !aligned16(c->k) || !aligned16(c->v)) fail(IEFWD_EINVAL, "k and v must be 16-byte aligned");
-    const bool e4m3 = c->kv_type == IEFWD_KV_E4M3;
-    if (e4m3 && (!c->k_scale || !c->v_scale)) fail(IEFWD_EINVAL, "an 8-bit cache needs k_scale and v_scale");
-    return {c->k, c->v, c->k_scale, c->v_scale, (int)c->n_pages, log2, (int)c->n_kv_heads, (int)c->head_dim, e4m3};
+    if (c->kv_type == IEFWD_KV_E4M3 && (!c->k_scale || !c->v_scale)) fail(IEFWD_EINVAL, "an 8-bit cache needs k_scale and v_scale");
+    return {c->k, c->v, c->k_scale, c->v_scale, (int)c->n_pages, log2, (int)c->n_kv_heads, (int)c->head_dim,
+            (KvKind)c->kv_type};
 }
 
 void check_table(uint32_t table_stride, uint32_t max_pages, int page_log2) {
@@ -58,6 +58,27 @@ void check_batch_heads(uint32_t batch, uint32_t n_heads, uint32_t n_kv_heads) {
 size_t paged_workspace(const PagedCache &c, uint32_t batch, uint32_t n_heads, uint32_t max_pages) {
     check_batch_heads(batch, n_heads, (uint32_t)c.kv_heads);
     return 4 * paged_workspace_floats((int)batch, (int)n_heads, c.kv_heads, c.head_dim, (int)(max_pages << c.page_log2));
+}
+
+// Both attention calls, within `guarded`.
+void paged_attention(const iefwd_paged_cache *cache, const void *q, uint64_t q_stride, uint32_t n_heads, const int32_t *table,
+                     uint32_t table_stride, uint32_t max_pages, const int32_t *lens, uint32_t batch, float scale,
+                     ScoreForm form, void *ctx, void *workspace, size_t workspace_bytes, void *stream) {
+    const PagedCache c = paged_cache(cache);
+    check_table(table_stride, max_pages, c.page_log2);
+    const size_t need = paged_workspace(c, batch, n_heads, max_pages);
+    check_row_stride("q", q, q_stride, (uint64_t)n_heads * c.head_dim);
+    if (!table || !lens || !ctx) fail(IEFWD_EINVAL, "NULL pointer");
+    if (!aligned16(ctx)) fail(IEFWD_EINVAL, "ctx must be 16-byte aligned");
+    // the kernel's exponent is in powers of two; infinity times a product of 0 would be NaN
+    if (!std::isfinite(scale * kLog2e)) fail(IEFWD_EINVAL, "scale * log2(e) must be finite");
+    if (workspace_bytes < need || (need && (!workspace || !aligned16(workspace))))
+        fail(IEFWD_EINVAL, "workspace of " + std::to_string(need) + " bytes (16-byte aligned) needed, " +
+                               std::to_string(workspace_bytes) + " given");
+    hip_check(launch_paged_attention(c, (const bf16_t *)q, (int64_t)q_stride, table, (int)table_stride, (int)max_pages, lens,
+                                     (bf16_t *)ctx, static_cast<float *>(workspace), (int)batch, (int)n_heads, scale, form,
+                                     (hipStream_t)stream),
+              "paged attention launch");
 }
 
 void check_q4(uint32_t N, uint32_t K, uint32_t group) {
@@ -116,9 +137,26 @@ int iefwd_paged_append(const iefwd_paged_cache *cache, const void *k, const void
         check_row_stride("v", v, v_stride, row);
         if (!slots) fail(IEFWD_EINVAL, "slots is NULL");
         if ((uint64_t)n_tokens * c.kv_heads > (1u << 28)) fail(IEFWD_EINVAL, "n_tokens * n_kv_heads must be at most 2^28");
-        hip_check(launch_paged_append(c, (const bf16_t *)k, (const bf16_t *)v, slots, (int)n_tokens, (int64_t)k_stride,
-                                      (int64_t)v_stride, (hipStream_t)stream),
+        const auto launch = c.kind == KvKind::Mx4 ? launch_paged_append_mx4 : launch_paged_append;
+        hip_check(launch(c, (const bf16_t *)k, (const bf16_t *)v, slots, (int)n_tokens, (int64_t)k_stride, (int64_t)v_stride,
+                         (hipStream_t)stream),
                   "paged append launch");
+    });
+}
+
+int iefwd_paged_read(const iefwd_paged_cache *cache, const int64_t *slots, void *k, void *v, uint32_t n_tokens,
+                     uint64_t k_stride, uint64_t v_stride, void *stream) {
+    return guarded([&] {
+        const PagedCache c = paged_cache(cache);
+        const uint64_t row = (uint64_t)c.kv_heads * c.head_dim;
+        if (n_tokens == 0) return;
+        check_row_stride("k", k, k_stride, row);
+        check_row_stride("v", v, v_stride, row);
+        if (!slots) fail(IEFWD_EINVAL, "slots is NULL");
+        if ((uint64_t)n_tokens * c.kv_heads > (1u << 28)) fail(IEFWD_EINVAL, "n_tokens * n_kv_heads must be at most 2^28");
+        hip_check(launch_paged_read(c, slots, (bf16_t *)k, (bf16_t *)v, (int)n_tokens, (int64_t)k_stride, (int64_t)v_stride,
+                                    (hipStream_t)stream),
+                  "paged read launch");
     });
 }
 
@@ -137,21 +175,20 @@ int iefwd_paged_attention(const iefwd_paged_cache *cache, const void *q, uint64_
                           uint32_t batch, float scale, void *ctx, void *workspace, size_t workspace_bytes,
                           void *stream) {
     return guarded([&] {
-        const PagedCache c = paged_cache(cache);
-        check_table(table_stride, max_pages, c.page_log2);
-        const size_t need = paged_workspace(c, batch, n_heads, max_pages);
-        check_row_stride("q", q, q_stride, (uint64_t)n_heads * c.head_dim);
-        if (!table || !lens || !ctx) fail(IEFWD_EINVAL, "NULL pointer");
-        if (!aligned16(ctx)) fail(IEFWD_EINVAL, "ctx must be 16-byte aligned");
-        // the kernel's exponent is in powers of two; infinity times a product of 0 would be NaN
-        if (!std::isfinite(scale * kLog2e)) fail(IEFWD_EINVAL, "scale * log2(e) must be finite");
-        if (workspace_bytes < need || (need && (!workspace || !aligned16(workspace))))
-            fail(IEFWD_EINVAL, "workspace of " + std::to_string(need) + " bytes (16-byte aligned) needed, " +
-                                   std::to_string(workspace_bytes) + " given");
-        hip_check(launch_paged_attention(c, (const bf16_t *)q, (int64_t)q_stride, table, (int)table_stride, (int)max_pages,
-                                         lens, (bf16_t *)ctx, static_cast<float *>(workspace), (int)batch, (int)n_heads,
-                                         scale, (hipStream_t)stream),
-                  "paged attention launch");
+        paged_attention(cache, q, q_stride, n_heads, table, table_stride, max_pages, lens, batch, scale, {0.f, nullptr}, ctx,
+                        workspace, workspace_bytes, stream);
+    });
+}
+
+int iefwd_paged_attention_scored(const iefwd_paged_cache *cache, const void *q, uint64_t q_stride, uint32_t n_heads,
+                                 const int32_t *table, uint32_t table_stride, uint32_t max_pages, const int32_t *lens,
+                                 uint32_t batch, float scale, float cap, const float *slopes, void *ctx, void *workspace,
+                                 size_t workspace_bytes, void *stream) {
+    return guarded([&] {
+        // beyond these the score over the cap leaves fp32's range
+        if (!(cap == 0.f || (cap >= 0x1p-60f && cap <= 0x1p60f))) fail(IEFWD_EINVAL, "cap must be 0 or in [2^-60, 2^60]");
+        paged_attention(cache, q, q_stride, n_heads, table, table_stride, max_pages, lens, batch, scale, {cap, slopes}, ctx,
+                        workspace, workspace_bytes, stream);
     });
 }
 

@@ -68,3 +68,47 @@ def v_pages(codes, scales):
     c = pairs(codes).reshape(p, page // 4, 4, h, d // 8, 4).transpose(0, 3, 1, 4, 2, 5).reshape(p, h, -1)
     s = scales.reshape(p, page // 4, 4, h, d // 32).transpose(0, 3, 1, 4, 2).reshape(p, h, -1)
     return np.ascontiguousarray(np.concatenate([c, s], -1).reshape(p, h, 17, page // 4, d // 8))
+
+
+def scored_attention(q, k, v, table, lens, scale, cap=0.0, slopes=None, q_exact=True):
+    """q [B, H, d], k and v [pages, place, kv head, d], fp64; pages outside the pool drop their tokens.  Returns the context, per
+    element a bound sum_j p_j |v_j| and per row a bound on a score's error in fp32: its sum of d terms and scaling (each
+    rounding 2^-23, rounded or cut), for a cache in 4 bits what splitting q leaves out (2^-21 of the largest of 32 columns, q_exact False),
+    the tanh (2^-19 of its result) and the roundings of the scaled score, the slope's product and their sum."""
+    batch, heads, d = q.shape
+    pages, page, kv, _ = k.shape
+    out, mag, err = np.zeros_like(q), np.zeros_like(q), np.zeros((batch, heads, 1))
+    for b in range(batch):
+        n = min(max(int(lens[b]), 0), table.shape[1] * page)
+        pos = np.arange(n)
+        ids = table[b][pos // page]
+        keep = (ids >= 0) & (ids < pages)
+        if not keep.any():
+            continue
+        kk, vv = (x[ids[keep], pos[keep] % page] for x in (k, v))
+        for h in range(heads):
+            g = h // (heads // kv)
+            s = kk[:, g] @ q[b, h] * scale
+            e = (d + 2) * 2.0 ** -23 * (np.abs(kk[:, g]) @ np.abs(q[b, h]) * abs(scale)).max()
+            if not q_exact:
+                top = np.abs(q[b, h]).reshape(-1, 32).max(1)
+                e += 2.0 ** -21 * (np.abs(kk[:, g]).reshape(len(kk), -1, 32).sum(2) @ top * abs(scale)).max()
+            if cap:
+                s = cap * np.tanh(s / cap)
+                e += 2.0 ** -19 * np.abs(s).max()
+            if slopes is not None:
+                bias = slopes[h] * (n - 1 - pos[keep])
+                s = s - bias
+                e += 2.0 ** -22 * np.abs(bias).max()
+            err[b, h] = e + 2.0 ** -22 * np.abs(s).max()
+            p = np.exp(s - s.max())
+            p /= p.sum()
+            out[b, h] = p @ vv[:, g]
+            mag[b, h] = p @ np.abs(vv[:, g])
+    return out, mag, err
+
+
+def scored_tolerance(ref, mag, err, n):
+    """Half a bf16 step of the result, and on sum p |v|: the probabilities' 16 bits, exp2 and the rescalings (2^-20), the
+    score's error (each p and their sum change by it) and the fp32 sums over the keys."""
+    return 2.0 ** -8 * np.abs(ref) + 2 * (2.0 ** -16 + 2.0 ** -20 + np.expm1(np.minimum(err, 1.0)) + (n + 64) * 2.0 ** -24) * mag

@@ -78,3 +78,50 @@ def test_plain_form():
     assert np.allclose(np.abs(np.clip(x / unit, -6, 6) - v / unit), best, atol=1e-12)
     top = np.abs(x.reshape(50, 3, 32)).max(-1)
     assert ((top / np.exp2(scales.astype(float) - 127) >= 4) & (top / np.exp2(scales.astype(float) - 127) < 8)).all()
+
+
+# ------------------------------------------------------------------------------------ a cache in this form
+def _desc(**kw):
+    d = dict(abi_version=ie.ABI_VERSION, kv_type=ie.KV_MX4, n_pages=10, page_size=16, n_kv_heads=4, head_dim=64, k=P, v=2 * P)
+    d.update(kw)
+    return ie.PagedCacheDesc(**d)
+
+
+def _read(cache, k=P, v=P, slots=P, n=5, ks=256, vs=256):
+    return ie.lib().iefwd_paged_read(None if cache is None else ctypes.byref(cache), slots, k, v, n, ks, vs, None)
+
+
+def _scored(cache, cap=0.0, slopes=None, scale=1.0, ctx=P, heads=8):
+    return ie.lib().iefwd_paged_attention_scored(None if cache is None else ctypes.byref(cache), P, 512, heads, P, 200, 200, P, 3, scale,
+                                                 cap, slopes, ctx, P, 1 << 30, None)
+
+
+@pytest.mark.parametrize("bad", [dict(kv_type=2), dict(kv_type=4), dict(n_pages=0), dict(page_size=8), dict(head_dim=96), dict(k=None), dict(v=P + 8),
+                                 dict(n_kv_heads=0)])
+def test_bad_caches_are_refused(bad):
+    c = _desc(**bad)
+    assert _read(c) == ie.EINVAL and ie.last_error()
+    assert _scored(c) == ie.EINVAL
+    assert ie.lib().iefwd_paged_append(ctypes.byref(c), P, P, P, 5, 256, 256, None) == ie.EINVAL
+
+
+def test_reads_and_scores_refuse():
+    c = _desc()
+    assert _read(None) == ie.EINVAL and _scored(None) == ie.EINVAL
+    assert _read(_desc(abi_version=9)) == ie.EVERSION
+    for kw in (dict(k=None), dict(v=None), dict(slots=None), dict(k=P + 8), dict(ks=255), dict(vs=252), dict(ks=(1 << 40) + 8),
+               dict(n=(1 << 26) + 1)):
+        assert _read(c, **kw) == ie.EINVAL, kw
+    assert _read(c, n=0) == ie.OK
+    for kw in (dict(cap=-1.0), dict(cap=float("nan")), dict(cap=float("inf")), dict(cap=1e-19), dict(cap=2e18), dict(scale=float("inf")),
+               dict(ctx=None), dict(heads=6)):
+        assert _scored(c, **kw) == ie.EINVAL, kw
+
+
+def test_workspace_of_a_4_bit_cache():
+    sizes = []
+    for kind in (ie.KV_BF16, ie.KV_MX4):
+        n = ctypes.c_size_t()
+        assert ie.lib().iefwd_paged_attention_workspace(ctypes.byref(_desc(kv_type=kind)), 3, 8, 200, ctypes.byref(n)) == ie.OK
+        sizes.append(n.value)
+    assert sizes[0] == sizes[1] > 0
