@@ -790,6 +790,37 @@ int iefwd_mx4_gemm(uint32_t epilogue, const void *a, const void *w, const void *
 int iefwd_mx4_gemm_bf16(uint32_t epilogue, const void *a, const void *w, const void *bias, const float *resid, void *out,
                         uint32_t M, uint32_t N, uint32_t K, void *stream);
 
+/* ---- log probabilities of tokens ----------------------------------------------------------
+ * What a generation server answers with its tokens, and what training on sampled tokens needs: for rows
+ * of logits over a vocabulary, with p = softmax(scale * x) (scale: the inverse of a temperature),
+ * the log probability of a given token, the entropy -sum p log p and the n_top most probable tokens.
+ * Calls launch on `stream` of the current device, return without synchronising, allocate nothing and
+ * may be captured.  logits IEFWD_BF16 or IEFWD_F32 [rows, vocab], rows stride >= vocab elements apart, no
+ * alignment beyond the type's; fp32 sums relative to the row's largest logit; the same bits on every call. */
+
+/* Bytes of workspace that iefwd_token_logprobs needs (0 where rows are not cut into parts). Host only. */
+int iefwd_token_logprobs_workspace(uint32_t rows, uint32_t vocab, uint32_t n_top, size_t *bytes);
+
+/* tokens int64 [rows]; logprobs f32 [rows], 0 for a token outside [0, vocab) (padding); entropy f32 [rows] or NULL; stats
+ * f32 [rows, 2] or NULL, for iefwd_token_logprobs_grad: the largest logit, and log sum exp(scale (x - largest)).
+ * top_ids int32 [rows, n_top] and top_logprobs f32 [rows, n_top]: in falling order, of equal logits the lowest index first,
+ * NaN above all numbers.  Logits of -inf are masked tokens: log probability -inf; a row of nothing else has
+ * entropy 0 and log probabilities of -inf, a row with a NaN or +inf has NaN for both.
+ * 1 <= rows <= 2^22, 1 <= vocab <= 2^24, rows * vocab <= 2^35, n_top <= min(32, vocab), scale in [2^-30, 2^30].
+ * workspace: iefwd_token_logprobs_workspace bytes, 16-byte aligned, any contents; calls that may overlap need
+ * one each. */
+int iefwd_token_logprobs(uint32_t type, const void *logits, uint64_t stride, uint32_t rows, uint32_t vocab,
+                         const int64_t *tokens, float scale, float *logprobs, float *entropy, float *stats, uint32_t n_top,
+                         int32_t *top_ids, float *top_logprobs, void *workspace, size_t workspace_bytes, void *stream);
+
+/* out (type and shape of logits, rows out_stride apart; may be logits themselves) = the gradient of sum_r grad_logprobs[r]
+ * logprobs[r] + grad_entropy[r] entropy[r] by the logits, f32 [rows] each or NULL (0), not both; entropy as computed above,
+ * needed with grad_entropy.  A token outside [0, vocab) has no part in it, a row of -inf alone gets zeros. */
+int iefwd_token_logprobs_grad(uint32_t type, const void *logits, uint64_t stride, uint32_t rows, uint32_t vocab,
+                              const int64_t *tokens, float scale, const float *stats, const float *entropy,
+                              const float *grad_logprobs, const float *grad_entropy, void *out, uint64_t out_stride,
+                              void *stream);
+
 /* CU residency probe: launches n_groups workgroups of 64 threads on `stream`;
  * workgroup g writes out[2g] = XCC id, out[2g+1] = the hardware id register
  * (CU, SIMD, shader-array and shader-engine fields).  out: device uint32

@@ -107,6 +107,9 @@ SIGNATURES = {
     "iefwd_mx4_values": (_i32, [_vp, _u32, _vp, _u64, _u32, _u32, _vp]),
     "iefwd_mx4_gemm": (_i32, [_u32, _vp, _vp, _vp, _vp, _vp, _u32, _u32, _u32, _vp]),
     "iefwd_mx4_gemm_bf16": (_i32, [_u32, _vp, _vp, _vp, _vp, _vp, _u32, _u32, _u32, _vp]),
+    "iefwd_token_logprobs_workspace": (_i32, [_u32, _u32, _u32, ctypes.POINTER(_sz)]),
+    "iefwd_token_logprobs": (_i32, [_u32, _vp, _u64, _u32, _u32, _vp, _f32, _vp, _vp, _vp, _u32, _vp, _vp, _vp, _sz, _vp]),
+    "iefwd_token_logprobs_grad": (_i32, [_u32, _vp, _u64, _u32, _u32, _vp, _f32, _vp, _vp, _vp, _vp, _vp, _u64, _vp]),
     "iefwd_decode_attention_noalloc": (_i32, [_vp, _vp, _vp, _vp, _u32, _u32, _u32, _u32, _u32, _u32, _vp]),
 }
 
@@ -798,6 +801,79 @@ class Mx4Matrix:
             name, at = "iefwd_mx4_gemm_bf16", a.data_ptr()
         _call(dev, stream, name, epilogue, at, self._at, None if bias is None else bias.data_ptr(),
               resid.data_ptr() if f32 else None, out.data_ptr(), m, n, k)
+
+
+# ------------------------------------------------------------------ log probabilities of tokens
+def token_logprobs_workspace(rows: int, vocab: int, n_top: int = 0, device="cuda:0") -> torch.Tensor:
+    """A workspace for ``token_logprobs``, in memory of torch's current stream: calls on another one have to be ordered
+    behind it, and the workspace to live until they have run."""
+    n = _sz()
+    _check(lib().iefwd_token_logprobs_workspace(rows, vocab, n_top, ctypes.byref(n)), "iefwd_token_logprobs_workspace")
+    return torch.empty(n.value, dtype=torch.uint8, device=device)
+
+
+def _logits(name: str, t) -> tuple[int, int, int, int, int]:
+    """Checks bf16 or fp32 [rows, vocab] with contiguous rows; returns its GPU, type, sizes and row stride."""
+    if not isinstance(t, torch.Tensor) or t.dtype not in _FLOATS or not t.is_cuda:
+        raise ValueError(f"{name} must be a bfloat16 or float32 tensor on the GPU")
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be [rows, vocab] with each row contiguous")
+    rows, vocab = t.shape
+    return t.get_device(), _FLOATS[t.dtype], rows, vocab, t.stride(0) if rows > 1 else vocab
+
+
+def token_logprobs(logits, tokens, logprobs, workspace, entropy=None, stats=None, top_ids=None, top_logprobs=None,
+                   scale: float = 1.0, stream=None) -> None:
+    """Log probabilities under softmax(scale * logits) (``iefwd_token_logprobs``): logits bf16 or fp32 [rows, vocab], whose rows
+    may lie apart, tokens int64 [rows] (outside the vocabulary: 0); fp32 logprobs and, if given, entropy [rows], stats [rows, 2]
+    for ``token_logprobs_grad``, and the most probable tokens, int32 top_ids and fp32 top_logprobs [rows, n].  Runs on
+    `stream`, by default torch's current stream of the logits' GPU."""
+    dev, kind, rows, vocab, stride = _logits("logits", logits)
+    f32 = torch.float32
+    n = 0 if top_ids is None else top_ids.shape[-1]
+    if not (_is(tokens, torch.int64, dev, (rows,)) and _is(logprobs, f32, dev, (rows,)) and
+            (entropy is None or _is(entropy, f32, dev, (rows,))) and (stats is None or _is(stats, f32, dev, (rows, 2))) and
+            (top_ids is None or _is(top_ids, torch.int32, dev, (rows, n))) and
+            (top_logprobs is None if top_ids is None else _is(top_logprobs, f32, dev, (rows, n))) and
+            _is(workspace, torch.uint8, dev, (workspace.numel(),) if isinstance(workspace, torch.Tensor) else ())):
+        _need("tokens", tokens, torch.int64, dev, (rows,))
+        _need("logprobs", logprobs, f32, dev, (rows,))
+        for name, t, shape in (("entropy", entropy, (rows,)), ("stats", stats, (rows, 2))):
+            if t is not None:
+                _need(name, t, f32, dev, shape)
+        if (top_ids is None) != (top_logprobs is None):
+            raise ValueError("top_ids and top_logprobs come together")
+        if top_ids is not None:
+            _need("top_ids", top_ids, torch.int32, dev, (rows, n))
+            _need("top_logprobs", top_logprobs, f32, dev, (rows, n))
+        _need("workspace", workspace, torch.uint8, dev)
+        _need("workspace", workspace, torch.uint8, dev, (workspace.numel(),))
+    _call(dev, stream, "iefwd_token_logprobs", kind, logits.data_ptr(), stride, rows, vocab, tokens.data_ptr(), scale,
+          logprobs.data_ptr(), None if entropy is None else entropy.data_ptr(), None if stats is None else stats.data_ptr(), n,
+          top_ids.data_ptr() if n else None, top_logprobs.data_ptr() if n else None, workspace.data_ptr(), workspace.numel())
+
+
+def token_logprobs_grad(logits, tokens, stats, out, grad_logprobs=None, entropy=None, grad_entropy=None, scale: float = 1.0,
+                        stream=None) -> None:
+    """out [rows, vocab] = the gradient by the logits of sum(grad_logprobs * logprobs + grad_entropy * entropy) (fp32 [rows], at
+    least one), with the arguments, stats and entropy of ``token_logprobs``; out as logits, whose rows may lie apart, or logits
+    themselves."""
+    dev, kind, rows, vocab, stride = _logits("logits", logits)
+    out_dev, out_kind, out_rows, out_vocab, out_stride = _logits("out", out)
+    if (out_dev, out_kind, out_rows, out_vocab) != (dev, kind, rows, vocab):
+        raise ValueError("out must be as logits")
+    f32 = torch.float32
+    given = (("grad_logprobs", grad_logprobs), ("entropy", entropy), ("grad_entropy", grad_entropy))
+    if not (_is(tokens, torch.int64, dev, (rows,)) and _is(stats, f32, dev, (rows, 2)) and
+            all(t is None or _is(t, f32, dev, (rows,)) for _, t in given)):
+        _need("tokens", tokens, torch.int64, dev, (rows,))
+        _need("stats", stats, f32, dev, (rows, 2))
+        for name, t in given:
+            if t is not None:
+                _need(name, t, f32, dev, (rows,))
+    _call(dev, stream, "iefwd_token_logprobs_grad", kind, logits.data_ptr(), stride, rows, vocab, tokens.data_ptr(), scale,
+          stats.data_ptr(), *[None if t is None else t.data_ptr() for t in (entropy, grad_logprobs, grad_entropy)],
+          out.data_ptr(), out_stride)
 
 
 # ------------------------------------------------------------------ quota controller

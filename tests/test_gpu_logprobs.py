@@ -1,0 +1,316 @@
+"""Token log probabilities, entropy, alternatives and their gradient on the GPU against 64 bits."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2503_05130_amd as ie
+from tests.gpu_util import DEV, f64, sync
+
+pytestmark = pytest.mark.gpu
+
+BF, F32 = torch.bfloat16, torch.float32
+
+
+def _logits(rows, vocab, dtype, seed, spread=2.5, masked=0.0):
+    g = torch.Generator().manual_seed(seed)
+    x = spread * torch.randn(rows, vocab, generator=g)
+    sure = torch.arange(0, rows, 2)
+    tokens = torch.randint(0, vocab, (rows,), generator=g)
+    x[sure, tokens[sure]] += 12.0
+    if masked:
+        hide = torch.rand(rows, vocab, generator=g) < masked
+        hide[torch.arange(rows), tokens] = False
+        x[hide] = -math.inf
+    return x.to(dtype), tokens
+
+
+def _apart(x, gap, first=0):
+    """x on the GPU as a slice of wider rows."""
+    wide = torch.full((x.shape[0], x.shape[1] + gap + first), 99.0, dtype=x.dtype, device=DEV)
+    part = wide[:, first:first + x.shape[1]]
+    part.copy_(x)
+    return part
+
+
+def _run(x, tokens, n, scale):
+    rows, vocab = x.shape
+    out = dict(logprobs=torch.full((rows,), 7.0, device=DEV), entropy=torch.full((rows,), 7.0, device=DEV),
+               stats=torch.full((rows, 2), 7.0, device=DEV))
+    if n:
+        out |= dict(top_ids=torch.full((rows, n), -7, dtype=torch.int32, device=DEV), top_logprobs=torch.full((rows, n), 7.0, device=DEV))
+    ws = ie.token_logprobs_workspace(rows, vocab, n)
+    ws.fill_(0xFF)
+    lp = out["logprobs"]
+    ie.token_logprobs(x, tokens.to(DEV), lp, ws, scale=scale, **{k: v for k, v in out.items() if k != "logprobs"})
+    sync()
+    return out
+
+
+def _plain(x, tokens, scale):
+    """fp64 on the CPU: log probabilities of every token and of the given ones, entropy, and the error bounds of the two.
+
+    A term e^(s d): its exponent is off by 2^-22 |s d| (difference, product, log2 e), the exponential by 2^-21; the sums of a lane,
+    a wave and the parts by 2^-24 an addition; log S by that and a rounding."""
+    x = x.double()
+    m = x.amax(1, keepdim=True)
+    sd = (x - m) * scale
+    p = torch.exp(sd)
+    total = p.sum(1, keepdim=True)
+    p = p / total
+    logp = sd - torch.log(total)
+    size = torch.where(p > 0, p * sd.abs(), 0.0).sum(1)             # E |s d|
+    h = -torch.where(p > 0, p * logp, 0.0).sum(1)
+    es = 2.0 ** -20 + 2.0 ** -22 * size + (x.shape[1] / 256 + 120) * 2.0 ** -24
+    given = torch.gather(logp, 1, tokens.clamp(0, x.shape[1] - 1)[:, None])[:, 0]
+    sdt = torch.gather(sd, 1, tokens.clamp(0, x.shape[1] - 1)[:, None])[:, 0].abs()
+    tol_lp = es + 2.0 ** -22 * (torch.where(sdt.isfinite(), sdt, 0.0) + torch.log(total)[:, 0])
+    tol_h = 2 * es * (1 + size) + 2.0 ** -22 * (h.abs() + torch.log(total)[:, 0])
+    return dict(logp=logp, p=p, given=given, h=h, tol_lp=tol_lp, tol_h=tol_h)
+
+
+def _best(x, n):
+    return torch.sort(x.cpu(), dim=1, descending=True, stable=True).indices[:, :n]
+
+
+def _check(x, tokens, n, scale=1.0, gap=0, first=0):
+    got = _run(_apart(x, gap, first), tokens, n, scale)
+    want = _plain(x, tokens, scale)
+    ok = (tokens >= 0) & (tokens < x.shape[1])
+    lp = torch.where(ok, want["given"], 0.0)
+    g = got["logprobs"].cpu().double()
+    both = (g == lp) | ((g - lp).abs() <= want["tol_lp"])
+    assert both.all(), (g[~both][:4], lp[~both][:4])
+    assert ((got["entropy"].cpu().double() - want["h"]).abs() <= want["tol_h"]).all()
+    if n:
+        ids = _best(x, n)
+        assert torch.equal(got["top_ids"].cpu().long(), ids)
+        top, want_top = got["top_logprobs"].cpu().double(), torch.gather(want["logp"], 1, ids)
+        far = torch.where(want_top.isfinite(), want_top.abs(), 0.0)
+        assert ((top == want_top) | ((top - want_top).abs() <= want["tol_lp"][:, None] + 2.0 ** -21 * far)).all()
+    return got, want
+
+
+VOCABS = [1, 2, 7, 64, 100, 255, 1500, 2049, 8191, 8192, 8193, 20001]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("vocab", VOCABS)
+@pytest.mark.parametrize("rows,n,scale,gap,first", [(1, 5, 1.0, 0, 0), (3, 0, 0.7, 13, 0), (70, 32, 1.0, 8, 0), (9, 1, 1.4, 1, 3), (600, 20, 1.0, 0, 0)])
+def test_rows(dtype, vocab, rows, n, scale, gap, first):
+    x, tokens = _logits(rows, vocab, dtype, rows * 7 + vocab)
+    _check(x, tokens, min(n, vocab), scale, gap, first)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows,vocab", [(1, 131072), (2, 524289), (17, 65003), (1, 1 << 20)])
+def test_long_rows(dtype, rows, vocab):
+    x, tokens = _logits(rows, vocab, dtype, vocab)
+    _check(x, tokens, 32, gap=5)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("vocab", [40, 3000, 70000])
+@pytest.mark.parametrize("masked", [0.5, 0.99, 1.0])
+def test_masked_tokens(dtype, vocab, masked):
+    x, tokens = _logits(12, vocab, dtype, vocab, masked=masked)
+    _check(x, tokens, 32)
+    _check(x, (tokens + 1) % vocab, 20)          # mostly masked themselves: -inf
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("vocab", [33, 5000, 70001])
+def test_equal_rising_and_falling_logits(dtype, vocab):
+    """Ties everywhere, and orders in which every number is a new candidate."""
+    up = torch.linspace(-20, 20, vocab)
+    rows = [torch.zeros(vocab), up, -up, (up * 3).round() / 3, torch.where(torch.arange(vocab) % 2 == 0, 0.0, -0.0), -torch.ones(vocab) * 7,
+            (torch.arange(vocab) % 64).float(), torch.full((vocab,), -3e38)]
+    x = torch.stack(rows).to(dtype)
+    _check(x, torch.arange(len(rows)) % vocab, 32)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("vocab", [50, 9000, 40000])
+def test_rows_without_numbers(dtype, vocab):
+    x, tokens = _logits(6, vocab, dtype, 5)
+    x[0] = -math.inf
+    x[1, vocab // 2] = math.nan
+    x[2, vocab - 1] = math.inf
+    x[3] = math.nan
+    x[4, 3], x[4, 40] = math.nan, math.inf
+    out = _run(_apart(x, 3), tokens, 5, 1.0)
+    lp, h, ids, top = (out[k].cpu() for k in ("logprobs", "entropy", "top_ids", "top_logprobs"))
+    assert lp[0] == -math.inf and h[0] == 0.0 and (top[0] == -math.inf).all() and ids[0].tolist() == [0, 1, 2, 3, 4]
+    for r in (1, 2, 3, 4):
+        assert lp[r].isnan() and h[r].isnan() and top[r].isnan().all(), r
+    assert ids[1, 0] == vocab // 2 and ids[2, 0] == vocab - 1 and ids[3].tolist() == [0, 1, 2, 3, 4] and ids[4, :2].tolist() == [3, 40]
+    rest = x[1].clone().float()
+    rest[vocab // 2] = math.inf
+    assert ids[1].tolist() == _best(rest[None], 5)[0].tolist()
+    want = _plain(x[5:], tokens[5:], 1.0)
+    assert abs(float(lp[5]) - float(want["given"])) <= float(want["tol_lp"])
+    # gradients: zeros for the empty row, NaN for the others
+    g = torch.ones(6, device=DEV)
+    d = torch.full((6, vocab), 7.0, dtype=dtype, device=DEV)
+    ie.token_logprobs_grad(x.to(DEV), tokens.to(DEV), out["stats"], d, grad_logprobs=g, entropy=out["entropy"], grad_entropy=g)
+    sync()
+    assert (d[0] == 0).all() and d[1:5].isnan().all() and d[5].isfinite().all()
+
+
+def test_tokens_outside_the_vocabulary():
+    x, _ = _logits(6, 300, F32, 9)
+    tokens = torch.tensor([-100, -1, 300, 2 ** 40, -2 ** 62, 299])
+    got, _ = _check(x, tokens, 3)
+    g = torch.ones(6, device=DEV)
+    d = torch.full((6, 300), 7.0, device=DEV)
+    ie.token_logprobs_grad(x.to(DEV), tokens.to(DEV), got["stats"], d, grad_logprobs=g)
+    sync()
+    assert (d[:5] == 0).all() and (d[5] != 0).any()
+
+
+def _grad_case(rows, vocab, dtype, scale, seed, masked=0.0):
+    x, tokens = _logits(rows, vocab, dtype, seed, masked=masked)
+    g = torch.Generator().manual_seed(seed + 1)
+    gl, gh = torch.randn(rows, generator=g), torch.randn(rows, generator=g)
+    if rows > 3:
+        tokens[3] = -100
+    want = _plain(x, tokens, scale)
+    ok = (tokens >= 0)
+    hot = torch.zeros_like(want["p"]).scatter_(1, tokens.clamp(min=0)[:, None], 1.0) * ok[:, None]
+    lp = torch.clamp(want["logp"], min=-1e6)
+    wl, wh = (gl.double() * ok)[:, None], gh.double()[:, None]
+    ref = scale * (wl * (hot - want["p"]) - wh * want["p"] * (lp + want["h"][:, None]))
+    # p: log p's own error (its rounding 2^-21 and those of the row's sums) and the exponential; then the factors'
+    ep = want["tol_lp"][:, None] + 2.0 ** -21 * lp.abs() + 2.0 ** -20
+    tol = scale * (want["p"] * (wl.abs() * ep + wh.abs() * ((lp + want["h"][:, None]).abs() * ep + ep + want["tol_h"][:, None]))
+                   + 2.0 ** -22 * wl.abs() * hot) + 2.0 ** -22 * ref.abs() + 2.0 ** -100
+    if dtype is BF:
+        tol = tol * (1 + 2.0 ** -8) + 2.0 ** -8 * ref.abs()
+    return x, tokens, gl, gh, ref, tol
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("vocab", [1, 6, 100, 4096, 8200, 33001])
+@pytest.mark.parametrize("rows,scale,gap,out_gap,masked", [(1, 1.0, 0, 0, 0.0), (5, 1.3, 13, 8, 0.9), (40, 0.7, 8, 1, 0.0), (33, 1.0, 1, 0, 0.0)])
+def test_gradient(dtype, vocab, rows, scale, gap, out_gap, masked):
+    x, tokens, gl, gh, ref, tol = _grad_case(rows, vocab, dtype, scale, rows + vocab, masked)
+    xd, td = _apart(x, gap), tokens.to(DEV)
+    got = _run(xd, tokens, 0, scale)
+    wide = torch.full((rows + 1, vocab + out_gap), 5.0, dtype=dtype, device=DEV)
+    d = wide[:rows, :vocab]
+    ie.token_logprobs_grad(xd, td, got["stats"], d, gl.to(DEV), got["entropy"], gh.to(DEV), scale)
+    sync()
+    assert ((d.cpu().double() - ref).abs() <= tol).all()
+    assert (wide[rows] == 5.0).all() and (wide[:, vocab:] == 5.0).all()
+    # one of the two alone: the other's is 0
+    both = d.clone().double()
+    ie.token_logprobs_grad(xd, td, got["stats"], d, gl.to(DEV), scale=scale)
+    one = d.clone().double()
+    ie.token_logprobs_grad(xd, td, got["stats"], d, entropy=got["entropy"], grad_entropy=gh.to(DEV), scale=scale)
+    sync()
+    size = (one.abs() + d.double().abs()).cpu()
+    assert ((one + d.double() - both).abs().cpu() <= 4 * tol + (2.0 ** -7 if dtype is BF else 2.0 ** -20) * size).all()
+    # in the logits' own place
+    ie.token_logprobs_grad(xd, td, got["stats"], xd, gl.to(DEV), got["entropy"], gh.to(DEV), scale)
+    sync()
+    assert torch.equal(xd.double(), both)
+
+
+def test_gradient_against_differences():
+    rows, vocab, scale, step = 4, 37, 0.8, 2.0 ** -5
+    x, tokens, gl, gh, _, _ = _grad_case(rows, vocab, F32, scale, 77)
+    got = _run(x.to(DEV), tokens, 0, scale)
+    d = torch.empty((rows, vocab), device=DEV)
+    ie.token_logprobs_grad(x.to(DEV), tokens.to(DEV), got["stats"], d, gl.to(DEV), got["entropy"], gh.to(DEV), scale)
+    sync()
+    d = d.cpu().double()
+    for j in range(vocab):
+        ends = []
+        for sign in (1, -1):
+            y = x.clone()
+            y[:, j] += sign * step
+            o = _run(y.to(DEV), tokens, 0, scale)
+            ends.append(gl.double() * o["logprobs"].cpu().double() + gh.double() * o["entropy"].cpu().double())
+        # the third derivative is at most 30 of these weights; the values are good to 1e-5
+        weight = gl.abs().double() + gh.abs().double() * 5
+        assert ((ends[0] - ends[1]) / (2 * step) - d[:, j]).abs().le(weight * (30 * step ** 2 / 6 + 1e-5 / step)).all()
+
+
+def test_rows_do_not_depend_on_each_other_and_calls_repeat():
+    x, tokens = _logits(30, 20000, BF, 3)
+    a = _run(x.to(DEV), tokens, 8, 1.0)
+    order = torch.randperm(30, generator=torch.Generator().manual_seed(4))
+    b = _run(x[order].to(DEV), tokens[order], 8, 1.0)
+    for k in a:
+        assert torch.equal(a[k][order.to(DEV)], b[k]), k
+
+
+def test_captured_and_on_two_streams():
+    rows, vocab, n = 40, 30011, 6
+    x, tokens = _logits(rows, vocab, BF, 21)
+    xd, td = x.to(DEV), tokens.to(DEV)
+    outs = [dict(logprobs=torch.zeros(rows, device=DEV), entropy=torch.zeros(rows, device=DEV), stats=torch.zeros(rows, 2, device=DEV),
+                 top_ids=torch.zeros(rows, n, dtype=torch.int32, device=DEV), top_logprobs=torch.zeros(rows, n, device=DEV)) for _ in range(3)]
+    ds = [torch.zeros_like(xd) for _ in range(3)]
+    spaces = [ie.token_logprobs_workspace(rows, vocab, n) for _ in range(3)]
+    g = torch.randn(rows, device=DEV)
+
+    def both(i, stream=None):
+        o = outs[i]
+        ie.token_logprobs(xd, td, o["logprobs"], spaces[i], o["entropy"], o["stats"], o["top_ids"], o["top_logprobs"], stream=stream)
+        ie.token_logprobs_grad(xd, td, o["stats"], ds[i], g, o["entropy"], g, stream=stream)
+
+    sync()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both(0)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for seed in (22, 23, 24):
+        y, t = _logits(rows, vocab, BF, seed)
+        xd.copy_(y)
+        td.copy_(t)
+        sync()
+        graph.replay()
+        for i, s in ((1, streams[0]), (2, streams[1])):
+            both(i, s)
+        sync()
+        want = _plain(y, t, 1.0)
+        assert ((outs[0]["logprobs"].cpu().double() - want["given"]).abs() <= want["tol_lp"]).all()
+        for i in (1, 2):
+            assert torch.equal(ds[0], ds[i]) and all(torch.equal(outs[0][k], outs[i][k]) for k in outs[0])
+
+
+def test_refusals_of_the_binding():
+    x, tokens = _logits(4, 50, BF, 1)
+    xd, td = x.to(DEV), tokens.to(DEV)
+    lp, ws = torch.full((4,), 3.0, device=DEV), ie.token_logprobs_workspace(4, 50, 5)
+    ids, top = torch.zeros(4, 5, dtype=torch.int32, device=DEV), torch.zeros(4, 5, device=DEV)
+    base = dict(logits=xd, tokens=td, logprobs=lp, workspace=ws)
+    for bad in (dict(logits=xd.half()), dict(logits=x), dict(logits=xd.t()), dict(logits=xd[0]), dict(tokens=td.int()), dict(tokens=td[:3]),
+                dict(logprobs=lp.double()), dict(logprobs=lp[:2]), dict(entropy=lp[:3]), dict(stats=lp), dict(top_ids=ids),
+                dict(top_logprobs=top), dict(top_ids=ids.long(), top_logprobs=top), dict(top_ids=ids, top_logprobs=top[:, :4]),
+                dict(workspace=ws.float()), dict(workspace=None)):
+        with pytest.raises(ValueError):
+            ie.token_logprobs(**(base | bad))
+    for bad in (dict(scale=0.0), dict(scale=-1.0), dict(scale=math.nan), dict(scale=1e30), dict(logits=xd[:0], tokens=td[:0], logprobs=lp[:0]),
+                dict(top_ids=torch.zeros(4, 33, dtype=torch.int32, device=DEV), top_logprobs=torch.zeros(4, 33, device=DEV))):
+        with pytest.raises(ie.IefwdError) as e:
+            ie.token_logprobs(**(base | bad))
+        assert e.value.status == ie.EINVAL
+    long = torch.zeros(1, 50000, dtype=BF, device=DEV)
+    with pytest.raises(ie.IefwdError) as e:
+        ie.token_logprobs(long, td[:1], lp[:1], ws[:0])
+    assert "workspace" in str(e.value)
+    st, d = torch.zeros(4, 2, device=DEV), torch.zeros_like(xd)
+    base = dict(logits=xd, tokens=td, stats=st, out=d, grad_logprobs=lp)
+    for bad in (dict(out=d.float()), dict(out=d[:, :49]), dict(out=d[:3]), dict(stats=st[:3]), dict(tokens=td.int()), dict(grad_logprobs=lp[:1]),
+                dict(grad_entropy=lp.half()), dict(entropy=lp[:2])):
+        with pytest.raises(ValueError):
+            ie.token_logprobs_grad(**(base | bad))
+    for bad in (dict(grad_logprobs=None), dict(grad_entropy=lp), dict(scale=0.0)):
+        with pytest.raises(ie.IefwdError) as e:
+            ie.token_logprobs_grad(**(base | bad))
+        assert e.value.status == ie.EINVAL
+    sync()
+    assert (lp == 3.0).all()
