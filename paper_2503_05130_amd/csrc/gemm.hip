@@ -34,55 +34,12 @@
 namespace iefwd {
 namespace {
 
-// Workgroups are dispatched round-robin over the 8 XCDs.  Renumber them so
-// that each XCD receives a contiguous range of logical tiles (bijective for
-// any grid size), which keeps tiles that share operands in one XCD's L2.
-__device__ inline int xcd_contiguous(int i, int g) {
-    constexpr int X = 8;
-    const int q = g / X, r = g % X;
-    const int x = i % X, local = i / X;
-    return x < r ? x * (q + 1) + local : r * (q + 1) + (x - r) * q + local;
-}
-
-// Logical tile -> (token tile, feature tile), grouped 4 token tiles deep so
-// that workgroups running together share both A rows and W rows.
-__device__ inline void grouped_tile(int l, int tiles_m, int tiles_n, int &tm, int &tn) {
-    constexpr int G = 4;
-    const int per_group = G * tiles_n;
-    const int g = l / per_group;
-    const int first = g * G;
-    const int gsize = min(tiles_m - first, G);
-    const int in = l - g * per_group;
-    tm = first + in % gsize;
-    tn = in / gsize;
-}
-
 // 16-byte chunk position of logical chunk 0 in LDS row r of a K tile (row r
 // holds its chunk c at position c ^ swizzle(r)), chosen so that the 16 rows one
 // ds_read_b128 fragment load reads fall in distinct banks: consecutive 128-byte
 // rows alternate between the two halves of a 256-byte bank line, and within
 // each parity the 8 rows of a 16-row fragment get 8 distinct positions.
 __device__ inline int swizzle(int r) { return ((r >> 1) & 7) ^ ((r & 1) << 2); }
-
-// One global->LDS copy of 16 bytes per lane (1 KB per wave) to the
-// wave-uniform LDS byte address `lds`.  Issued through inline asm: the
-// compiler's wait-count model treats these copies as LDS traffic that may
-// complete out of order with LDS reads, and would then drain every
-// outstanding LDS read before each use of any of them; the main loop orders
-// the copies itself (s_waitcnt vmcnt before each barrier).  The M0 write
-// needs one wait state before the copy reads it.
-__device__ inline void dma16(const bf16_t *base, uint32_t off, uint32_t lds) {
-    uint32_t m0;   // the asm writes M0; naming it as an output tells the compiler so
-    asm volatile("s_mov_b32 %0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-                 : "={m0}"(m0)
-                 : "v"(off), "s"(base), "s"(lds)
-                 : "memory");
-    (void)m0;
-}
-
-// s_waitcnt immediate: wait until at most vm vector-memory and lgkm LDS
-// operations of this wave are outstanding (expcnt left unconstrained).
-constexpr int waitcnt_imm(int vm, int lgkm) { return (vm & 15) | (7 << 4) | ((lgkm & 15) << 8) | ((vm >> 4) << 14); }
 
 // Tile configuration: BM x BN output tile of WGM x WGN waves; A tiles and W
 // tiles of the K loop in a ring of S slots each, 64 K deep

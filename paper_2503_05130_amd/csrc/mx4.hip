@@ -1,4 +1,4 @@
-// Matrices in microscaled 4 bits for gfx950: quantisation, layout, values and products.
+// Matrices in microscaled 4 bits for gfx950: quantisation, layout and values.
 #include "mx4.h"
 
 #include <algorithm>
@@ -165,140 +165,6 @@ __global__ __launch_bounds__(256) void mx4_pack_kernel(const uint8_t *__restrict
     *reinterpret_cast<uint32_t *>(out + (size_t)chunks * 1024 + (size_t)g * 256 + lane * 4) = bytes;
 }
 
-// ------------------------------------------------------------------------------ products
-//
-// out^T = W A^T on the matrix cores, which take the codes and the scales as they are stored: a product of 16 features x 16
-// rows x 128 of K is one instruction of two 16-byte operands and a scale byte a lane, exact products summed in fp32.
-struct Mx4Params {
-    const char *a, *w;
-    const bf16_t *a16;           // A in bf16 instead
-    const bf16_t *bias;
-    const float *resid;
-    void *out;
-    int M, N, K;
-    int row_tiles;               // workgroups' tiles along M
-    Epi epi;
-};
-
-// Four features n .. n + 3 of row m.
-__device__ inline void mx4_store(const Mx4Params &p, int m, int n, f32x4 v) {
-    if (m >= p.M) return;
-    const int count = min(4, p.N - n);
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-        if (e < count && p.bias) v[e] += __uint_as_float((uint32_t)p.bias[n + e] << 16);
-    const size_t i = (size_t)m * p.N + n;
-    if (p.epi == Epi::BiasResidF32) {
-        float *out = static_cast<float *>(p.out) + i;
-        if ((p.N & 3) == 0) {
-            if (count > 0) *reinterpret_cast<f32x4 *>(out) = *reinterpret_cast<const f32x4 *>(p.resid + i) + v;
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (e < count) out[e] = p.resid[i + e] + v[e];
-        }
-        return;
-    }
-    if (p.epi == Epi::BiasGeluBf16)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = gelu(v[e]);
-    bf16_t *out = static_cast<bf16_t *>(p.out) + i;
-    if ((p.N & 3) == 0) {
-        if (count > 0) *reinterpret_cast<u32x2 *>(out) = u32x2{pack2(v[0], v[1]), pack2(v[2], v[3])};
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (e < count) out[e] = f32_to_bf16(v[e]);
-    }
-}
-
-// A workgroup's tile of 16 FT features x 16 RT rows with K spread over its waves, chunk by chunk, and the waves' sums
-// added in wave order through LDS.  Operands go from memory to registers.  NL > 0: A is bf16, 4 NL >= M rows: a chunk of them is loaded in
-// rows, quantised by quads of lanes and laid out as the operand in the wave's LDS.
-template <int FT, int RT, int WAVES, int NL>
-__global__ __launch_bounds__(64 * WAVES) void mx4_split_kernel(Mx4Params p) {
-    static_assert(NL == 0 || RT == 1, "bf16 rows are one tile");
-    constexpr int kStage = 1024 + 64;
-    constexpr int kLds = WAVES * FT * RT * 1024 > WAVES * kStage || NL == 0 ? WAVES * FT * RT * 1024 : WAVES * kStage;
-    __shared__ __attribute__((aligned(16))) char lds[kLds];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int r = lane & 15, c = lane >> 4;
-    const int chunks = mx4_chunks(p.K);
-    const size_t tile_bytes = mx4_tile_bytes(p.K);
-    const int ft0 = blockIdx.x / p.row_tiles * FT, rt0 = blockIdx.x % p.row_tiles * RT;
-    const int last_f = (p.N + 15) / 16 - 1, last_r = (p.M + 15) / 16 - 1;
-    const char *w[FT], *a[RT];      // a tile past the last reads the last one and is not stored
-#pragma unroll
-    for (int f = 0; f < FT; ++f) w[f] = p.w + (size_t)min(ft0 + f, last_f) * tile_bytes;
-    if (NL == 0)
-#pragma unroll
-        for (int t = 0; t < RT; ++t) a[t] = p.a + (size_t)min(rt0 + t, last_r) * tile_bytes;
-    char *stage = lds + wave * kStage;
-    f32x4 acc[FT][RT] = {};
-    for (int j = wave; j < chunks; j += WAVES) {
-        const size_t scales = (size_t)chunks * 1024 + (size_t)(j >> 2) * 256 + lane * 4;
-        const int shift = 8 * (j & 3);
-        u32x4 wf[FT], af[RT];
-        uint32_t ws[FT], as[RT];
-#pragma unroll
-        for (int f = 0; f < FT; ++f) {
-            wf[f] = *reinterpret_cast<const u32x4 *>(w[f] + (size_t)j * 1024 + lane * 16);
-            ws[f] = *reinterpret_cast<const uint32_t *>(w[f] + scales) >> shift;
-        }
-        if constexpr (NL == 0) {
-#pragma unroll
-            for (int t = 0; t < RT; ++t) {
-                af[t] = *reinterpret_cast<const u32x4 *>(a[t] + (size_t)j * 1024 + lane * 16);
-                as[t] = *reinterpret_cast<const uint32_t *>(a[t] + scales) >> shift;
-            }
-        } else {
-            const int piece = lane & 15, col = j * 128 + 8 * piece;
-            Eight x[NL];
-#pragma unroll
-            for (int i = 0; i < NL; ++i) {
-                x[i] = Eight{};
-                if (col < p.K)
-                    x[i].lo = *reinterpret_cast<const u32x4 *>(p.a16 + (size_t)min(4 * i + (lane >> 4), p.M - 1) * p.K + col);
-            }
-#pragma unroll
-            for (int i = 0; i < NL; ++i) {
-                const int row = 4 * i + (lane >> 4), at = row + 16 * (piece >> 2);
-                const uint32_t scale = mx4_scale<false>(x[i]);
-                *reinterpret_cast<uint32_t *>(stage + at * 16 + (piece & 3) * 4) = mx4_codes<false>(x[i], scale);
-                if ((piece & 3) == 0) stage[1024 + at] = (char)scale;
-            }
-            // columns of rows past 4 NL hold whatever was there: they are sums of their own and not stored
-            af[0] = *reinterpret_cast<const u32x4 *>(stage + lane * 16);
-            as[0] = (uint8_t)stage[1024 + lane];
-        }
-#pragma unroll
-        for (int f = 0; f < FT; ++f)
-#pragma unroll
-            for (int t = 0; t < RT; ++t) acc[f][t] = mfma_mx4(wf[f], af[t], acc[f][t], ws[f], as[t]);
-    }
-    __syncthreads();
-    f32x4 (*part)[FT * RT][64] = reinterpret_cast<f32x4 (*)[FT * RT][64]>(lds);
-#pragma unroll
-    for (int f = 0; f < FT; ++f)
-#pragma unroll
-        for (int t = 0; t < RT; ++t) part[wave][f * RT + t][lane] = acc[f][t];
-    __syncthreads();
-    for (int b = wave; b < FT * RT; b += WAVES) {
-        f32x4 v = part[0][b][lane];
-#pragma unroll
-        for (int i = 1; i < WAVES; ++i) v += part[i][b][lane];
-        mx4_store(p, (rt0 + b % RT) * 16 + r, (ft0 + b / RT) * 16 + 4 * c, v);
-    }
-}
-
-template <int FT, int RT, int WAVES, int NL>
-hipError_t launch_split(Mx4Params p, hipStream_t stream) {
-    const int f_groups = ((p.N + 15) / 16 + FT - 1) / FT;
-    p.row_tiles = ((p.M + 15) / 16 + RT - 1) / RT;
-    return launch_kernel(mx4_split_kernel<FT, RT, WAVES, NL>, dim3((unsigned)((int64_t)f_groups * p.row_tiles)),
-                         dim3(64 * WAVES), stream, p);
-}
-
 }  // namespace
 
 hipError_t launch_mx4_quantize(bool f32, const void *x, int64_t stride, void *dst, int rows, int K, hipStream_t stream) {
@@ -331,22 +197,6 @@ hipError_t launch_mx4_values(const void *src, bool f32, void *out, int64_t strid
     };
     if (f32) return vector ? launch(mx4_values_kernel<true, true>) : launch(mx4_values_kernel<true, false>);
     return vector ? launch(mx4_values_kernel<false, true>) : launch(mx4_values_kernel<false, false>);
-}
-
-hipError_t launch_mx4_gemm(Epi epi, const void *a, const void *w, const bf16_t *bias, const float *resid, void *out, int M,
-                           int N, int K, hipStream_t stream) {
-    Mx4Params p{static_cast<const char *>(a), static_cast<const char *>(w), nullptr, bias, resid, out, M, N, K, 0, epi};
-    if (M <= 16) return launch_split<1, 1, 8, 0>(p, stream);
-    if (M <= 32) return launch_split<2, 2, 8, 0>(p, stream);
-    return launch_split<4, 4, 4, 0>(p, stream);
-}
-
-hipError_t launch_mx4_gemm_bf16(Epi epi, const bf16_t *a, const void *w, const bf16_t *bias, const float *resid, void *out,
-                                int M, int N, int K, hipStream_t stream) {
-    Mx4Params p{nullptr, static_cast<const char *>(w), a, bias, resid, out, M, N, K, 0, epi};
-    if (M <= 4) return launch_split<1, 1, 8, 1>(p, stream);
-    if (M <= 8) return launch_split<1, 1, 8, 2>(p, stream);
-    return launch_split<1, 1, 8, 4>(p, stream);
 }
 
 }  // namespace iefwd

@@ -79,11 +79,12 @@ __device__ inline u32x4 mx4_bf16(uint32_t codes, uint32_t scale_byte) {
 }
 
 // D += A B of 16 x 128 by 128 x 16 in 4 bits.  Lane l: row (column) l % 16 and the 32 of K from 32 (l / 16) on, of
-// which the lowest byte of its scale register is the scale; D as for every 16 x 16 product.
+// which byte B of its scale register is the scale; D as for every 16 x 16 product.
+template <int B = 0>
 __device__ inline f32x4 mfma_mx4(u32x4 a, u32x4 b, f32x4 d, uint32_t a_scale, uint32_t b_scale) {
     const i32x8 x = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0};
     const i32x8 y = {(int)b[0], (int)b[1], (int)b[2], (int)b[3], 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, d, 4, 4, 0, (int)a_scale, 0, (int)b_scale);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, d, 4, 4, B, (int)a_scale, B, (int)b_scale);
 }
 
 }  // namespace

@@ -274,3 +274,27 @@ def test_refusals_of_the_binding():
         with pytest.raises(ie.IefwdError) as e:
             call()
         assert e.value.status == ie.EINVAL
+
+
+@pytest.mark.parametrize("m,n,k", [(1100, 1040, 416), (1025, 1025, 128), (2100, 700, 1700), (3501, 3603, 384), (4096, 3500, 640), (8200, 1601, 96)])
+@pytest.mark.parametrize("epilogue", ["bias", "residual"])
+def test_many_rows(m, n, k, epilogue):
+    w, wv = _weight(n, k, n + k)
+    x, av = _given(m, k, m)
+    g = torch.Generator().manual_seed(m)
+    bias, resid = torch.randn(n, generator=g).to(BF), torch.randn(m, n, generator=g)
+    y = (torch.from_numpy(av) @ torch.from_numpy(wv).T).numpy() + f64(bias)
+    a = ie.Mx4Matrix(m, k)
+    a.quantize(to_dev(x))
+    if epilogue == "bias":
+        out = torch.full((m + 1, n), 7.0, dtype=BF, device=DEV)
+        w.product(a, out[:m], bias=to_dev(bias))
+    else:
+        out = torch.full((m + 1, n), 7.0, device=DEV)
+        w.product(a, out[:m], ie.EPI_BIAS_RESID_F32, bias=to_dev(bias), resid=to_dev(resid))
+        y = y + f64(resid)
+    sync()
+    assert (out[m:] == 7.0).all()
+    size = torch.from_numpy(np.abs(av)) @ torch.from_numpy(np.abs(wv)).T
+    tol = 2.0 ** -23 * (128 + -(-k // 128) + 12) * size.numpy() + 2.0 ** -21 * (np.abs(y) + np.abs(f64(resid)))
+    assert (np.abs(f64(out[:m]) - y) <= tol + (2.0 ** -8 * np.abs(y) if epilogue == "bias" else 0)).all()
