@@ -73,6 +73,7 @@ __global__ __launch_bounds__(64 * kWaves) void mx4_quantize_kernel(const char *_
             if (part == 0) stage[4096 + (r + 16 * c) * 4 + s] = (char)scale;
         }
     }
+    wave_lds_fence();
     char *out = dst + (size_t)tile * mx4_tile_bytes(K);
     const int r = lane & 15, cc = lane >> 4;
 #pragma unroll
@@ -106,6 +107,7 @@ __global__ __launch_bounds__(64 * kWaves) void mx4_values_kernel(const char *__r
         for (int j = 0; j < 4; ++j) *reinterpret_cast<u32x4 *>(stage + turned(r, c, j)) = w[j];
         *reinterpret_cast<uint32_t *>(stage + 4096 + lane * 4) = scales;
     }
+    wave_lds_fence();
     const int s = lane >> 4, c = (lane >> 2) & 3, part = lane & 3, col = 512 * g + 8 * lane;
     if (col >= K) return;
     const int n = min(16, rows - 16 * tile);

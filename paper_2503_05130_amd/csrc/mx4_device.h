@@ -17,6 +17,10 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
+// Between a wave's writes to its own LDS and other lanes' reads of them (and the other way round).  The hardware keeps a wave's LDS
+// accesses in order; without this the compiler may take what a lane has read before, or read it where the lane itself has written.
+__device__ inline void wave_lds_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
+
 // Eight neighbours of a lane, and 4 lanes (a quad) a block.
 struct Eight {
     u32x4 lo, hi;      // bf16: lo alone; fp32: both

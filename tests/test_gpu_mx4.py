@@ -276,7 +276,8 @@ def test_refusals_of_the_binding():
         assert e.value.status == ie.EINVAL
 
 
-@pytest.mark.parametrize("m,n,k", [(1100, 1040, 416), (1025, 1025, 128), (2100, 700, 1700), (3501, 3603, 384), (4096, 3500, 640), (8200, 1601, 96)])
+@pytest.mark.parametrize("m,n,k", [(1100, 1040, 416), (1025, 1025, 128), (2100, 700, 1700), (3501, 3603, 384), (4096, 3500, 640), (8200, 1601, 96),
+                                   (2100, 2100, 300), (1601, 2304, 1152), (4000, 1500, 2700), (3500, 3600, 2176), (1100, 1040, 4160)])
 @pytest.mark.parametrize("epilogue", ["bias", "residual"])
 def test_many_rows(m, n, k, epilogue):
     w, wv = _weight(n, k, n + k)
@@ -298,3 +299,20 @@ def test_many_rows(m, n, k, epilogue):
     size = torch.from_numpy(np.abs(av)) @ torch.from_numpy(np.abs(wv)).T
     tol = 2.0 ** -23 * (128 + -(-k // 128) + 12) * size.numpy() + 2.0 ** -21 * (np.abs(y) + np.abs(f64(resid)))
     assert (np.abs(f64(out[:m]) - y) <= tol + (2.0 ** -8 * np.abs(y) if epilogue == "bias" else 0)).all()
+
+
+@pytest.mark.parametrize("m", [1, 6, 16, 29])
+@pytest.mark.parametrize("n,k", [(8200, 160), (16400, 672), (96, 8192), (40, 16500), (8208, 8320)])
+def test_few_rows_of_wide_and_long_matrices(m, n, k):
+    w, wv = _weight(n, k, n + k)
+    x, av = _given(m, k, m)
+    y = (torch.from_numpy(av) @ torch.from_numpy(wv).T).numpy()
+    size = (torch.from_numpy(np.abs(av)) @ torch.from_numpy(np.abs(wv)).T).numpy()
+    tol = 2.0 ** -23 * (128 + -(-k // 128) + 12) * size + 2.0 ** -22 * np.abs(y) + 2.0 ** -8 * np.abs(y)
+    a = ie.Mx4Matrix(m, k)
+    a.quantize(to_dev(x))
+    for way in [a] + ([to_dev(x)] if m <= 16 and k % 8 == 0 else []):
+        out = torch.full((m + 1, n), 7.0, dtype=BF, device=DEV)
+        w.product(way, out[:m])
+        sync()
+        assert (np.abs(f64(out[:m]) - y) <= tol).all() and (out[m:] == 7.0).all()
