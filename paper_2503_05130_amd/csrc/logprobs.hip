@@ -12,13 +12,13 @@
 #include <algorithm>
 #include <cmath>
 
-#include "gemm_device.h"
+#include "mx4_device.h"
 
 namespace iefwd {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLeast = -3.0e38f;
-constexpr int kWaves = 4, kThreads = 64 * kWaves;
+constexpr int kThreads = 256;
 constexpr int kBuffer = 128;      // candidates of a wave
 
 // Rows may begin anywhere: 16-byte loads and stores of any alignment, which the memory of gfx950 takes.
@@ -78,17 +78,35 @@ struct Sums {
     }
 };
 
+// Over all lanes by row shifts of 1, 2, 4 and 8, then lane 15's row result to the next row and lane 31's to the upper half.
+template <class Op>
+__device__ inline uint32_t over_wave(uint32_t v, uint32_t neutral, Op op) {
+    v = op(v, (uint32_t)__builtin_amdgcn_update_dpp((int)neutral, (int)v, 0x111, 0xf, 0xf, false));
+    v = op(v, (uint32_t)__builtin_amdgcn_update_dpp((int)neutral, (int)v, 0x112, 0xf, 0xf, false));
+    v = op(v, (uint32_t)__builtin_amdgcn_update_dpp((int)neutral, (int)v, 0x114, 0xf, 0xf, false));
+    v = op(v, (uint32_t)__builtin_amdgcn_update_dpp((int)neutral, (int)v, 0x118, 0xf, 0xf, false));
+    v = op(v, (uint32_t)__builtin_amdgcn_update_dpp((int)neutral, (int)v, 0x142, 0xa, 0xf, false));
+    v = op(v, (uint32_t)__builtin_amdgcn_update_dpp((int)neutral, (int)v, 0x143, 0xc, 0xf, false));
+    return __builtin_amdgcn_readlane(v, 63);
+}
+
+__device__ inline uint32_t largest_of(uint32_t v) {
+    return over_wave(v, 0, [](uint32_t x, uint32_t y) { return max(x, y); });
+}
+__device__ inline float sum_of(float v) {
+    return __uint_as_float(over_wave(__float_as_uint(v), 0, [](uint32_t x, uint32_t y) {
+        return __float_as_uint(__uint_as_float(x) + __uint_as_float(y));
+    }));
+}
+
 // All lanes' sums together, in every lane.
 __device__ inline Sums across_wave(Sums a, float c) {
-    float m = a.m;
-#pragma unroll
-    for (int i = 32; i >= 1; i >>= 1) m = top_of(m, __shfl_xor(m, i));
-    a.rescale(m, c);
-#pragma unroll
-    for (int i = 32; i >= 1; i >>= 1) {
-        a.s += __shfl_xor(a.s, i);
-        a.t += __shfl_xor(a.t, i);
-    }
+    a.rescale(__uint_as_float(over_wave(__float_as_uint(a.m), __float_as_uint(-INFINITY), [](uint32_t x, uint32_t y) {
+                  return __float_as_uint(top_of(__uint_as_float(x), __uint_as_float(y)));
+              })),
+              c);
+    a.s = sum_of(a.s);
+    a.t = sum_of(a.t);
     return a;
 }
 
@@ -113,60 +131,56 @@ __device__ inline void write_row(const LogprobArgs &a, int row, const Sums &s, f
 
 __device__ inline float log_sum(const Sums &s) { return s.m == -INFINITY ? 0.f : logf(s.s); }
 
-__device__ inline void write_top(const LogprobArgs &a, int row, int place, uint32_t key, int id, float m, float log_s) {
-    const float x = value_of(key, a.f32);
-    a.top_ids[(int64_t)row * a.top + place] = id;
+// A token that may be among the most probable: its logit's key above the complement of its index, so that the larger number comes
+// before the other.  0: none.
+typedef unsigned long long Candidate;
+typedef Candidate Candidate2 __attribute__((ext_vector_type(2)));
+
+__device__ inline Candidate candidate(uint32_t key, uint32_t id) { return (Candidate)key << 32 | (0xffffffffu - id); }
+
+__device__ inline void write_top(const LogprobArgs &a, int row, int place, Candidate c, float m, float log_s) {
+    const float x = value_of((uint32_t)(c >> 32), a.f32);
+    a.top_ids[(int64_t)row * a.top + place] = (int)(0xffffffffu - (uint32_t)c);
     a.top_logprobs[(int64_t)row * a.top + place] = x == -INFINITY ? (log_s != log_s ? log_s : x) : (x - m) * a.scale - log_s;
 }
 
-// A wave's candidates for the row's largest, in LDS.
-struct Candidates {
-    uint32_t key[kBuffer];
-    int id[kBuffer];
-};
-
-__device__ inline bool before(uint32_t ka, int ia, uint32_t kb, int ib) { return ka > kb || (ka == kb && ia < ib); }
-
-// Sorts the first `count` candidates, the largest first and of equal ones the lowest index, and keeps n of them.
-__device__ inline int keep_best(Candidates &b, int count, int n) {
+// Sorts a wave's first `count` candidates (in LDS, 16-byte aligned) and keeps n of them: a lane counts those before its own two,
+// eight at a time.
+__device__ inline int keep_best(Candidate *list, int count, int n) {
     const int lane = threadIdx.x & 63;
-    uint32_t key[2];
-    int id[2], rank[2] = {0, 0};
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");      // other lanes' candidates
+    if (lane < 8 && count + lane < kBuffer) list[count + lane] = 0;
+    wave_lds_fence();
+    Candidate own[2];
+    int rank[2] = {0, 0};
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int i = min(lane + 64 * h, kBuffer - 1);
-        key[h] = b.key[i];
-        id[h] = b.id[i];
-    }
-    for (int i = 0; i < count; ++i) {
-        const uint32_t k = b.key[i];
-        const int j = b.id[i];
+    for (int h = 0; h < 2; ++h) own[h] = lane + 64 * h < count ? list[lane + 64 * h] : 0;
+    for (int i = 0; i < count; i += 8) {
+        Candidate2 c[4];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) rank[h] += before(k, j, key[h], id[h]);
+        for (int j = 0; j < 4; ++j) c[j] = *reinterpret_cast<const Candidate2 *>(list + i + 2 * j);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) rank[h] += c[j / 2][j % 2] > own[h];
     }
+    wave_lds_fence();
 #pragma unroll
     for (int h = 0; h < 2; ++h)
-        if (lane + 64 * h < count && rank[h] < n) {
-            b.key[rank[h]] = key[h];
-            b.id[rank[h]] = id[h];
-        }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (own[h] && rank[h] < n) list[rank[h]] = own[h];
+    wave_lds_fence();
     return min(count, n);
 }
 
-// The workspace of a call whose rows are cut into parts: per row and part its sums, and its best candidates.
+// The workspace of a call whose rows are cut into parts: per row and part its best candidates, and its sums.
 struct Parts {
+    Candidate *best;
     Sums *sums;
-    uint32_t *keys;
-    int *ids;
 };
 
 __device__ __host__ inline Parts parts_in(void *ws, int64_t row_parts, int top) {
     Parts p;
-    p.sums = static_cast<Sums *>(ws);
-    p.keys = reinterpret_cast<uint32_t *>(p.sums + row_parts);
-    p.ids = reinterpret_cast<int *>(p.keys + row_parts * top);
+    p.best = static_cast<Candidate *>(ws);
+    p.sums = reinterpret_cast<Sums *>(p.best + row_parts * top);
     return p;
 }
 
@@ -177,23 +191,23 @@ __device__ __host__ inline Parts parts_in(void *ws, int64_t row_parts, int top) 
 // element; what exceeds it becomes a candidate, and equal ones up to n in the order of their indices.  From then on only
 // larger numbers do, which few are: one comparison a lane and tile finds that there are none.  A full buffer is sorted and cut to n, whose
 // last is the new border.
-template <bool F32, bool TOP>
-__global__ __launch_bounds__(kThreads) void logprobs_kernel(LogprobArgs a, int parts, int part) {
+template <bool F32, bool TOP, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void logprobs_kernel(LogprobArgs a, int parts, int part) {
     constexpr int N = Piece<F32>::N, kUnits = F32 ? 6 : 4, kTile = 64 * N * kUnits;
-    __shared__ Candidates best[TOP ? kWaves : 1];
-    __shared__ int counts[kWaves];
-    __shared__ Sums sums[kWaves];
+    __shared__ __attribute__((aligned(16))) Candidate best[TOP ? WAVES : 1][kBuffer];
+    __shared__ int counts[WAVES];
+    __shared__ Sums sums[WAVES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int row = blockIdx.x / parts, p = blockIdx.x - row * parts;
     const int first = p * part, end = min(a.vocab, first + part);
     const char *x = static_cast<const char *>(a.logits) + row * a.stride * (F32 ? 4 : 2);
     const float c = a.scale * kLog2e;
     Sums own{-INFINITY, 0.f, 0.f};
-    Candidates &mine = best[TOP ? wave : 0];
-    int count = 0, border_id = 0;      // a candidate comes before (border, border_id)
-    uint32_t border = 0;
+    Candidate *mine = best[TOP ? wave : 0];
+    int count = 0;
+    Candidate border = 0;      // what comes before it is a candidate
     bool begun = false;
-    for (int at = first + wave * kTile; at < end; at += kWaves * kTile) {
+    for (int at = first + wave * kTile; at < end; at += WAVES * kTile) {
         Piece<F32> v[kUnits];
         const int e0 = at + lane * N;
         if (at + kTile <= end) {
@@ -216,90 +230,86 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(LogprobArgs a, int p
         }
         if constexpr (TOP) {
             const uint32_t lane_top = e0 < end ? key_of<F32>(top) : 0;
-            bool take = __any(lane_top > border), ties = false;
+            const bool ties = !begun;
+            uint32_t reach = (uint32_t)(border >> 32);
             if (!begun) {
-                begun = take = ties = true;
                 // the largest number that at least n lanes reach, 0 if fewer have an element
                 for (int bit = 31; bit >= (F32 ? 0 : 16); --bit) {
-                    const uint32_t t = border | 1u << bit;
-                    if (__popcll(__ballot(lane_top >= t)) >= a.top) border = t;
+                    const uint32_t t = reach | 1u << bit;
+                    if (__popcll(__ballot(lane_top >= t)) >= a.top) reach = t;
                 }
-                border = __builtin_amdgcn_readfirstlane(border);
+                reach = __builtin_amdgcn_readfirstlane(reach);
+                border = reach ? (Candidate)reach << 32 | 0xffffffffu : 0;      // larger numbers alone
+                begun = true;
             }
-            if (take) {
+            if (__any(lane_top > reach)) {
+                // what is surely none is found by the numbers; at no border, or one of NaN, nothing is
+                const float low = reach && reach != key_of<F32>(NAN) ? value_of(reach, F32) : NAN;
+#pragma unroll
+                for (int i = 0; i < kUnits * N; ++i) {
+                    const float w = v[i / N].value(i % N);
+                    if (!__any(!(w < low))) continue;
+                    const int id = e0 + i / N * 64 * N + i % N;
+                    const Candidate own_c = id < end ? candidate(key_of<F32>(w), id) : 0;
+                    uint64_t who = __ballot(own_c > border);
+                    if (!who) continue;
+                    if (count + __popcll(who) > kBuffer) {
+                        count = keep_best(mine, count, a.top);
+                        border = mine[a.top - 1];
+                        border = (Candidate)__builtin_amdgcn_readfirstlane((uint32_t)(border >> 32)) << 32 |
+                                 (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)border);
+                        who = __ballot(own_c > border);
+                    }
+                    if (who >> lane & 1) mine[count + __popcll(who & ((1ull << lane) - 1))] = own_c;
+                    count += __popcll(who);
+                }
+            }
+            if (ties && count < a.top && reach) {
 #pragma unroll 1
-                for (int u = 0; u < kUnits; ++u) {
+                for (int u = 0; u < kUnits && count < a.top; ++u) {
                     Piece<F32> w = v[0];
 #pragma unroll
                     for (int i = 1; i < kUnits; ++i)
                         if (i == u) w = v[i];
+                    uint32_t same = 0;
 #pragma unroll
-                    for (int e = 0; e < N; ++e) {
-                        const int id = e0 + u * 64 * N + e;
-                        const uint32_t k = id < end ? key_of<F32>(w.value(e)) : 0;
-                        uint64_t who = __ballot(k != 0 && before(k, id, border, border_id));
-                        if (!who) continue;
-                        if (count + __popcll(who) > kBuffer) {
-                            count = keep_best(mine, count, a.top);
-                            border = __builtin_amdgcn_readfirstlane(mine.key[a.top - 1]);
-                            border_id = __builtin_amdgcn_readfirstlane(mine.id[a.top - 1]);
-                            ties = false;
-                            who = __ballot(k != 0 && before(k, id, border, border_id));
-                        }
-                        if (who >> lane & 1) {
-                            const int i = count + __popcll(who & ((1ull << lane) - 1));
-                            mine.key[i] = k;
-                            mine.id[i] = id;
-                        }
-                        count += __popcll(who);
+                    for (int e = 0; e < N; ++e)
+                        if (e0 + u * 64 * N + e < end && key_of<F32>(w.value(e)) == reach) same |= 1u << e;
+                    int to = __popc(same);      // of this lane and those before it
+#pragma unroll
+                    for (int s = 1; s < 64; s <<= 1) {
+                        const int o = __shfl_up(to, s);
+                        if (lane >= s) to += o;
                     }
-                }
-                if (ties && count < a.top && border != 0) {
-#pragma unroll 1
-                    for (int u = 0; u < kUnits && count < a.top; ++u) {
-                        Piece<F32> w = v[0];
-#pragma unroll
-                        for (int i = 1; i < kUnits; ++i)
-                            if (i == u) w = v[i];
-                        uint32_t same = 0;
-#pragma unroll
-                        for (int e = 0; e < N; ++e)
-                            if (e0 + u * 64 * N + e < end && key_of<F32>(w.value(e)) == border) same |= 1u << e;
-                        int to = __popc(same);      // of this lane and those before it
-#pragma unroll
-                        for (int s = 1; s < 64; s <<= 1) {
-                            const int o = __shfl_up(to, s);
-                            if (lane >= s) to += o;
-                        }
-                        const int all = __builtin_amdgcn_readlane(to, 63);
-                        for (int i = count + to - __popc(same); same && i < a.top; ++i, same &= same - 1) {
-                            mine.key[i] = border;
-                            mine.id[i] = e0 + u * 64 * N + __builtin_ctz(same);
-                        }
-                        count = min(count + all, a.top);
-                    }
+                    const int all = __builtin_amdgcn_readlane(to, 63);
+                    for (int i = count + to - __popc(same); same && i < a.top; ++i, same &= same - 1)
+                        mine[i] = candidate(reach, e0 + u * 64 * N + __builtin_ctz(same));
+                    count = min(count + all, a.top);
                 }
             }
         }
     }
     own = across_wave(own, c);
     if constexpr (TOP) count = keep_best(mine, count, a.top);
-    if (lane == 0) {
-        sums[wave] = own;
-        counts[wave] = count;
-    }
-    __syncthreads();
-    Sums all = sums[0];
-    float m = all.m;
+    Sums all = own;
+    if constexpr (WAVES > 1) {
+        if (lane == 0) {
+            sums[wave] = own;
+            counts[wave] = count;
+        }
+        __syncthreads();
+        all = sums[0];
+        float m = all.m;
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) m = top_of(m, sums[w].m);
-    all.rescale(m, c);
+        for (int w = 1; w < WAVES; ++w) m = top_of(m, sums[w].m);
+        all.rescale(m, c);
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) {
-        Sums o = sums[w];
-        o.rescale(m, c);
-        all.s += o.s;
-        all.t += o.t;
+        for (int w = 1; w < WAVES; ++w) {
+            Sums o = sums[w];
+            o.rescale(m, c);
+            all.s += o.s;
+            all.t += o.t;
+        }
     }
     const float log_s = log_sum(all);
     const Parts out = parts_in(a.workspace, (int64_t)a.rows * parts, a.top);
@@ -310,45 +320,49 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(LogprobArgs a, int p
     }
     if constexpr (TOP) {
         // a candidate's place: those before it in every wave's sorted list
-        const int w = threadIdx.x / kMaxTop, i = threadIdx.x % kMaxTop;
-        int total = 0;
-#pragma unroll
-        for (int o = 0; o < kWaves; ++o) total += counts[o];
-        if (w < kWaves && i < counts[w]) {
-            const uint32_t k = best[w].key[i];
-            const int id = best[w].id[i];
+        const int i = lane;
+        if (i < count) {
+            const Candidate own_c = mine[i];
             int place = i;
+            if constexpr (WAVES > 1) {
+                int before[WAVES] = {};
 #pragma unroll
-            for (int o = 0; o < kWaves; ++o)
-                if (o != w)
-                    for (int j = 0; j < counts[o] && before(best[o].key[j], best[o].id[j], k, id); ++j) ++place;
+                for (int step = kMaxTop; step >= 1; step >>= 1)
+#pragma unroll
+                    for (int o = 0; o < WAVES; ++o) {
+                        const int to = before[o] + step;
+                        if (to <= counts[o] && best[o][to - 1] > own_c) before[o] = to;
+                    }
+                place = 0;
+#pragma unroll
+                for (int o = 0; o < WAVES; ++o) place += before[o];      // of its own list: i
+            }
             if (place < a.top) {
-                if (parts == 1) {
-                    write_top(a, row, place, k, id, all.m, log_s);
-                } else {
-                    out.keys[slot * a.top + place] = k;
-                    out.ids[slot * a.top + place] = id;
-                }
+                if (parts == 1) write_top(a, row, place, own_c, all.m, log_s);
+                else out.best[slot * a.top + place] = own_c;
             }
         }
-        if (parts > 1 && threadIdx.x >= total && threadIdx.x < a.top) out.keys[slot * a.top + threadIdx.x] = 0;      // no further ones
+        if (parts > 1) {
+            int total = count;
+            if constexpr (WAVES > 1) {
+                total = 0;
+#pragma unroll
+                for (int o = 0; o < WAVES; ++o) total += counts[o];
+            }
+            if ((int)threadIdx.x >= total && (int)threadIdx.x < a.top) out.best[slot * a.top + threadIdx.x] = 0;      // no further ones
+        }
     }
 }
 
 // A row's parts together: a wave a row, a lane a part (at most 64).  Their sorted lists are merged from their heads.
 template <bool TOP>
 __global__ __launch_bounds__(64) void logprobs_join_kernel(LogprobArgs a, int parts) {
-    __shared__ uint32_t keys[TOP ? 64 * kMaxTop : 1];
-    __shared__ int ids[TOP ? 64 * kMaxTop : 1];
+    __shared__ Candidate lists[TOP ? 64 * kMaxTop : 1];
     const int row = blockIdx.x, lane = threadIdx.x;
     const Parts in = parts_in(a.workspace, (int64_t)a.rows * parts, a.top);
     const int64_t slot = (int64_t)row * parts;
-    if constexpr (TOP) {
-        for (int i = lane; i < parts * a.top; i += 64) {
-            keys[i] = in.keys[slot * a.top + i];
-            ids[i] = in.ids[slot * a.top + i];
-        }
-    }
+    if constexpr (TOP)
+        for (int i = lane; i < parts * a.top; i += 64) lists[i] = in.best[slot * a.top + i];
     Sums own{-INFINITY, 0.f, 0.f};
     if (lane < parts) own = in.sums[slot + lane];
     own = across_wave(own, a.scale * kLog2e);
@@ -356,28 +370,22 @@ __global__ __launch_bounds__(64) void logprobs_join_kernel(LogprobArgs a, int pa
     if (lane == 0) write_row(a, row, own, log_s);
     if constexpr (TOP) {
         __syncthreads();
-        int at = 0;
+        int next = lane * a.top;
+        const int last = lane < parts ? next + a.top : next;
+        Candidate head = next < last ? lists[next] : 0;
         for (int place = 0; place < a.top; ++place) {
-            uint32_t k = lane < parts && at < a.top ? keys[lane * a.top + at] : 0;
-            int id = k ? ids[lane * a.top + at] : 0x7fffffff;
-            const uint32_t k0 = k;
-            const int id0 = id;
-#pragma unroll
-            for (int s = 32; s >= 1; s >>= 1) {
-                const uint32_t ok = __shfl_xor(k, s);
-                const int oid = __shfl_xor(id, s);
-                if (before(ok, oid, k, id)) {
-                    k = ok;
-                    id = oid;
-                }
+            const uint32_t key = largest_of((uint32_t)(head >> 32));
+            const uint32_t low = largest_of((uint32_t)(head >> 32) == key ? (uint32_t)head : 0);
+            if (head == ((Candidate)key << 32 | low)) {      // one lane: indices differ
+                write_top(a, row, place, head, own.m, log_s);
+                ++next;
+                head = next < last ? lists[next] : 0;
             }
-            if (k0 && k0 == k && id0 == id) ++at;
-            if (lane == 0) write_top(a, row, place, k, id, own.m, log_s);
         }
     }
 }
 
-// The gradient: a workgroup takes kGradTile elements of a row.
+// The gradient: a workgroup takes 4 pieces a thread of a row.
 template <bool F32>
 __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(LogprobGradArgs a, int segments) {
     constexpr int N = Piece<F32>::N, kUnits = 4, kTile = kThreads * N * kUnits, ES = F32 ? 4 : 2;
@@ -435,16 +443,23 @@ int parts_of(int rows, int vocab) {
 
 size_t logprobs_workspace(int rows, int vocab, int top) {
     const int parts = parts_of(rows, vocab);
-    return parts == 1 ? 0 : (size_t)rows * parts * (sizeof(Sums) + (size_t)top * 8);
+    return parts == 1 ? 0 : (size_t)rows * parts * (sizeof(Sums) + (size_t)top * sizeof(Candidate));
 }
 
 hipError_t launch_logprobs(const LogprobArgs &a, hipStream_t stream) {
     const int parts = parts_of(a.rows, a.vocab);
     const int part = ((a.vocab + parts - 1) / parts + 7) / 8 * 8;
     const dim3 grid((unsigned)((int64_t)a.rows * parts));
-    auto launch = [&](auto kernel) { return launch_kernel(kernel, grid, dim3(kThreads), stream, a, parts, part); };
-    const hipError_t e = a.f32 ? (a.top ? launch(logprobs_kernel<true, true>) : launch(logprobs_kernel<true, false>))
-                               : (a.top ? launch(logprobs_kernel<false, true>) : launch(logprobs_kernel<false, false>));
+    // a wave a row where its tiles are two at most
+    const int waves = a.vocab <= 4096 ? 1 : 4;
+    auto launch = [&](auto kernel) { return launch_kernel(kernel, grid, dim3(64 * waves), stream, a, parts, part); };
+    hipError_t e;
+    if (waves == 1)
+        e = a.f32 ? (a.top ? launch(logprobs_kernel<true, true, 1>) : launch(logprobs_kernel<true, false, 1>))
+                  : (a.top ? launch(logprobs_kernel<false, true, 1>) : launch(logprobs_kernel<false, false, 1>));
+    else
+        e = a.f32 ? (a.top ? launch(logprobs_kernel<true, true, 4>) : launch(logprobs_kernel<true, false, 4>))
+                  : (a.top ? launch(logprobs_kernel<false, true, 4>) : launch(logprobs_kernel<false, false, 4>));
     if (e != hipSuccess || parts == 1) return e;
     return a.top ? launch_kernel(logprobs_join_kernel<true>, dim3(a.rows), dim3(64), stream, a, parts)
                  : launch_kernel(logprobs_join_kernel<false>, dim3(a.rows), dim3(64), stream, a, parts);

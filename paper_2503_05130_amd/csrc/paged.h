@@ -66,7 +66,7 @@ struct ScoreForm {
 
 // q bf16 rows of heads * head_dim elements q_stride apart (a multiple of 8);
 // ctx bf16 [batch, heads * head_dim]; partials: paged_workspace_floats floats.
-size_t paged_workspace_floats(int batch, int heads, int kv_heads, int head_dim, int max_keys);
+size_t paged_workspace_floats(const PagedCache &c, int batch, int heads, int max_keys);
 hipError_t launch_paged_attention(const PagedCache &c, const bf16_t *q, int64_t q_stride, const int32_t *table,
                                   int table_stride, int max_pages, const int32_t *lens, bf16_t *ctx, float *partials,
                                   int batch, int heads, float scale, ScoreForm form, hipStream_t stream);

@@ -890,9 +890,9 @@ hipError_t launch_paged_append(const PagedCache &c, const bf16_t *k, const bf16_
     return stream_out ? launch(paged_append_kernel<false, true>) : launch(paged_append_kernel<false, false>);
 }
 
-size_t paged_workspace_floats(int batch, int heads, int kv_heads, int head_dim, int max_keys) {
-    const size_t slots = paged_most_parts(max_keys, paged_split(batch, heads, kv_heads));
-    return slots == 1 ? 0 : (size_t)batch * heads * slots * (head_dim + 2);
+size_t paged_workspace_floats(const PagedCache &c, int batch, int heads, int max_keys) {
+    const size_t slots = paged_most_parts(max_keys, paged_split(batch, heads, c.kv_heads, c.kind == KvKind::Mx4));
+    return slots == 1 ? 0 : (size_t)batch * heads * slots * (c.head_dim + 2);
 }
 
 hipError_t launch_paged_attention(const PagedCache &c, const bf16_t *q, int64_t q_stride, const int32_t *table,
@@ -909,7 +909,7 @@ hipError_t launch_paged_attention(const PagedCache &c, const bf16_t *q, int64_t 
     a.batch = batch;
     a.heads = heads;
     a.max_keys = max_pages << c.page_log2;
-    a.split = paged_split(batch, heads, c.kv_heads);
+    a.split = paged_split(batch, heads, c.kv_heads, c.kind == KvKind::Mx4);
     a.slots = paged_most_parts(a.max_keys, a.split);
     a.scale_log2e = scale * kLog2e;
     a.cap_log2e = form.cap * kLog2e;

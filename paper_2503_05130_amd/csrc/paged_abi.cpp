@@ -57,7 +57,7 @@ void check_batch_heads(uint32_t batch, uint32_t n_heads, uint32_t n_kv_heads) {
 // The workspace's size, with the argument checks that it shares with the launch.
 size_t paged_workspace(const PagedCache &c, uint32_t batch, uint32_t n_heads, uint32_t max_pages) {
     check_batch_heads(batch, n_heads, (uint32_t)c.kv_heads);
-    return 4 * paged_workspace_floats((int)batch, (int)n_heads, c.kv_heads, c.head_dim, (int)(max_pages << c.page_log2));
+    return 4 * paged_workspace_floats(c, (int)batch, (int)n_heads, (int)(max_pages << c.page_log2));
 }
 
 // Both attention calls, within `guarded`.

@@ -31,14 +31,18 @@ constexpr int kPagedWholeLog2 = 9, kPagedMinLog2 = 8, kPagedMaxLog2 = 10;
 struct PagedSplit {
     int log2_parts;   // up to this many parts (log2)
     int waves;        // of a workgroup
+    int max_log2;     // of the keys in a part
 };
 
 inline __host__ __device__ int log2_up(int n) { return n <= 1 ? 0 : 32 - __builtin_clz((unsigned)(n - 1)); }
 
-inline __host__ __device__ PagedSplit paged_split(int batch, int n_heads, int n_kv_heads) {
+// A cache in 4 bits has a fourth of the bytes a key: its parts have up to 2048 keys, and a workgroup 2 waves from 2048 rows on (64 x
+// 4000 - 8192 keys, 32 / 8 heads of 128, in parts of 1024 / 2048 / 4096 keys 110 / 105 / 103 us, 96 x 5 - 12000 27 / 28 / 37, 256 x 800 - 1600 104 /
+// 88 / 89, and 79 with 2 waves).
+inline __host__ __device__ PagedSplit paged_split(int batch, int n_heads, int n_kv_heads, bool mx4 = false) {
     const long rows = (long)batch * n_kv_heads * paged_tiles(n_heads, n_kv_heads);
     const int spare = rows >= 256 ? 0 : 8 - log2_up((int)rows);
-    return {spare < 6 ? spare : 6, rows >= 4096 ? 2 : 8};
+    return {spare < 6 ? spare : 6, rows >= (mx4 ? 2048 : 4096) ? 2 : 8, kPagedMaxLog2 + mx4};
 }
 
 // log2 of the keys in each part of a request of n_keys >= 0; from 513 keys on it never falls as n_keys grows
@@ -46,7 +50,7 @@ inline __host__ __device__ int paged_part_log2(int n_keys, PagedSplit s) {
     if (n_keys <= 1 << kPagedWholeLog2) return kPagedWholeLog2;
     const int even = log2_up((n_keys + (1 << s.log2_parts) - 1) >> s.log2_parts);
     const int most = log2_up((n_keys + 127) >> 7);      // for 128 parts
-    const int part = even < kPagedMinLog2 ? kPagedMinLog2 : even > kPagedMaxLog2 ? kPagedMaxLog2 : even;
+    const int part = even < kPagedMinLog2 ? kPagedMinLog2 : even > s.max_log2 ? s.max_log2 : even;
     return part < most ? most : part;
 }
 

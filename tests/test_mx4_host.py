@@ -124,4 +124,4 @@ def test_workspace_of_a_4_bit_cache():
         n = ctypes.c_size_t()
         assert ie.lib().iefwd_paged_attention_workspace(ctypes.byref(_desc(kv_type=kind)), 3, 8, 200, ctypes.byref(n)) == ie.OK
         sizes.append(n.value)
-    assert sizes[0] == sizes[1] > 0
+    assert sizes[0] >= sizes[1] > 0
