@@ -20,6 +20,7 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f, kLeast = -3.0e38f;
 constexpr int kThreads = 256;
 constexpr int kBuffer = 128;      // candidates of a wave
+constexpr int kSlack = 16;       // more than n of them are cut to n after a tile
 
 // Rows may begin anywhere: 16-byte loads and stores of any alignment, which the memory of gfx950 takes.
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
@@ -110,18 +111,24 @@ __device__ inline Sums across_wave(Sums a, float c) {
     return a;
 }
 
-// What a row's sums and its given logit come to; one lane.
-__device__ inline void write_row(const LogprobArgs &a, int row, const Sums &s, float log_s) {
-    const bool empty = s.m == -INFINITY;      // every token masked
-    const int64_t token = a.tokens[row];
-    float lp = 0.f;
-    if (token >= 0 && token < a.vocab) {
-        const int64_t at = row * a.stride + token;
-        const float x = a.f32 ? static_cast<const float *>(a.logits)[at]
-                              : __uint_as_float((uint32_t) static_cast<const bf16_t *>(a.logits)[at] << 16);
-        lp = empty ? -INFINITY : (x - s.m) * a.scale - log_s;
+// The row's given token and its logit, asked for early: two loads in a row.
+struct Given {
+    float logit;
+    bool there;
+
+    __device__ Given(const LogprobArgs &a, int row) {
+        const int64_t token = a.tokens[row];
+        there = token >= 0 && token < a.vocab;
+        const int64_t at = row * a.stride + (there ? token : 0);
+        logit = a.f32 ? static_cast<const float *>(a.logits)[at]
+                      : __uint_as_float((uint32_t) static_cast<const bf16_t *>(a.logits)[at] << 16);
     }
-    a.logprobs[row] = lp;
+};
+
+// What a row's sums and its given logit come to; one lane.
+__device__ inline void write_row(const LogprobArgs &a, int row, const Given &given, const Sums &s, float log_s) {
+    const bool empty = s.m == -INFINITY;      // every token masked
+    a.logprobs[row] = !given.there ? 0.f : empty ? -INFINITY : (given.logit - s.m) * a.scale - log_s;
     if (a.entropy) a.entropy[row] = empty ? 0.f : top_of(log_s - a.scale * (s.t / s.s), 0.f);
     if (a.stats) {
         a.stats[2 * row] = s.m;
@@ -188,13 +195,13 @@ __device__ __host__ inline Parts parts_in(void *ws, int64_t row_parts, int top) 
 // adds to its own sums under its own maximum.
 //
 // The best n: of a wave's first tile, the largest number that n lanes' own maxima reach is at most its n-th largest
-// element; what exceeds it becomes a candidate, and equal ones up to n in the order of their indices.  From then on only
-// larger numbers do, which few are: one comparison a lane and tile finds that there are none.  A full buffer is sorted and cut to n, whose
-// last is the new border.
+// element; what reaches it becomes a candidate.  From then on only larger numbers do, which few are: one comparison a lane and tile
+// finds that there are none.  A full buffer is sorted and cut to n, whose last is the new border.
 template <bool F32, bool TOP, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void logprobs_kernel(LogprobArgs a, int parts, int part) {
     constexpr int N = Piece<F32>::N, kUnits = F32 ? 6 : 4, kTile = 64 * N * kUnits;
     __shared__ __attribute__((aligned(16))) Candidate best[TOP ? WAVES : 1][kBuffer];
+    __shared__ u32x4 stage[TOP ? WAVES : 1][TOP ? kUnits : 1][64];      // a wave's tile
     __shared__ int counts[WAVES];
     __shared__ Sums sums[WAVES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -202,11 +209,19 @@ __global__ __launch_bounds__(64 * WAVES) void logprobs_kernel(LogprobArgs a, int
     const int first = p * part, end = min(a.vocab, first + part);
     const char *x = static_cast<const char *>(a.logits) + row * a.stride * (F32 ? 4 : 2);
     const float c = a.scale * kLog2e;
+    const Given given(a, row);
     Sums own{-INFINITY, 0.f, 0.f};
     Candidate *mine = best[TOP ? wave : 0];
     int count = 0;
     Candidate border = 0;      // what comes before it is a candidate
+    uint32_t reach = 0;        // its key, or the first tile's
     bool begun = false;
+    auto cut = [&] {      // n or more candidates to the best n
+        count = keep_best(mine, count, a.top);
+        border = mine[a.top - 1];
+        reach = __builtin_amdgcn_readfirstlane((uint32_t)(border >> 32));
+        border = (Candidate)reach << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)border);
+    };
     for (int at = first + wave * kTile; at < end; at += WAVES * kTile) {
         Piece<F32> v[kUnits];
         const int e0 = at + lane * N;
@@ -230,8 +245,7 @@ __global__ __launch_bounds__(64 * WAVES) void logprobs_kernel(LogprobArgs a, int
         }
         if constexpr (TOP) {
             const uint32_t lane_top = e0 < end ? key_of<F32>(top) : 0;
-            const bool ties = !begun;
-            uint32_t reach = (uint32_t)(border >> 32);
+            bool take = __any(lane_top > reach);
             if (!begun) {
                 // the largest number that at least n lanes reach, 0 if fewer have an element
                 for (int bit = 31; bit >= (F32 ? 0 : 16); --bit) {
@@ -239,53 +253,40 @@ __global__ __launch_bounds__(64 * WAVES) void logprobs_kernel(LogprobArgs a, int
                     if (__popcll(__ballot(lane_top >= t)) >= a.top) reach = t;
                 }
                 reach = __builtin_amdgcn_readfirstlane(reach);
-                border = reach ? (Candidate)reach << 32 | 0xffffffffu : 0;      // larger numbers alone
-                begun = true;
+                border = reach ? ((Candidate)reach << 32) - 1 : 0;      // it and larger ones, whatever the index
+                begun = take = true;
             }
-            if (__any(lane_top > reach)) {
-                // what is surely none is found by the numbers; at no border, or one of NaN, nothing is
+            if (take) {
+                // which of the lane's elements may be: by the numbers; at no border, or one of NaN, all of them
                 const float low = reach && reach != key_of<F32>(NAN) ? value_of(reach, F32) : NAN;
+                uint32_t left = 0;
 #pragma unroll
-                for (int i = 0; i < kUnits * N; ++i) {
-                    const float w = v[i / N].value(i % N);
-                    if (!__any(!(w < low))) continue;
-                    const int id = e0 + i / N * 64 * N + i % N;
-                    const Candidate own_c = id < end ? candidate(key_of<F32>(w), id) : 0;
+                for (int i = kUnits * N - 1; i >= 0; --i) left = 2 * left + !(v[i / N].value(i % N) < low);
+#pragma unroll
+                for (int u = 0; u < kUnits; ++u) stage[wave][u][lane] = v[u].raw;
+                wave_lds_fence();
+                // a lane's next such element from LDS (in a loop: code that runs once costs more for being fetched)
+#pragma unroll 1
+                while (__any(left != 0)) {
+                    Candidate own_c = 0;
+                    if (left) {
+                        const int i = __builtin_ctz(left), id = e0 + i / N * 64 * N + i % N;
+                        left &= left - 1;
+                        const void *piece = &stage[wave][i / N][lane];
+                        const float w = F32 ? static_cast<const float *>(piece)[i % N]
+                                            : __uint_as_float((uint32_t) static_cast<const uint16_t *>(piece)[i % N] << 16);
+                        if (id < end) own_c = candidate(key_of<F32>(w), id);
+                    }
                     uint64_t who = __ballot(own_c > border);
-                    if (!who) continue;
                     if (count + __popcll(who) > kBuffer) {
-                        count = keep_best(mine, count, a.top);
-                        border = mine[a.top - 1];
-                        border = (Candidate)__builtin_amdgcn_readfirstlane((uint32_t)(border >> 32)) << 32 |
-                                 (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)border);
+                        cut();
                         who = __ballot(own_c > border);
                     }
                     if (who >> lane & 1) mine[count + __popcll(who & ((1ull << lane) - 1))] = own_c;
                     count += __popcll(who);
                 }
-            }
-            if (ties && count < a.top && reach) {
-#pragma unroll 1
-                for (int u = 0; u < kUnits && count < a.top; ++u) {
-                    Piece<F32> w = v[0];
-#pragma unroll
-                    for (int i = 1; i < kUnits; ++i)
-                        if (i == u) w = v[i];
-                    uint32_t same = 0;
-#pragma unroll
-                    for (int e = 0; e < N; ++e)
-                        if (e0 + u * 64 * N + e < end && key_of<F32>(w.value(e)) == reach) same |= 1u << e;
-                    int to = __popc(same);      // of this lane and those before it
-#pragma unroll
-                    for (int s = 1; s < 64; s <<= 1) {
-                        const int o = __shfl_up(to, s);
-                        if (lane >= s) to += o;
-                    }
-                    const int all = __builtin_amdgcn_readlane(to, 63);
-                    for (int i = count + to - __popc(same); same && i < a.top; ++i, same &= same - 1)
-                        mine[i] = candidate(reach, e0 + u * 64 * N + __builtin_ctz(same));
-                    count = min(count + all, a.top);
-                }
+                wave_lds_fence();
+                if (count >= a.top + kSlack) cut();
             }
         }
     }
@@ -315,7 +316,7 @@ __global__ __launch_bounds__(64 * WAVES) void logprobs_kernel(LogprobArgs a, int
     const Parts out = parts_in(a.workspace, (int64_t)a.rows * parts, a.top);
     const int64_t slot = (int64_t)row * parts + p;
     if (threadIdx.x == 0) {
-        if (parts == 1) write_row(a, row, all, log_s);
+        if (parts == 1) write_row(a, row, given, all, log_s);
         else out.sums[slot] = all;
     }
     if constexpr (TOP) {
@@ -359,6 +360,7 @@ template <bool TOP>
 __global__ __launch_bounds__(64) void logprobs_join_kernel(LogprobArgs a, int parts) {
     __shared__ Candidate lists[TOP ? 64 * kMaxTop : 1];
     const int row = blockIdx.x, lane = threadIdx.x;
+    const Given given(a, row);
     const Parts in = parts_in(a.workspace, (int64_t)a.rows * parts, a.top);
     const int64_t slot = (int64_t)row * parts;
     if constexpr (TOP)
@@ -367,21 +369,25 @@ __global__ __launch_bounds__(64) void logprobs_join_kernel(LogprobArgs a, int pa
     if (lane < parts) own = in.sums[slot + lane];
     own = across_wave(own, a.scale * kLog2e);
     const float log_s = log_sum(own);
-    if (lane == 0) write_row(a, row, own, log_s);
+    if (lane == 0) write_row(a, row, given, own, log_s);
     if constexpr (TOP) {
         __syncthreads();
         int next = lane * a.top;
         const int last = lane < parts ? next + a.top : next;
-        Candidate head = next < last ? lists[next] : 0;
+        Candidate head = next < last ? lists[next] : 0, second = next + 1 < last ? lists[next + 1] : 0, mine = 0;
+        next += 2;
         for (int place = 0; place < a.top; ++place) {
             const uint32_t key = largest_of((uint32_t)(head >> 32));
             const uint32_t low = largest_of((uint32_t)(head >> 32) == key ? (uint32_t)head : 0);
-            if (head == ((Candidate)key << 32 | low)) {      // one lane: indices differ
-                write_top(a, row, place, head, own.m, log_s);
+            const Candidate first = (Candidate)key << 32 | low;
+            if (lane == place) mine = first;
+            if (head == first) {      // one lane: indices differ
+                head = second;
+                second = next < last ? lists[next] : 0;
                 ++next;
-                head = next < last ? lists[next] : 0;
             }
         }
+        if (lane < a.top) write_top(a, row, lane, mine, own.m, log_s);
     }
 }
 
@@ -431,28 +437,33 @@ __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(LogprobGradArgs
     }
 }
 
-// Few rows are cut into parts that the whole chip works on, each of at least kLeastPart elements.
-constexpr int kLeastPart = 8192;
+// Few rows are cut into parts that the whole chip works on: up to 2048 workgroups, whole rounds of their waves' tiles each (F32: of
+// 6144 elements, bf16 of 8192, taken for both).
+struct Split {
+    int parts, part;
+};
 
-int parts_of(int rows, int vocab) {
-    const int most = std::min(64, (vocab + kLeastPart - 1) / kLeastPart);
-    return std::max(1, std::min(most, 1024 / std::max(rows, 1)));
+Split split_of(int rows, int vocab) {
+    constexpr int kRound = 8192;
+    const int rounds = (vocab + kRound - 1) / kRound, most = std::max(1, std::min({64, rounds, 2048 / std::max(rows, 1)}));
+    const int each = (rounds + most - 1) / most;
+    return {(rounds + each - 1) / each, each * kRound};
 }
 
 }  // namespace
 
 size_t logprobs_workspace(int rows, int vocab, int top) {
-    const int parts = parts_of(rows, vocab);
+    const int parts = split_of(rows, vocab).parts;
     return parts == 1 ? 0 : (size_t)rows * parts * (sizeof(Sums) + (size_t)top * sizeof(Candidate));
 }
 
 hipError_t launch_logprobs(const LogprobArgs &a, hipStream_t stream) {
-    const int parts = parts_of(a.rows, a.vocab);
-    const int part = ((a.vocab + parts - 1) / parts + 7) / 8 * 8;
+    const Split s = split_of(a.rows, a.vocab);
+    const int parts = s.parts;
     const dim3 grid((unsigned)((int64_t)a.rows * parts));
     // a wave a row where its tiles are two at most
     const int waves = a.vocab <= 4096 ? 1 : 4;
-    auto launch = [&](auto kernel) { return launch_kernel(kernel, grid, dim3(64 * waves), stream, a, parts, part); };
+    auto launch = [&](auto kernel) { return launch_kernel(kernel, grid, dim3(64 * waves), stream, a, s.parts, s.part); };
     hipError_t e;
     if (waves == 1)
         e = a.f32 ? (a.top ? launch(logprobs_kernel<true, true, 1>) : launch(logprobs_kernel<true, false, 1>))
