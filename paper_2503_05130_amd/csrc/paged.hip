@@ -4,27 +4,13 @@
 
 #include <algorithm>
 
-#include "mx4_device.h"
-#include "paged_split.h"
+#include "paged_device.h"
 
 namespace iefwd {
 namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
-
-// Inclusive scan over the wave's lanes: row shifts by 1, 2, 4, 8, then lane 15's row
-// result to the next row and lane 31's to the upper half.  0 is neutral to `add`.
-template <class T, class Add>
-__device__ inline T wave_scan(T v, Add add) {
-    v = add(v, (T)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, false));
-    v = add(v, (T)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, false));
-    v = add(v, (T)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, false));
-    v = add(v, (T)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, false));
-    v = add(v, (T)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false));
-    v = add(v, (T)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false));
-    return v;
-}
 
 // ------------------------------------------------------------------------------ plan
 //
@@ -228,8 +214,6 @@ __device__ inline float to_e4m3_range(float x, const E4m3Scale &s) {
     return __builtin_elementwise_minimum(__builtin_elementwise_maximum(y, -448.f), 448.f);
 }
 
-__device__ inline float bf16_of(uint32_t w, int half) { return __uint_as_float(half ? w & 0xffff0000u : w << 16); }
-
 // Two 32-bit words of bf16 pairs as 4 e4m3 values
 __device__ inline uint32_t narrow(uint32_t a, uint32_t b, const E4m3Scale &scale) {
     const int w = __builtin_amdgcn_cvt_pk_fp8_f32(to_e4m3_range(bf16_of(a, 0), scale), to_e4m3_range(bf16_of(a, 1), scale), 0,
@@ -368,76 +352,6 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(PagedCache c, co
 // 32 / 2 (one tile) 74; 64 / 1 145, 16 / 1 41.
 // Not kept: K of the next step requested before this step's V is used, and 2 or 4 steps at once (249 registers and 18% slower
 // in bf16, no faster in 8 bits).
-struct AttnArgs {
-    PagedCache c;
-    const bf16_t *q;
-    int64_t q_stride;
-    const int32_t *table;
-    const int32_t *lens;
-    bf16_t *ctx;
-    float *part_o;       // [batch, heads, slots, head_dim]
-    float *part_ml;      // [batch, heads, slots, 2]
-    int table_stride, batch, heads, max_keys, slots;
-    PagedSplit split;
-    float scale_log2e;
-    float cap_log2e, cap_inv;      // cap * log2(e) and its inverse; 0: no cap
-    const float *slopes;           // [heads] or null
-};
-
-// The lane, hidden from the compiler: what is computed from it inside the loop over
-// items stays there instead of being held in registers through it (153 -> 140 VGPRs).
-__device__ inline int opaque_lane() {
-    int lane = threadIdx.x & 63;
-    asm volatile("" : "+v"(lane));
-    return lane;
-}
-
-struct AttnItem {
-    int b, part, keys;
-};
-
-// The item-th (request, part) of the batch, requests in order; false past the last.
-// Every wave finds it by itself from the lengths, 64 requests at a time.  A request
-// without keys has one part, which writes its zeros.
-__device__ inline bool find_item(const AttnArgs &a, int item, int &b0, int &before, AttnItem &out) {
-    const int lane = opaque_lane();
-    for (; b0 < a.batch; b0 += 64) {
-        const bool in = b0 + lane < a.batch;
-        const int n = in ? min(max(a.lens[b0 + lane], 0), a.max_keys) : 0;
-        const int parts = in ? paged_parts(n, a.split) : 0;
-        const int to = before + wave_scan(parts, [](int x, int y) { return x + y; });
-        const int total = __builtin_amdgcn_readlane(to, 63);
-        if (item < total) {
-            const int src = __builtin_ctzll(__ballot(to > item));
-            out.b = __builtin_amdgcn_readfirstlane(b0 + src);
-            out.part = __builtin_amdgcn_readfirstlane(item - __builtin_amdgcn_readlane(to, src) +
-                                                      __builtin_amdgcn_readlane(parts, src));
-            out.keys = __builtin_amdgcn_readlane(n, src);
-            return true;
-        }
-        before = total;
-    }
-    return false;
-}
-
-// v of lanes l, l ^ 16, l ^ 32 and l ^ 48 together: each swap leaves a row's (half's) value
-// in one result and its neighbour's in the other.
-__device__ inline float across_rows_max(float v) {
-    const uint32_t x = __float_as_uint(v);
-    const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-    const uint32_t y = __float_as_uint(fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1])));
-    const auto b = __builtin_amdgcn_permlane32_swap(y, y, false, false);
-    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
-}
-
-__device__ inline float across_rows_sum(float v) {
-    const uint32_t x = __float_as_uint(v);
-    const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-    const uint32_t y = __float_as_uint(__uint_as_float(a[0]) + __uint_as_float(a[1]));
-    const auto b = __builtin_amdgcn_permlane32_swap(y, y, false, false);
-    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
-}
-
 // four e4m3 values as four bf16 (exact)
 __device__ inline u32x2 widen(uint32_t w) {
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -448,95 +362,13 @@ __device__ inline u32x2 widen(uint32_t w) {
 
 __device__ inline bf16x8 operand(u32x2 a, u32x2 b) { return __builtin_bit_cast(bf16x8, u32x4{a[0], a[1], b[0], b[1]}); }
 
-// A page of one head as a buffer: its base in scalar registers, so that a load needs one
-// 32-bit offset a lane.
-__device__ inline __amdgpu_buffer_rsrc_t page_buffer(const char *base, size_t at, uint32_t bytes) {
-    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)at), hi = __builtin_amdgcn_readfirstlane((uint32_t)(at >> 32));
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base + ((uint64_t)hi << 32 | lo)), 0, bytes, 0x00027000);
-}
-
-// A head's query for the product with 4-bit keys: q = hi + lo in e4m3 (4 bits of significance each), under scales per 32 columns
-// that bring the block's largest to 128 .. 256 and let lo have 2^-4 of hi's.  bf16 has 8 bits: hi and lo are exact down to 2^-13
-// of the block's largest and off by 2^-21 of it below.  Lane (r, c) holds columns 16 c to 16 c + 15 and 64 + 16 c
-// to 64 + 16 c + 15 of head r, and the scale of block c.  A block with an infinity or a NaN becomes NaN.
-struct Q8 {
-    i32x8 hi, lo;
-    int hi_scale, lo_scale;
-};
-
-template <int DH>
-__device__ inline Q8 q8_operand(const bf16_t *qh, int r, int c) {
-    Q8 q{};
-    int scale[2] = {127, 127};      // of the blocks that the lane's two pieces lie in
-#pragma unroll
-    for (int h = 0; h < DH / 64; ++h) {
-        const u32x4 w[2] = {*reinterpret_cast<const u32x4 *>(qh + 64 * h + 16 * c),
-                            *reinterpret_cast<const u32x4 *>(qh + 64 * h + 16 * c + 8)};
-        uint32_t top = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t x = w[i / 4][i % 4] & 0x7fff7fffu;
-            top = max(top, max(x & 0xffffu, x >> 16));
-        }
-        const auto both = __builtin_amdgcn_permlane16_swap(top, top, false, false);      // a block is two lanes' pieces, l and l ^ 16
-        const int field = (int)(max(both[0], both[1]) >> 7);
-        scale[h] = field == 255 ? 255 : max(field - 7, 4);
-        const float unit = __uint_as_float((uint32_t)(254 - min(scale[h], 250)) << 23);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float x[4], hi[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = bf16_of(w[i / 2][2 * (i % 2) + e / 2], e % 2) * unit;
-            int b = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
-            b = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], b, true);
-            const f32x2 back[2] = {__builtin_amdgcn_cvt_pk_f32_fp8(b, false), __builtin_amdgcn_cvt_pk_f32_fp8(b, true)};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) hi[e] = back[e / 2][e % 2];
-            int l = __builtin_amdgcn_cvt_pk_fp8_f32((x[0] - hi[0]) * 16.f, (x[1] - hi[1]) * 16.f, 0, false);
-            l = __builtin_amdgcn_cvt_pk_fp8_f32((x[2] - hi[2]) * 16.f, (x[3] - hi[3]) * 16.f, l, true);
-            q.hi[4 * h + i] = b;
-            q.lo[4 * h + i] = l;
-        }
-    }
-    // block c of 64 columns' two is that of the pieces of lanes 2 c and 2 c + 1
-    const int from = r + 32 * (c & 1);
-    const int first = __shfl(scale[0], from), second = __shfl(scale[1], from);
-    q.hi_scale = c < 2 ? first : second;
-    q.lo_scale = q.hi_scale == 255 ? 255 : q.hi_scale - 4;
-    return q;
-}
-
-// Columns 2 m and 2 m + 1 of the lane's W of token e of a quad, as bf16.  The conversion reads of its scale the exponent field alone, whatever
-// the other bits: a shift puts the token's byte there.
-template <int W>
-__device__ inline uint32_t v_pair(uint32_t codes, uint32_t scales, int e, int m, int r) {
-    const float s = __uint_as_float(e == 3 ? scales >> 1 : scales << (23 - 8 * e));
-    if (W == 4) codes >>= 16 * (r & 1);
-    const bf16x2 x = m == 0   ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 0)
-                     : m == 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 1)
-                     : m == 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 2)
-                              : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 3);
-    return __builtin_bit_cast(uint32_t, x);
-}
-
-// tanh to 2^-20 of its value: by its power series where it is small, whose 1 - 2 / (e^2x + 1) would lose that.
-__device__ inline float tanh_of(float x) {
-    const float y = x * x;
-    float series = fmaf(y, 62.f / 2835.f, -17.f / 315.f);
-    series = fmaf(y, series, 2.f / 15.f);
-    series = fmaf(y, series, -1.f / 3.f);
-    series = fmaf(x * y, series, x);
-    const float far = fmaf(-2.f, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * (2.f * kLog2e)) + 1.f), 1.f);
-    return fabsf(x) < 0.25f ? series : far;
-}
-
 // STREAM: pages are read with the non-temporal hint (see kStreamBytes).  SCORED: scores have a cap or a slope.
 template <int DH, KvKind KIND, int WAVES, bool STREAM, bool SCORED>
 __global__ __launch_bounds__(64 * WAVES, 2) void paged_attention_kernel(AttnArgs a) {
-    constexpr bool E4M3 = KIND == KvKind::E4m3, MX4 = KIND == KvKind::Mx4;
+    constexpr bool E4M3 = KIND == KvKind::E4m3;
     constexpr int ES = E4M3 ? 1 : 2;             // bytes per element
-    constexpr int NK = MX4 ? 1 : DH * ES / 64;   // 16-byte loads per lane and key tile: DH columns of 16 keys
-    constexpr int W = MX4 ? DH / 16 : E4M3 ? 4 : 2;      // columns of V that a lane takes of a 16-byte load
+    constexpr int NK = DH * ES / 64;             // 16-byte loads per lane and key tile: DH columns of 16 keys
+    constexpr int W = E4M3 ? 4 : 2;              // columns of V in a 16-byte load
     constexpr int NV = DH / (16 * W);            // such loads per key tile
     constexpr int ROW = DH + 4;
     __shared__ __attribute__((aligned(16))) float o_lds[WAVES][16][ROW];
@@ -550,17 +382,11 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attention_kernel(AttnArgs
     const int kvh = row / tiles, tile = row - kvh * tiles;
     const int head0 = kvh * group + tile * 16, n_heads = min(16, group - tile * 16);
     const int page = 1 << a.c.page_log2;
-    const uint32_t page_bytes = MX4 ? page * (DH / 32 * 17) : page * DH * ES;
-    const uint32_t codes = page * (DH / 2);      // MX4: where a page's scales begin
+    const uint32_t page_bytes = page * DH * ES;
     const char *K = static_cast<const char *>(a.c.k), *V = static_cast<const char *>(a.c.v);
     const float scale = E4M3 ? a.scale_log2e * a.c.k_scale[kvh] : a.scale_log2e;
     const float v_scale = E4M3 ? a.c.v_scale[kvh] : 1.f;
-    // MX4: lane (r, c) takes columns 32 c and on of key r, and of V the tokens 4 c to 4 c + 3 and columns W r and on, which for
-    // heads of 64 are half of a load; lanes past the last block of K read the first one's and drop it
-    const int k_block = MX4 && DH == 64 ? c & 1 : c;
-    const uint32_t k_lane = (k_block * page + r) * 16;
-    const uint32_t v_lane = MX4 ? (c * (DH / 8) + r * W / 8) * 16 : c * DH * 4 * ES + r * 16;
-    const uint32_t ks_lane = codes + k_block * page + r, vs_lane = codes + (c * (DH / 32) + r * W / 32) * 4;
+    const uint32_t k_lane = (c * page + r) * 16, v_lane = c * DH * 4 * ES + r * 16;
 
     int b0 = 0, before = 0;
     AttnItem it;
@@ -569,18 +395,13 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attention_kernel(AttnArgs
         const int k0 = it.part << part_log2, k1 = min(it.keys, k0 + (1 << part_log2));
         const int32_t *ids = a.table + (size_t)it.b * a.table_stride;
         // the queries as the first product's second operand: column r, rows as K's pieces have them
-        bf16x8 q[MX4 ? 1 : DH / 32];
-        Q8 q8;
+        bf16x8 q[DH / 32];
         {
             const bf16_t *qh = a.q + (int64_t)it.b * a.q_stride + (head0 + min(r, n_heads - 1)) * DH;
-            if constexpr (MX4) {
-                q8 = q8_operand<DH>(qh, r, c);
-            } else {
 #pragma unroll
-                for (int i = 0; i < DH / 32; ++i) {
-                    const int d = E4M3 ? 16 * (4 * (i / 2) + c) + 8 * (i % 2) : 8 * (4 * i + c);
-                    q[i] = *reinterpret_cast<const bf16x8 *>(qh + d);
-                }
+            for (int i = 0; i < DH / 32; ++i) {
+                const int d = E4M3 ? 16 * (4 * (i / 2) + c) + 8 * (i % 2) : 8 * (4 * i + c);
+                q[i] = *reinterpret_cast<const bf16x8 *>(qh + d);
             }
         }
         const float slope = SCORED && a.slopes ? a.slopes[head0 + min(r, n_heads - 1)] * kLog2e : 0.f;
@@ -598,7 +419,6 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attention_kernel(AttnArgs
             for (int i = 0; i < 32 && s0 + wave + WAVES * i < steps; ++i) {
                 const int key0 = k0 + (s0 + wave + WAVES * i) * 32;
                 u32x4 kr[2][NK], vr[2][NV];
-                uint32_t ks[2], vs[2];      // MX4: scales
                 int limit[2];     // keys of each tile that take part
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
@@ -611,30 +431,18 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attention_kernel(AttnArgs
                     for (int j = 0; j < NK; ++j)
                         kr[t][j] = __builtin_amdgcn_raw_buffer_load_b128(kp, k_lane, off * 16 + j * 64 * page,
                                                                          STREAM ? 2 : 0);
-                    if constexpr (MX4)
-                        ks[t] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(kp, ks_lane, off, STREAM ? 2 : 0);
 #pragma unroll
                     for (int j = 0; j < NV; ++j)
-                        vr[t][j] = __builtin_amdgcn_raw_buffer_load_b128(vp, v_lane, MX4 ? off * (DH / 2) : off * DH * ES + j * 256,
+                        vr[t][j] = __builtin_amdgcn_raw_buffer_load_b128(vp, v_lane, off * DH * ES + j * 256,
                                                                          STREAM ? 2 : 0);
-                    if constexpr (MX4)
-                        vs[t] = __builtin_amdgcn_raw_buffer_load_b32(vp, vs_lane, off * (DH / 32), STREAM ? 2 : 0);
                 }
                 float p[8];
                 float mx = m;
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
                     f32x4 s = {0.f, 0.f, 0.f, 0.f};
-                    if constexpr (MX4) {
-                        const bool there = DH == 128 || c < 2;
-                        const i32x8 x = {there ? (int)kr[t][0][0] : 0, there ? (int)kr[t][0][1] : 0, there ? (int)kr[t][0][2] : 0,
-                                         there ? (int)kr[t][0][3] : 0, 0, 0, 0, 0};
-                        const int x_scale = there ? (int)ks[t] : 127;
-                        s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, q8.lo, s, 4, 0, 0, x_scale, 0, q8.lo_scale);
-                        s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, q8.hi, s, 4, 0, 0, x_scale, 0, q8.hi_scale);
-                    }
 #pragma unroll
-                    for (int j = 0; j < (MX4 ? 0 : NK); ++j) {
+                    for (int j = 0; j < NK; ++j) {
                         if constexpr (E4M3) {
                             s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(widen(kr[t][j][0]), widen(kr[t][j][1])),
                                                                         q[2 * j], s, 0, 0, 0);
@@ -649,7 +457,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attention_kernel(AttnArgs
                     for (int e = 0; e < 4; ++e) {
                         float z = s[e] * scale;
                         if constexpr (SCORED) {
-                            if (a.cap_log2e != 0.f) z = a.cap_log2e * tanh_of(z * a.cap_inv);
+                            if (a.cap_log2e != 0.f) z = capped(a, z);
                             if (a.slopes) z = fmaf(-slope, (float)(it.keys - 1 - (key0 + 16 * t + 4 * c + e)), z);
                         }
                         p[4 * t + e] = 4 * c + e < limit[t] ? z : -INFINITY;
@@ -684,10 +492,6 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attention_kernel(AttnArgs
                 for (int t = 0; t < 2; ++t) {
                     if (limit[t] < 16) {
                         const int n = min(max(limit[t] - 4 * c, 0), 4);
-                        if constexpr (MX4) {      // any codes are finite under a finite scale
-                            vs[t] &= n == 4 ? 0xffffffffu : (1u << (8 * n)) - 1u;
-                            continue;
-                        }
 #pragma unroll
                         for (int j = 0; j < NV; ++j)
 #pragma unroll
@@ -697,30 +501,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attention_kernel(AttnArgs
                             }
                     }
                 }
-                if constexpr (MX4) {
-                    // a byte holds two columns of one token: the pairs of tokens that the operand wants come of two bytes
 #pragma unroll
-                    for (int m = 0; m < W / 2; ++m) {
-                        uint32_t lo_col[4], hi_col[4];
-#pragma unroll
-                        for (int t = 0; t < 2; ++t)
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                const uint32_t x = v_pair<W>(vr[t][0][2 * e], vs[t], 2 * e, m, r);
-                                const uint32_t y = v_pair<W>(vr[t][0][2 * e + 1], vs[t], 2 * e + 1, m, r);
-                                lo_col[2 * t + e] = __builtin_amdgcn_perm(y, x, 0x05040100u);
-                                hi_col[2 * t + e] = __builtin_amdgcn_perm(y, x, 0x07060302u);
-                            }
-                        const bf16x8 x0 = __builtin_bit_cast(bf16x8, u32x4{lo_col[0], lo_col[1], lo_col[2], lo_col[3]});
-                        const bf16x8 x1 = __builtin_bit_cast(bf16x8, u32x4{hi_col[0], hi_col[1], hi_col[2], hi_col[3]});
-                        o[0][2 * m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x0, p_hi, o[0][2 * m], 0, 0, 0);
-                        o[0][2 * m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x0, p_lo, o[0][2 * m], 0, 0, 0);
-                        o[0][2 * m + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x1, p_hi, o[0][2 * m + 1], 0, 0, 0);
-                        o[0][2 * m + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x1, p_lo, o[0][2 * m + 1], 0, 0, 0);
-                    }
-                }
-#pragma unroll
-                for (int j = 0; j < (MX4 ? 0 : NV); ++j)
+                for (int j = 0; j < NV; ++j)
 #pragma unroll
                     for (int w = 0; w < W; ++w) {
                         bf16x8 x;
@@ -846,24 +628,13 @@ hipError_t launch_attention_w(const AttnArgs &a, bool stream_pages, dim3 grid, h
                         : launch_kernel(paged_attention_kernel<DH, KIND, WAVES, false, SCORED>, grid, dim3(64 * WAVES), stream, a);
 }
 
-template <int DH, KvKind KIND, bool SCORED>
-hipError_t launch_attention(const AttnArgs &a, dim3 grid, hipStream_t stream) {
-    const int64_t pages = std::min((int64_t)a.c.n_pages, (int64_t)a.batch * (a.max_keys >> a.c.page_log2));
-    const bool stream_pages = pages * a.c.kv_heads * 2 * (int64_t)a.c.page_bytes() >= kStreamBytes;      // K and V
-    const hipError_t e = a.split.waves == 8 ? launch_attention_w<DH, KIND, 8, SCORED>(a, stream_pages, grid, stream)
-                                            : launch_attention_w<DH, KIND, 2, SCORED>(a, stream_pages, grid, stream);
-    if (e != hipSuccess || a.slots == 1) return e;     // no request can have a second part
-    return launch_kernel(paged_join_kernel<DH>, dim3(a.batch * a.heads), dim3(kThreads), stream, a);
-}
-
-template <int DH, bool SCORED>
-hipError_t launch_attention_kind(const AttnArgs &a, dim3 grid, hipStream_t stream) {
-    switch (a.c.kind) {
-    case KvKind::Bf16: return launch_attention<DH, KvKind::Bf16, SCORED>(a, grid, stream);
-    case KvKind::E4m3: return launch_attention<DH, KvKind::E4m3, SCORED>(a, grid, stream);
-    case KvKind::Mx4: return launch_attention<DH, KvKind::Mx4, SCORED>(a, grid, stream);
-    }
-    return hipErrorInvalidValue;
+template <int DH, KvKind KIND>
+hipError_t launch_attention(const AttnArgs &a, bool stream_pages, dim3 grid, hipStream_t stream) {
+    if (a.cap_log2e != 0.f || a.slopes)
+        return a.split.waves == 8 ? launch_attention_w<DH, KIND, 8, true>(a, stream_pages, grid, stream)
+                                  : launch_attention_w<DH, KIND, 2, true>(a, stream_pages, grid, stream);
+    return a.split.waves == 8 ? launch_attention_w<DH, KIND, 8, false>(a, stream_pages, grid, stream)
+                              : launch_attention_w<DH, KIND, 2, false>(a, stream_pages, grid, stream);
 }
 
 }  // namespace
@@ -923,10 +694,25 @@ hipError_t launch_paged_attention(const PagedCache &c, const bf16_t *q, int64_t 
     const int rows = c.kv_heads * paged_tiles(heads, c.kv_heads);
     const int64_t items = (int64_t)batch * a.slots;
     const dim3 grid((unsigned)(std::min<int64_t>(items, std::max(1, 2048 / rows)) * rows));
-    const bool scored = form.cap != 0.f || form.slopes;
-    if (c.head_dim == 64)
-        return scored ? launch_attention_kind<64, true>(a, grid, stream) : launch_attention_kind<64, false>(a, grid, stream);
-    return scored ? launch_attention_kind<128, true>(a, grid, stream) : launch_attention_kind<128, false>(a, grid, stream);
+    const int64_t pages = std::min((int64_t)c.n_pages, (int64_t)batch * max_pages);
+    const bool stream_pages = pages * c.kv_heads * 2 * (int64_t)c.page_bytes() >= kStreamBytes;      // K and V
+    const bool narrow = c.head_dim == 64;
+    hipError_t e;
+    switch (c.kind) {
+    case KvKind::Bf16:
+        e = narrow ? launch_attention<64, KvKind::Bf16>(a, stream_pages, grid, stream)
+                   : launch_attention<128, KvKind::Bf16>(a, stream_pages, grid, stream);
+        break;
+    case KvKind::E4m3:
+        e = narrow ? launch_attention<64, KvKind::E4m3>(a, stream_pages, grid, stream)
+                   : launch_attention<128, KvKind::E4m3>(a, stream_pages, grid, stream);
+        break;
+    default: e = launch_attention_mx4(a, stream_pages, grid, stream);
+    }
+    if (e != hipSuccess || a.slots == 1) return e;     // no request can have a second part
+    const dim3 join_grid(batch * heads);
+    return narrow ? launch_kernel(paged_join_kernel<64>, join_grid, dim3(kThreads), stream, a)
+                  : launch_kernel(paged_join_kernel<128>, join_grid, dim3(kThreads), stream, a);
 }
 
 }  // namespace iefwd

@@ -36,13 +36,17 @@ struct PagedSplit {
 
 inline __host__ __device__ int log2_up(int n) { return n <= 1 ? 0 : 32 - __builtin_clz((unsigned)(n - 1)); }
 
-// A cache in 4 bits has a fourth of the bytes a key: its parts have up to 2048 keys, and a workgroup 2 waves from 2048 rows on (64 x
-// 4000 - 8192 keys, 32 / 8 heads of 128, in parts of 1024 / 2048 / 4096 keys 110 / 105 / 103 us, 96 x 5 - 12000 27 / 28 / 37, 256 x 800 - 1600 104 /
-// 88 / 89, and 79 with 2 waves).
+// A cache in 4 bits has little more than a fourth of the bytes a key: its parts have up to 2048 keys, and its workgroups 8 waves up to 255
+// rows, 4 up to 2047 and 2 from there (us; 32 / 8 heads of 128 unless stated):
+//   parts of up to 512, 1024, 2048, 4096, 8192 keys: 64 x 4000 - 8192  102 92 92 95 88     256 x 800 - 1600  89 88 74 75 73
+//     96 x 5 - 12000, 16 / 4 heads of 64  23 22 25 33 45     16 x 600 - 1200, 12 heads of 64  12.2 12.6 10.6 10.6 10.6
+//   8 / 4 waves: 64 x 4000 - 8192  95 / 92     64 x 2000 - 4096, 16 / 16 heads  95 / 93     1 x 32001  14.9 / 15.8
+//     64 x 2000 - 8192, 16 / 1 heads  20 / 23     256 x 800 - 1600 with 8 / 2 waves  88 / 79
 inline __host__ __device__ PagedSplit paged_split(int batch, int n_heads, int n_kv_heads, bool mx4 = false) {
     const long rows = (long)batch * n_kv_heads * paged_tiles(n_heads, n_kv_heads);
     const int spare = rows >= 256 ? 0 : 8 - log2_up((int)rows);
-    return {spare < 6 ? spare : 6, rows >= (mx4 ? 2048 : 4096) ? 2 : 8, kPagedMaxLog2 + mx4};
+    const int waves = mx4 ? (rows >= 2048 ? 2 : rows >= 256 ? 4 : 8) : rows >= 4096 ? 2 : 8;
+    return {spare < 6 ? spare : 6, waves, kPagedMaxLog2 + mx4};
 }
 
 // log2 of the keys in each part of a request of n_keys >= 0; from 513 keys on it never falls as n_keys grows

@@ -74,7 +74,7 @@ def scored_attention(q, k, v, table, lens, scale, cap=0.0, slopes=None, q_exact=
     """q [B, H, d], k and v [pages, place, kv head, d], fp64; pages outside the pool drop their tokens.  Returns the context, per
     element a bound sum_j p_j |v_j| and per row a bound on a score's error in fp32: its sum of d terms and scaling (each
     rounding 2^-23, rounded or cut), for a cache in 4 bits what splitting q leaves out (2^-21 of the largest of 32 columns, q_exact False),
-    the tanh (2^-19 of its result) and the roundings of the scaled score, the slope's product and their sum."""
+    the tanh (2^-20 of the cap up to 64, beyond 2^-19 of its result) and the roundings of the scaled score, the slope's product and their sum."""
     batch, heads, d = q.shape
     pages, page, kv, _ = k.shape
     out, mag, err = np.zeros_like(q), np.zeros_like(q), np.zeros((batch, heads, 1))
@@ -95,7 +95,7 @@ def scored_attention(q, k, v, table, lens, scale, cap=0.0, slopes=None, q_exact=
                 e += 2.0 ** -21 * (np.abs(kk[:, g]).reshape(len(kk), -1, 32).sum(2) @ top * abs(scale)).max()
             if cap:
                 s = cap * np.tanh(s / cap)
-                e += 2.0 ** -19 * np.abs(s).max()
+                e += 2.0 ** -20 * cap if cap <= 64 else 2.0 ** -19 * np.abs(s).max()
             if slopes is not None:
                 bias = slopes[h] * (n - 1 - pos[keep])
                 s = s - bias
