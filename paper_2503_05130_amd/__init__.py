@@ -587,7 +587,7 @@ class PagedCache:
         """Writes new tokens' keys and values, bf16 [tokens, n_kv_heads, head_dim] (rows may lie apart), to
         their slots (int64 [tokens], from ``paged_plan``; outside the pool: skipped)."""
         dev = self._dev
-        n = len(slots)
+        n = _count(slots)
         if not _is(slots, torch.int64, dev, (n,)):
             _need("slots", slots, torch.int64, dev, (n,))
         ks = _rows("k", k, dev, n, self.n_kv_heads, self.head_dim)
@@ -598,7 +598,7 @@ class PagedCache:
         """k and v, bf16 [tokens, n_kv_heads, head_dim] (rows may lie apart) = what the cache holds at slots (int64 [tokens];
         outside the pool: zeros)."""
         dev = self._dev
-        n = len(slots)
+        n = _count(slots)
         if not _is(slots, torch.int64, dev, (n,)):
             _need("slots", slots, torch.int64, dev, (n,))
         ks = _rows("k", k, dev, n, self.n_kv_heads, self.head_dim)
@@ -729,15 +729,24 @@ class Q4Weight:
 _FLOATS = {torch.bfloat16: BF16, torch.float32: F32}
 
 
-def _float_rows(name: str, t, device: int, rows: int | None, cols: int) -> tuple[int, int, int]:
-    """Checks bf16 or fp32 [rows, cols] (any number of rows for None) whose rows are contiguous and may lie apart; returns its
-    type, the rows' stride in elements and the number of rows."""
-    if not isinstance(t, torch.Tensor) or t.dtype not in _FLOATS or t.get_device() != device or not t.is_cuda:
-        raise ValueError(f"{name} must be a bfloat16 or float32 tensor on cuda:{device}")
-    if t.dim() != 2 or t.shape[1] != cols or (rows is not None and t.shape[0] != rows) or (cols > 1 and t.stride(1) != 1):
-        raise ValueError(f"{name} must be [{'rows' if rows is None else rows}, {cols}] with each row contiguous")
-    n = t.shape[0]
-    return _FLOATS[t.dtype], (t.stride(0) if n > 1 else cols), n
+def _float_rows(name: str, t, device: int, cols: int) -> tuple[int, int, int]:
+    """Checks bf16 or fp32 [rows, cols] whose rows are contiguous and may lie apart; returns its type, the rows' stride in
+    elements and the number of rows."""
+    try:
+        kind, shape, stride = _FLOATS.get(t.dtype), t.shape, t.stride()
+        if kind is not None and t.get_device() == device and len(shape) == 2 and shape[1] == cols and (cols == 1 or stride[1] == 1):
+            return kind, (stride[0] if shape[0] > 1 else cols), shape[0]
+    except AttributeError:
+        pass
+    raise ValueError(f"{name} must be a bfloat16 or float32 tensor [rows, {cols}] on cuda:{device} with each row contiguous")
+
+
+def _count(t) -> int:
+    """len(t) of a tensor in a third of its time; 0 for what is none."""
+    try:
+        return t.shape[0]
+    except (AttributeError, IndexError):
+        return 0
 
 
 class Mx4Matrix:
@@ -757,7 +766,7 @@ class Mx4Matrix:
     def quantize(self, x, stream=None) -> None:
         """The first len(x) rows (and the rest of their 16 as zeros) = x, bf16 or fp32 [at most rows, K], whose rows may lie
         apart."""
-        kind, stride, n = _float_rows("x", x, self._dev, None, self.K)
+        kind, stride, n = _float_rows("x", x, self._dev, self.K)
         if n > self.rows:
             raise ValueError(f"x has {n} rows, the matrix {self.rows}")
         _call(self._dev, stream, "iefwd_mx4_quantize", kind, x.data_ptr(), stride, self._at, n, self.K)
@@ -773,7 +782,7 @@ class Mx4Matrix:
 
     def values(self, out, stream=None) -> None:
         """out, bf16 or fp32 [at most rows, K], whose rows may lie apart, = the values of the first rows."""
-        kind, stride, n = _float_rows("out", out, self._dev, None, self.K)
+        kind, stride, n = _float_rows("out", out, self._dev, self.K)
         if n > self.rows:
             raise ValueError(f"out has {n} rows, the matrix {self.rows}")
         _call(self._dev, stream, "iefwd_mx4_values", self._at, kind, out.data_ptr(), stride, n, self.K)
@@ -782,7 +791,7 @@ class Mx4Matrix:
         """out [M, N] = epilogue(a W^T + bias) with this matrix as W [N, K]: a another Mx4Matrix, of which the first M
         rows are taken, or bf16 [M, K], M <= 16 and K a multiple of 8, which is quantised on the way; out bf16, or fp32 (as resid)
         for EPI_BIAS_RESID_F32; bias bf16 [N] or None."""
-        dev, m, n, k = self._dev, len(out), self.rows, self.K
+        dev, m, n, k = self._dev, _count(out), self.rows, self.K
         f32 = epilogue == EPI_BIAS_RESID_F32
         kind = torch.float32 if f32 else torch.bfloat16
         if not (_is(out, kind, dev, (m, n)) and (bias is None or _is(bias, torch.bfloat16, dev, (n,))) and

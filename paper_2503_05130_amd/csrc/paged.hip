@@ -4,7 +4,7 @@
 
 #include <algorithm>
 
-#include "paged_device.h"
+#include "paged_mx4.h"
 
 namespace iefwd {
 namespace {

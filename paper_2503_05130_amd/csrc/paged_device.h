@@ -1,4 +1,4 @@
-// What the paged attention kernels (paged.hip, paged_mx4.hip) share on the device.
+// What the paged attention kernels (paged.hip, paged_mx4.h) share on the device.
 #pragma once
 
 #include "mx4_device.h"
@@ -23,9 +23,6 @@ struct AttnArgs {
     float cap_log2e, cap_inv;      // cap * log2(e) and its inverse; 0: no cap
     const float *slopes;           // [heads] or null
 };
-
-// The attention over a cache in 4 bits (csrc/paged_mx4.hip), up to the joining of parts.
-hipError_t launch_attention_mx4(const AttnArgs &a, bool stream_pages, dim3 grid, hipStream_t stream);
 
 namespace {
 

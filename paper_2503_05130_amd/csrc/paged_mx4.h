@@ -1,13 +1,13 @@
 // A paged cache in microscaled 4 bits for gfx950: new tokens, attention of one query per request, and tokens of
-// every kind of cache read back.
-#include <algorithm>
+// every kind of cache read back.  Part of paged.hip.
+#pragma once
 
 #include "paged_device.h"
 
 namespace iefwd {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kTileThreads = 256;
 
 // The place of 8 columns' codes (4 bytes) and of their block's scale in a head's part of a page.
 struct Mx4Place {
@@ -29,7 +29,7 @@ __device__ inline Mx4Place mx4_place(bool v, int page, int dh, int place, int ei
 // in the order of the pages' pieces 36); 48 tokens take 2.5 us either way, a launch and two loads in a row.
 template <int DH>
 struct Tile {
-    static constexpr int EIGHTHS = DH / 8, TOKENS = kThreads / EIGHTHS;
+    static constexpr int EIGHTHS = DH / 8, TOKENS = kTileThreads / EIGHTHS;
     int token, head, eighth;
 
     __device__ Tile(int kv_heads) {
@@ -41,7 +41,7 @@ struct Tile {
 };
 
 template <int DH>
-__global__ __launch_bounds__(kThreads) void paged_append_mx4_kernel(PagedCache c, const bf16_t *__restrict__ k,
+__global__ __launch_bounds__(kTileThreads) void paged_append_mx4_kernel(PagedCache c, const bf16_t *__restrict__ k,
                                                                     const bf16_t *__restrict__ v,
                                                                     const int64_t *__restrict__ slots, int tokens,
                                                                     int64_t k_stride, int64_t v_stride) {
@@ -107,7 +107,7 @@ __device__ inline u32x4 read_eight(const PagedCache &c, bool is_v, size_t part, 
 }
 
 template <int DH, KvKind KIND>
-__global__ __launch_bounds__(kThreads) void paged_read_kernel(PagedCache c, const int64_t *__restrict__ slots,
+__global__ __launch_bounds__(kTileThreads) void paged_read_kernel(PagedCache c, const int64_t *__restrict__ slots,
                                                               bf16_t *__restrict__ k, bf16_t *__restrict__ v, int tokens,
                                                               int64_t k_stride, int64_t v_stride) {
     const Tile<DH> at(c.kv_heads);
@@ -513,7 +513,7 @@ hipError_t launch_mx4_heads(const AttnArgs &a, bool stream_pages, dim3 grid, hip
 }
 
 dim3 grid_of(const PagedCache &c, int tokens) {
-    const int per_tile = kThreads / (c.head_dim / 8);
+    const int per_tile = kTileThreads / (c.head_dim / 8);
     return dim3((unsigned)((int64_t)((tokens + per_tile - 1) / per_tile) * c.kv_heads));
 }
 
@@ -521,13 +521,14 @@ template <KvKind KIND>
 hipError_t launch_read(const PagedCache &c, const int64_t *slots, bf16_t *k, bf16_t *v, int tokens, int64_t k_stride,
                        int64_t v_stride, hipStream_t stream) {
     auto launch = [&](auto kernel) {
-        return launch_kernel(kernel, grid_of(c, tokens), dim3(kThreads), stream, c, slots, k, v, tokens, k_stride, v_stride);
+        return launch_kernel(kernel, grid_of(c, tokens), dim3(kTileThreads), stream, c, slots, k, v, tokens, k_stride, v_stride);
     };
     return c.head_dim == 64 ? launch(paged_read_kernel<64, KIND>) : launch(paged_read_kernel<128, KIND>);
 }
 
 }  // namespace
 
+// Up to the joining of parts.
 hipError_t launch_attention_mx4(const AttnArgs &a, bool stream_pages, dim3 grid, hipStream_t stream) {
     const bool narrow = a.c.head_dim == 64;
     switch (a.split.waves) {
@@ -544,7 +545,7 @@ hipError_t launch_attention_mx4(const AttnArgs &a, bool stream_pages, dim3 grid,
 hipError_t launch_paged_append_mx4(const PagedCache &c, const bf16_t *k, const bf16_t *v, const int64_t *slots, int tokens,
                                    int64_t k_stride, int64_t v_stride, hipStream_t stream) {
     auto launch = [&](auto kernel) {
-        return launch_kernel(kernel, grid_of(c, tokens), dim3(kThreads), stream, c, k, v, slots, tokens, k_stride, v_stride);
+        return launch_kernel(kernel, grid_of(c, tokens), dim3(kTileThreads), stream, c, k, v, slots, tokens, k_stride, v_stride);
     };
     return c.head_dim == 64 ? launch(paged_append_mx4_kernel<64>) : launch(paged_append_mx4_kernel<128>);
 }
