@@ -112,3 +112,11 @@ def scored_tolerance(ref, mag, err, n):
     """Half a bf16 step of the result, and on sum p |v|: the probabilities' 16 bits, exp2 and the rescalings (2^-20), the
     score's error (each p and their sum change by it) and the fp32 sums over the keys."""
     return 2.0 ** -8 * np.abs(ref) + 2 * (2.0 ** -16 + 2.0 ** -20 + np.expm1(np.minimum(err, 1.0)) + (n + 64) * 2.0 ** -24) * mag
+
+
+def product_tolerance(a, w, y, k, f32):
+    """Exact terms, summed in fp32: 128 at a time (each addition off by at most 2^-23 of what it adds up, rounded or cut),
+    then the chunks and the waves, the bias; the result's own rounding."""
+    chunks = -(-k // 128)
+    e = 2.0 ** -23 * (128 + chunks + 12) * (np.abs(a) @ np.abs(w).T) + 2.0 ** -22 * np.abs(y)
+    return e if f32 else e + 2.0 ** -8 * np.abs(y)

@@ -115,14 +115,6 @@ def _weight(n, k, seed):
     return w, X.values(codes, scales)[:, :k]
 
 
-def _tolerance(a, w, y, k, f32):
-    """Exact terms, summed in fp32: 128 at a time (each addition off by at most 2^-23 of what it adds up, rounded or cut),
-    then the chunks and the waves, the bias; the result's own rounding."""
-    chunks = -(-k // 128)
-    e = 2.0 ** -23 * (128 + chunks + 12) * (np.abs(a) @ np.abs(w).T) + 2.0 ** -22 * np.abs(y)
-    return e if f32 else e + 2.0 ** -8 * np.abs(y)
-
-
 def _given(m, k, seed):
     x = _rows(m, k, BF, seed)
     codes, scales = X.quantize(f64(x))
@@ -139,7 +131,7 @@ def test_product(m, n, k):
     x, av = _given(m, k, m)
     bias = torch.randn(n, generator=torch.Generator().manual_seed(m)).to(BF)
     y = av @ wv.T + f64(bias)
-    tol = _tolerance(av, wv, y, k, False)
+    tol = X.product_tolerance(av, wv, y, k, False)
     a = ie.Mx4Matrix(m, k)
     a.quantize(to_dev(x))
     ways = [a] + ([to_dev(x)] if m <= 16 else [])
@@ -165,19 +157,19 @@ def test_epilogues(m, n, k):
         out = torch.empty((m, n), dtype=BF, device=DEV)
         w.product(way, out)
         sync()
-        assert (np.abs(f64(out) - plain) <= _tolerance(av, wv, plain, k, False)).all()
+        assert (np.abs(f64(out) - plain) <= X.product_tolerance(av, wv, plain, k, False)).all()
         y = plain + f64(bias)
         w.product(way, out, ie.EPI_BIAS_GELU_BF16, bias=to_dev(bias))
         sync()
         act = 0.5 * y * (1.0 + np.vectorize(math.erf)(y / math.sqrt(2.0)))
         # the GELU's slope is at most 1.13; its erf is good to 1.5e-7 and its exponential to 2^-20
-        tol = 1.13 * _tolerance(av, wv, y, k, True) + 2.0 ** -19 * np.abs(y) + 2.0 ** -8 * np.abs(act)
+        tol = 1.13 * X.product_tolerance(av, wv, y, k, True) + 2.0 ** -19 * np.abs(y) + 2.0 ** -8 * np.abs(act)
         assert (np.abs(f64(out) - act) <= tol).all()
         rd = to_dev(resid)
         w.product(way, rd, ie.EPI_BIAS_RESID_F32, bias=to_dev(bias), resid=rd)      # in place
         sync()
         z = y + f64(resid)
-        assert (np.abs(f64(rd) - z) <= _tolerance(av, wv, np.abs(y) + np.abs(z), k, True)).all()
+        assert (np.abs(f64(rd) - z) <= X.product_tolerance(av, wv, np.abs(y) + np.abs(z), k, True)).all()
 
 
 @pytest.mark.parametrize("m", [3, 16, 40, 200])
@@ -245,13 +237,13 @@ def test_captured_and_on_another_stream():
         sync()
         y = av @ wv.T
         assert _same(f64(back), av)
-        assert (np.abs(f64(out) - y) <= _tolerance(av, wv, y, k, False)).all()
+        assert (np.abs(f64(out) - y) <= X.product_tolerance(av, wv, y, k, False)).all()
     out.zero_()
     sync()
     a.quantize(xd, stream=side)
     w.product(a, out, stream=side)
     side.synchronize()
-    assert (np.abs(f64(out) - y) <= _tolerance(av, wv, y, k, False)).all()
+    assert (np.abs(f64(out) - y) <= X.product_tolerance(av, wv, y, k, False)).all()
 
 
 def test_refusals_of_the_binding():
