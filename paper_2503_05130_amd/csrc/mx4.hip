@@ -8,7 +8,7 @@
 namespace iefwd {
 namespace {
 
-constexpr int kWaves = 4;
+constexpr int kWaves = 4;      // of a workgroup at most
 
 // ------------------------------------------------------------------------------ to the form and back
 //
@@ -18,15 +18,15 @@ constexpr int kWaves = 4;
 // turned by c + 4 s, which spreads the 16 pieces of a row over the banks.
 __device__ inline int turned(int r, int c, int s) { return s * 1024 + (c * 16 + ((r + c + 4 * s) & 15)) * 16; }
 
-// VECTOR: rows begin at multiples of 16 bytes and have a multiple of 8 elements.
-template <bool F32, bool VECTOR>
+// VECTOR: rows begin at multiples of 16 bytes and have a multiple of 8 elements.  FAR: more than the caches hold (far_reads).
+template <bool F32, bool VECTOR, bool FAR>
 __device__ inline Eight load_eight(const void *row, int col, int K) {
     Eight x = {};
     if (VECTOR) {
         if (col < K) {
             const u32x4 *p = reinterpret_cast<const u32x4 *>(static_cast<const char *>(row) + (size_t)col * (F32 ? 4 : 2));
-            x.lo = p[0];
-            if (F32) x.hi = p[1];
+            x.lo = FAR ? __builtin_nontemporal_load(p) : p[0];
+            if (F32) x.hi = FAR ? __builtin_nontemporal_load(p + 1) : p[1];
         }
     } else {
 #pragma unroll
@@ -44,12 +44,12 @@ __device__ inline Eight load_eight(const void *row, int col, int K) {
     return x;
 }
 
-template <bool F32, bool VECTOR>
+template <bool F32, bool VECTOR, bool FAR>
 __global__ __launch_bounds__(64 * kWaves) void mx4_quantize_kernel(const char *__restrict__ x, int64_t row_bytes,
                                                                    char *__restrict__ dst, int rows, int K, int64_t items) {
     __shared__ __attribute__((aligned(16))) char lds[kWaves][4096 + 256];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t item = (int64_t)blockIdx.x * kWaves + wave;
+    const int64_t item = (int64_t)blockIdx.x * (blockDim.x >> 6) + wave;
     if (item >= items) return;
     const int chunks = mx4_chunks(K), groups = (chunks + 3) / 4;
     const int tile = (int)(item / groups), g = (int)(item - (int64_t)tile * groups);
@@ -63,7 +63,7 @@ __global__ __launch_bounds__(64 * kWaves) void mx4_quantize_kernel(const char *_
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
             v[i] = Eight{};
-            if (r0 + i < n) v[i] = load_eight<F32, VECTOR>(row0 + (r0 + i) * row_bytes, col, K);
+            if (r0 + i < n) v[i] = load_eight<F32, VECTOR, FAR>(row0 + (r0 + i) * row_bytes, col, K);
         }
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
@@ -85,12 +85,12 @@ __global__ __launch_bounds__(64 * kWaves) void mx4_quantize_kernel(const char *_
         *reinterpret_cast<const uint32_t *>(stage + 4096 + lane * 4);
 }
 
-template <bool F32, bool VECTOR>
+template <bool F32, bool VECTOR, bool FAR>
 __global__ __launch_bounds__(64 * kWaves) void mx4_values_kernel(const char *__restrict__ src, char *__restrict__ out,
                                                                  int64_t row_bytes, int rows, int K, int64_t items) {
     __shared__ __attribute__((aligned(16))) char lds[kWaves][4096 + 256];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t item = (int64_t)blockIdx.x * kWaves + wave;
+    const int64_t item = (int64_t)blockIdx.x * (blockDim.x >> 6) + wave;
     if (item >= items) return;
     const int chunks = mx4_chunks(K), groups = (chunks + 3) / 4;
     const int tile = (int)(item / groups), g = (int)(item - (int64_t)tile * groups);
@@ -132,7 +132,8 @@ __global__ __launch_bounds__(64 * kWaves) void mx4_values_kernel(const char *__r
             const u32x4 v = mx4_bf16(codes, scale);
             bf16_t *p = reinterpret_cast<bf16_t *>(row) + col;
             if (VECTOR) {
-                *reinterpret_cast<u32x4 *>(p) = v;
+                if (FAR) __builtin_nontemporal_store(v, reinterpret_cast<u32x4 *>(p));
+                else *reinterpret_cast<u32x4 *>(p) = v;
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
@@ -167,19 +168,34 @@ __global__ __launch_bounds__(256) void mx4_pack_kernel(const uint8_t *__restrict
     *reinterpret_cast<uint32_t *>(out + (size_t)chunks * 1024 + (size_t)g * 256 + lane * 4) = bytes;
 }
 
+// What a call reads once and what it writes for later goes past the last cache from here on.  Quantised and back, bf16, us, without a hint /
+// stores / loads / both:
+//   2000 x 8192  16.9  16.7  17.6  17.4      4000 x 8192  38.4  28.6  29.8  30.7
+//   6000 x 8192  51.3  44.8  43.6  43.1      8191 x 8192  68.5  61.6  58.1  55.6
+constexpr int64_t kFarReads = 96 << 20, kFarWrites = 32 << 20;
+
+int64_t items_of(int rows, int K) { return (int64_t)((rows + 15) / 16) * ((mx4_chunks(K) + 3) / 4); }
+
+// A wave a workgroup spreads few items over the chip: 100 x 2048 there and back 6.7 -> 6.3 us; many of them are better off in fours
+// (4000 x 8192 of fp32 63 -> 70), and 4 items as one workgroup (1 x 2048 5.1, else 5.4).
+int waves_of(int64_t items) { return items > 4 && items <= 2048 ? 1 : kWaves; }
+
 }  // namespace
 
 hipError_t launch_mx4_quantize(bool f32, const void *x, int64_t stride, void *dst, int rows, int K, hipStream_t stream) {
     const int es = f32 ? 4 : 2;
-    const int64_t items = (int64_t)((rows + 15) / 16) * ((mx4_chunks(K) + 3) / 4);
-    const dim3 grid((unsigned)((items + kWaves - 1) / kWaves)), block(64 * kWaves);
+    const int64_t items = items_of(rows, K);
+    const int waves = waves_of(items);
+    const dim3 grid((unsigned)((items + waves - 1) / waves)), block(64 * waves);
     const bool vector = K % 8 == 0 && stride * es % 16 == 0 && (uintptr_t)x % 16 == 0;
+    const bool far = (int64_t)rows * K * es > kFarReads;
     auto launch = [&](auto kernel) {
         return launch_kernel(kernel, grid, block, stream, static_cast<const char *>(x), stride * es, static_cast<char *>(dst),
                              rows, K, items);
     };
-    if (f32) return vector ? launch(mx4_quantize_kernel<true, true>) : launch(mx4_quantize_kernel<true, false>);
-    return vector ? launch(mx4_quantize_kernel<false, true>) : launch(mx4_quantize_kernel<false, false>);
+    if (!vector) return f32 ? launch(mx4_quantize_kernel<true, false, false>) : launch(mx4_quantize_kernel<false, false, false>);
+    if (f32) return far ? launch(mx4_quantize_kernel<true, true, true>) : launch(mx4_quantize_kernel<true, true, false>);
+    return far ? launch(mx4_quantize_kernel<false, true, true>) : launch(mx4_quantize_kernel<false, true, false>);
 }
 
 hipError_t launch_mx4_pack(const uint8_t *codes, const uint8_t *scales, void *dst, int rows, int K, hipStream_t stream) {
@@ -190,15 +206,19 @@ hipError_t launch_mx4_pack(const uint8_t *codes, const uint8_t *scales, void *ds
 
 hipError_t launch_mx4_values(const void *src, bool f32, void *out, int64_t stride, int rows, int K, hipStream_t stream) {
     const int es = f32 ? 4 : 2;
-    const int64_t items = (int64_t)((rows + 15) / 16) * ((mx4_chunks(K) + 3) / 4);
-    const dim3 grid((unsigned)((items + kWaves - 1) / kWaves)), block(64 * kWaves);
+    const int64_t items = items_of(rows, K);
+    const int waves = waves_of(items);
+    const dim3 grid((unsigned)((items + waves - 1) / waves)), block(64 * waves);
     const bool vector = K % 8 == 0 && stride * es % 16 == 0 && (uintptr_t)out % 16 == 0;
     auto launch = [&](auto kernel) {
         return launch_kernel(kernel, grid, block, stream, static_cast<const char *>(src), static_cast<char *>(out), stride * es,
                              rows, K, items);
     };
-    if (f32) return vector ? launch(mx4_values_kernel<true, true>) : launch(mx4_values_kernel<true, false>);
-    return vector ? launch(mx4_values_kernel<false, true>) : launch(mx4_values_kernel<false, false>);
+    // fp32: a lane's two stores leave halves of the lines, which the hint makes 91 us of 63 for 4000 x 8192
+    if (f32) return vector ? launch(mx4_values_kernel<true, true, false>) : launch(mx4_values_kernel<true, false, false>);
+    if (!vector) return launch(mx4_values_kernel<false, false, false>);
+    return (int64_t)rows * K * es >= kFarWrites ? launch(mx4_values_kernel<false, true, true>)
+                                                : launch(mx4_values_kernel<false, true, false>);
 }
 
 }  // namespace iefwd

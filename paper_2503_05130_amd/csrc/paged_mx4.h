@@ -40,7 +40,7 @@ struct Tile {
     }
 };
 
-template <int DH>
+template <int DH, bool FAR>
 __global__ __launch_bounds__(kTileThreads) void paged_append_mx4_kernel(PagedCache c, const bf16_t *__restrict__ k,
                                                                     const bf16_t *__restrict__ v,
                                                                     const int64_t *__restrict__ slots, int tokens,
@@ -51,8 +51,9 @@ __global__ __launch_bounds__(kTileThreads) void paged_append_mx4_kernel(PagedCac
     const int64_t slot = slots[at.token];
     const int col = at.head * DH + 8 * at.eighth;
     Eight x[2] = {};
-    x[0].lo = *reinterpret_cast<const u32x4 *>(k + at.token * k_stride + col);
-    x[1].lo = *reinterpret_cast<const u32x4 *>(v + at.token * v_stride + col);
+    const u32x4 *kp = reinterpret_cast<const u32x4 *>(k + at.token * k_stride + col), *vp = reinterpret_cast<const u32x4 *>(v + at.token * v_stride + col);
+    x[0].lo = FAR ? __builtin_nontemporal_load(kp) : *kp;
+    x[1].lo = FAR ? __builtin_nontemporal_load(vp) : *vp;
     if (slot < 0 || slot >= (int64_t)c.n_pages << c.page_log2) return;
     const size_t part = ((size_t)(slot >> c.page_log2) * c.kv_heads + at.head) * (page * (DH / 32 * 17));
 #pragma unroll
@@ -106,7 +107,7 @@ __device__ inline u32x4 read_eight(const PagedCache &c, bool is_v, size_t part, 
     }
 }
 
-template <int DH, KvKind KIND>
+template <int DH, KvKind KIND, bool FAR>
 __global__ __launch_bounds__(kTileThreads) void paged_read_kernel(PagedCache c, const int64_t *__restrict__ slots,
                                                               bf16_t *__restrict__ k, bf16_t *__restrict__ v, int tokens,
                                                               int64_t k_stride, int64_t v_stride) {
@@ -121,8 +122,14 @@ __global__ __launch_bounds__(kTileThreads) void paged_read_kernel(PagedCache c, 
         for (int i = 0; i < 2; ++i) x[i] = read_eight<DH, KIND>(c, i, part, page, (int)(slot & (page - 1)), at.eighth, at.head);
     }
     const int col = at.head * DH + 8 * at.eighth;
-    *reinterpret_cast<u32x4 *>(k + at.token * k_stride + col) = x[0];
-    *reinterpret_cast<u32x4 *>(v + at.token * v_stride + col) = x[1];
+    u32x4 *kp = reinterpret_cast<u32x4 *>(k + at.token * k_stride + col), *vp = reinterpret_cast<u32x4 *>(v + at.token * v_stride + col);
+    if (FAR) {
+        __builtin_nontemporal_store(x[0], kp);
+        __builtin_nontemporal_store(x[1], vp);
+    } else {
+        *kp = x[0];
+        *vp = x[1];
+    }
 }
 
 // ------------------------------------------------------------------------------ attention
@@ -517,13 +524,20 @@ dim3 grid_of(const PagedCache &c, int tokens) {
     return dim3((unsigned)((int64_t)((tokens + per_tile - 1) / per_tile) * c.kv_heads));
 }
 
+// Of the tokens' keys and values in bf16.  From 64 MiB on new ones are read, from 32 MiB on read ones written past the last cache: append and
+// read of tokens of 8 x 128, us, without a hint / stores / both:
+//   2000  7.7  7.4  7.0     4000 10.9  9.8  9.8     8000 18.7 16.8 17.9     16000 41.2 33.3 33.7     24001 and 26000 62.2 53.3 49.4
+int64_t bytes_of(const PagedCache &c, int tokens) { return (int64_t)tokens * c.kv_heads * c.head_dim * 4; }
+
 template <KvKind KIND>
 hipError_t launch_read(const PagedCache &c, const int64_t *slots, bf16_t *k, bf16_t *v, int tokens, int64_t k_stride,
                        int64_t v_stride, hipStream_t stream) {
     auto launch = [&](auto kernel) {
         return launch_kernel(kernel, grid_of(c, tokens), dim3(kTileThreads), stream, c, slots, k, v, tokens, k_stride, v_stride);
     };
-    return c.head_dim == 64 ? launch(paged_read_kernel<64, KIND>) : launch(paged_read_kernel<128, KIND>);
+    const bool far = bytes_of(c, tokens) >= 32 << 20;
+    if (c.head_dim == 64) return far ? launch(paged_read_kernel<64, KIND, true>) : launch(paged_read_kernel<64, KIND, false>);
+    return far ? launch(paged_read_kernel<128, KIND, true>) : launch(paged_read_kernel<128, KIND, false>);
 }
 
 }  // namespace
@@ -547,7 +561,9 @@ hipError_t launch_paged_append_mx4(const PagedCache &c, const bf16_t *k, const b
     auto launch = [&](auto kernel) {
         return launch_kernel(kernel, grid_of(c, tokens), dim3(kTileThreads), stream, c, k, v, slots, tokens, k_stride, v_stride);
     };
-    return c.head_dim == 64 ? launch(paged_append_mx4_kernel<64>) : launch(paged_append_mx4_kernel<128>);
+    const bool far = bytes_of(c, tokens) >= 64 << 20;
+    if (c.head_dim == 64) return far ? launch(paged_append_mx4_kernel<64, true>) : launch(paged_append_mx4_kernel<64, false>);
+    return far ? launch(paged_append_mx4_kernel<128, true>) : launch(paged_append_mx4_kernel<128, false>);
 }
 
 hipError_t launch_paged_read(const PagedCache &c, const int64_t *slots, bf16_t *k, bf16_t *v, int tokens, int64_t k_stride,

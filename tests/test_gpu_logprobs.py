@@ -314,3 +314,23 @@ def test_refusals_of_the_binding():
         assert e.value.status == ie.EINVAL
     sync()
     assert (lp == 3.0).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_a_large_gradient_is_that_of_its_rows(dtype):
+    """Logits and gradient of more than the last cache (last rows first, non-temporal writes) against the same rows a few at a
+    time, in their own place as well."""
+    rows, vocab = (1103, 65003) if dtype is BF else (1103, 32771)
+    g = torch.Generator(device=DEV).manual_seed(3)
+    x = torch.randn(rows, vocab, generator=g, device=DEV).to(dtype)
+    tokens = torch.randint(-1, vocab, (rows,), generator=g, device=DEV)
+    gl, gh = torch.randn(rows, generator=g, device=DEV), torch.randn(rows, generator=g, device=DEV)
+    got = _run(x, tokens.cpu(), 0, 0.9)
+    large, small = torch.empty_like(x), torch.empty_like(x)
+    ie.token_logprobs_grad(x, tokens, got["stats"], large, gl, got["entropy"], gh, 0.9)
+    for at in range(0, rows, 100):
+        some = slice(at, at + 100)
+        ie.token_logprobs_grad(x[some], tokens[some], got["stats"][some], small[some], gl[some], got["entropy"][some], gh[some], 0.9)
+    ie.token_logprobs_grad(x, tokens, got["stats"], x, gl, got["entropy"], gh, 0.9)
+    sync()
+    assert torch.equal(large, small) and torch.equal(x, small)

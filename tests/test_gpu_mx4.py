@@ -308,3 +308,30 @@ def test_few_rows_of_wide_and_long_matrices(m, n, k):
         w.product(way, out[:m])
         sync()
         assert (np.abs(f64(out[:m]) - y) <= tol).all() and (out[m:] == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_large_matrices_are_their_parts(dtype):
+    """More than the last cache keeps (non-temporal reads and writes) against the same rows a few at a time; short and
+    unaligned rows as well."""
+    rows, k = (6303, 8200) if dtype is BF else (3101, 8200)
+    g = torch.Generator(device=DEV).manual_seed(5)
+    wide = torch.randn((rows, k + 9), generator=g, device=DEV).to(dtype)
+    for first, cols in ((0, k), (1, k)):
+        x = wide[:, first:first + cols]
+        if first == 0:
+            x = x.contiguous()
+        a, part = ie.Mx4Matrix(rows, cols), ie.Mx4Matrix(800, cols)
+        a.quantize(x)
+        outs = [torch.empty(rows, cols, dtype=t, device=DEV) for t in (BF, F32)]
+        for out in outs:
+            a.values(out)
+        small = torch.empty(800, cols, dtype=BF, device=DEV)
+        for at in range(0, rows, 800):
+            n = min(800, rows - at)
+            part.quantize(x[at:at + n])
+            part.values(small[:n])
+            assert torch.equal(outs[0][at:at + n], small[:n]) and torch.equal(outs[1][at:at + n], small[:n].float())
+            if n == 800:
+                size = part.packed.numel()
+                assert torch.equal(a.packed[at // 800 * size:][:size], part.packed)

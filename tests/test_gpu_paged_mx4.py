@@ -325,3 +325,27 @@ def test_refusals_of_the_binding():
             c.read(**dict(dict(k=k, v=k, slots=slots), **b))
     sync()
     assert (out == 5.0).all()
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_many_tokens_are_their_parts(dim):
+    """More than the last cache keeps of (non-temporal reads and writes) against the same tokens in parts."""
+    kv, page, tokens = 2048 // dim, 32, 16501
+    pages = tokens // page + 2
+    g = torch.Generator(device=DEV).manual_seed(dim)
+    k, v = (torch.randn(tokens, kv, dim, generator=g, device=DEV).to(BF) for _ in range(2))
+    slots = torch.randperm(pages * page, generator=g, device=DEV)[:tokens]
+    caches = [ie.PagedCache.empty(pages, page, kv, dim, mx4=True) for _ in range(2)]
+    for c in caches:
+        c.k.fill_(7)
+        c.v.fill_(7)
+    caches[0].append(k, v, slots)
+    out = [torch.empty_like(k) for _ in range(4)]
+    caches[0].read(slots, *out[:2])
+    for at in range(0, tokens, 3001):
+        some = slice(at, at + 3001)
+        caches[1].append(k[some], v[some], slots[some])
+        caches[1].read(slots[some], out[2][some], out[3][some])
+    sync()
+    assert torch.equal(caches[0].k, caches[1].k) and torch.equal(caches[0].v, caches[1].v)
+    assert torch.equal(out[0], out[2]) and torch.equal(out[1], out[3])
