@@ -11,6 +11,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "mx4_device.h"
 
@@ -194,14 +195,19 @@ __device__ __host__ inline Parts parts_in(void *ws, int64_t row_parts, int top) 
 // A workgroup takes a part of a row, its waves tiles of it in turn: kUnits loads of 16 bytes a lane, whose elements a lane
 // adds to its own sums under its own maximum.
 //
-// The best n: of a wave's first tile, the largest number that n lanes' own maxima reach is at most its n-th largest
+// The best n: the largest number that n lanes' own maxima of the first tile reach is at most the n-th largest
 // element; what reaches it becomes a candidate.  From then on only larger numbers do, which few are: one comparison a lane and tile
 // finds that there are none.  A full buffer is sorted and cut to n, whose last is the new border.
-template <bool F32, bool TOP, int WAVES>
+// LISTS: 0 no such tokens; 1 each wave goes by its own lanes; 2 by all of the workgroup's, which leaves the waves a quarter of the
+// candidates for a barrier and three more ballots a bit: taken for n > 8.  us, 1 / 2:
+//   48 x 131072, n = 5 12.7 13.1     300 x 50001, 20 37.8 22.6     1000 x 128000, 32 117 79     500 x 128000 fp32, 20 78 65
+template <bool F32, int LISTS, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void logprobs_kernel(LogprobArgs a, int parts, int part) {
     constexpr int N = Piece<F32>::N, kUnits = F32 ? 6 : 4, kTile = 64 * N * kUnits;
+    constexpr bool TOP = LISTS > 0, SHARED = LISTS == 2 && WAVES > 1;
     __shared__ __attribute__((aligned(16))) Candidate best[TOP ? WAVES : 1][kBuffer];
     __shared__ u32x4 stage[TOP ? WAVES : 1][TOP ? kUnits : 1][64];      // a wave's tile
+    __shared__ uint32_t tops[SHARED ? 64 * WAVES : 1];
     __shared__ int counts[WAVES];
     __shared__ Sums sums[WAVES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -246,11 +252,22 @@ __global__ __launch_bounds__(64 * WAVES) void logprobs_kernel(LogprobArgs a, int
         if constexpr (TOP) {
             const uint32_t lane_top = e0 < end ? key_of<F32>(top) : 0;
             bool take = __any(lane_top > reach);
-            if (!begun) {
-                // the largest number that at least n lanes reach, 0 if fewer have an element
+            const bool first_tile = !begun;
+            if (first_tile) {
+                // the largest number that at least n lanes of the workgroup reach, 0 if fewer have an element
+                uint32_t of[SHARED ? WAVES : 1] = {lane_top};
+                if constexpr (SHARED) {
+                    tops[threadIdx.x] = lane_top;
+                    __syncthreads();
+#pragma unroll
+                    for (int w = 0; w < WAVES; ++w) of[w] = tops[64 * w + lane];
+                }
                 for (int bit = 31; bit >= (F32 ? 0 : 16); --bit) {
                     const uint32_t t = reach | 1u << bit;
-                    if (__popcll(__ballot(lane_top >= t)) >= a.top) reach = t;
+                    int lanes = 0;
+#pragma unroll
+                    for (int w = 0; w < (SHARED ? WAVES : 1); ++w) lanes += __popcll(__ballot(of[w] >= t));
+                    if (lanes >= a.top) reach = t;
                 }
                 reach = __builtin_amdgcn_readfirstlane(reach);
                 border = reach ? ((Candidate)reach << 32) - 1 : 0;      // it and larger ones, whatever the index
@@ -262,6 +279,14 @@ __global__ __launch_bounds__(64 * WAVES) void logprobs_kernel(LogprobArgs a, int
                 uint32_t left = 0;
 #pragma unroll
                 for (int i = kUnits * N - 1; i >= 0; --i) left = 2 * left + !(v[i / N].value(i % N) < low);
+                if (low == -INFINITY && first_tile) {
+                    // fewer than n lanes have another number: the first n of -inf are in the lanes' first pieces, whose indices are
+                    // the lowest
+                    uint32_t others = 0;
+#pragma unroll
+                    for (int i = kUnits * N - 1; i >= N; --i) others = 2 * others + (v[i / N].value(i % N) != low);
+                    left &= others << N | ((1u << N) - 1);
+                }
 #pragma unroll
                 for (int u = 0; u < kUnits; ++u) stage[wave][u][lane] = v[u].raw;
                 wave_lds_fence();
@@ -290,6 +315,11 @@ __global__ __launch_bounds__(64 * WAVES) void logprobs_kernel(LogprobArgs a, int
             }
         }
     }
+    if constexpr (SHARED)
+        if (!begun) {      // no tile: the others wait for this wave's part of theirs
+            tops[threadIdx.x] = 0;
+            __syncthreads();
+        }
     own = across_wave(own, c);
     if constexpr (TOP) count = keep_best(mine, count, a.top);
     Sums all = own;
@@ -475,13 +505,15 @@ hipError_t launch_logprobs(const LogprobArgs &a, hipStream_t stream) {
     // a wave a row where its tiles are two at most
     const int waves = a.vocab <= 4096 ? 1 : 4;
     auto launch = [&](auto kernel) { return launch_kernel(kernel, grid, dim3(64 * waves), stream, a, s.parts, s.part); };
-    hipError_t e;
-    if (waves == 1)
-        e = a.f32 ? (a.top ? launch(logprobs_kernel<true, true, 1>) : launch(logprobs_kernel<true, false, 1>))
-                  : (a.top ? launch(logprobs_kernel<false, true, 1>) : launch(logprobs_kernel<false, false, 1>));
-    else
-        e = a.f32 ? (a.top ? launch(logprobs_kernel<true, true, 4>) : launch(logprobs_kernel<true, false, 4>))
-                  : (a.top ? launch(logprobs_kernel<false, true, 4>) : launch(logprobs_kernel<false, false, 4>));
+    const int lists = a.top == 0 ? 0 : a.top <= 8 || waves == 1 ? 1 : 2;
+    auto choose = [&](auto f32) {
+        constexpr bool F32 = decltype(f32)::value;
+        if (waves == 1) return lists ? launch(logprobs_kernel<F32, 1, 1>) : launch(logprobs_kernel<F32, 0, 1>);
+        return lists == 2   ? launch(logprobs_kernel<F32, 2, 4>)
+               : lists == 1 ? launch(logprobs_kernel<F32, 1, 4>)
+                            : launch(logprobs_kernel<F32, 0, 4>);
+    };
+    const hipError_t e = a.f32 ? choose(std::true_type{}) : choose(std::false_type{});
     if (e != hipSuccess || parts == 1) return e;
     return a.top ? launch_kernel(logprobs_join_kernel<true>, dim3(a.rows), dim3(64), stream, a, parts)
                  : launch_kernel(logprobs_join_kernel<false>, dim3(a.rows), dim3(64), stream, a, parts);

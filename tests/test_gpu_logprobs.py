@@ -55,9 +55,10 @@ def _plain(x, tokens, scale):
     a wave and the parts by 2^-24 an addition; log S by that and a rounding."""
     x = x.double()
     m = x.amax(1, keepdim=True)
-    sd = (x - m) * scale
+    empty = m == -math.inf                                          # log probabilities of -inf, entropy 0
+    sd = (x - torch.where(empty, 0.0, m)) * scale
     p = torch.exp(sd)
-    total = p.sum(1, keepdim=True)
+    total = p.sum(1, keepdim=True) + empty
     p = p / total
     logp = sd - torch.log(total)
     size = torch.where(p > 0, p * sd.abs(), 0.0).sum(1)             # E |s d|
@@ -334,3 +335,36 @@ def test_a_large_gradient_is_that_of_its_rows(dtype):
     ie.token_logprobs_grad(x, tokens, got["stats"], x, gl, got["entropy"], gh, 0.9)
     sync()
     assert torch.equal(large, small) and torch.equal(x, small)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("vocab", [50, 300, 600, 5000, 9000, 40000, 140001])
+@pytest.mark.parametrize("n", [1, 5, 8, 9, 20, 32])
+def test_the_best_of_few_allowed_tokens(dtype, vocab, n):
+    """Rows with 0 to 70 tokens that are not masked, the first, the last, next to each other or anywhere: the rest of the n are the first masked
+    ones; waves and parts without a number, and without a tile."""
+    g = torch.Generator().manual_seed(vocab + n)
+    x = torch.full((12, vocab), -math.inf)
+    for r, held in enumerate([0, 1, 1, 3, n - 1, n, n, n + 1, 33, 70, 70, 40]):
+        held = min(held, vocab)
+        at = torch.randperm(vocab, generator=g)[:held]
+        at = {1: at * 0, 2: at * 0 + vocab - 1, 6: torch.arange(held), 10: vocab - 1 - torch.arange(held)}.get(r, at)
+        x[r, at] = torch.randn(len(at), generator=g).to(dtype).float()
+    x[11, ::7] = 1.5          # equal ones among them
+    _check(x.to(dtype), torch.randint(vocab, (12,), generator=g), n)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("vocab", [700, 9000, 70000])
+@pytest.mark.parametrize("n", [4, 20])
+def test_not_a_number_among_masked_tokens_comes_first(dtype, vocab, n):
+    x = torch.full((3, vocab), -math.inf)
+    g = torch.Generator().manual_seed(vocab)
+    bad = [torch.randperm(vocab, generator=g)[:k].sort().values for k in (1, 3, 30)]
+    for r, at in enumerate(bad):
+        x[r, at] = math.nan
+    got = _run(x.to(dtype).to(DEV), torch.zeros(3, dtype=torch.int64), n, 1.0)
+    masked = torch.arange(vocab)
+    for r, at in enumerate(bad):
+        want = torch.cat([at, masked[~torch.isin(masked, at)]])[:n]
+        assert torch.equal(got["top_ids"][r].cpu().long(), want), r
