@@ -721,7 +721,8 @@ int iefwd_paged_attention_scored(const iefwd_paged_cache *cache, const void *q, 
                                  size_t workspace_bytes, void *stream);
 
 /* Pure host function: the keys in each part that iefwd_paged_attention splits a
- * request of n_keys into, in a batch of this many requests.  n_keys <= 2^30, the
+ * request of n_keys into, in a batch of this many requests (16- and 8-bit caches;
+ * those in 4 bits have parts of at most 2048 keys).  n_keys <= 2^30, the
  * rest as there. */
 int iefwd_test_paged_split(uint32_t batch, uint32_t n_heads, uint32_t n_kv_heads, uint32_t n_keys, uint32_t *part_keys);
 
@@ -776,7 +777,8 @@ int iefwd_mx4_quantize(uint32_t type, const void *x, uint64_t x_stride, void *ds
  * uint8 [rows, K / 32], as checkpoints hold them; K a multiple of 32. */
 int iefwd_mx4_pack(const void *codes, const void *scales, void *dst, uint32_t rows, uint32_t K, void *stream);
 
-/* out [rows, K], rows out_stride >= K elements apart = the values that src stands for (exact in both types). */
+/* out [rows, K], rows out_stride >= K elements apart = the values that src stands for (exact in both types; infinite
+ * from 2^128 on, which only packed scales reach). */
 int iefwd_mx4_values(const void *src, uint32_t type, void *out, uint64_t out_stride, uint32_t rows, uint32_t K, void *stream);
 
 /* out [M, N] = epilogue(A W^T + b) of a [M, K] and w [N, K] in this form: epilogues IEFWD_EPI_BIAS_BF16, _BIAS_GELU_BF16 and

@@ -6,7 +6,9 @@
 //   log p_j = s d_j - log S,  entropy = -sum p_j log p_j = log S - s T / S
 // Both are differences of small numbers where the row is sure of a token: relative to m nothing large cancels.
 //   gradient of g_l log p_t + g_h entropy:  s (g_l (1[j = t] - p_j) - g_h p_j (log p_j + entropy))
-// Bound by reading the logits once (and writing the gradient).
+// Bound by reading the logits once (and writing the gradient): 4095 x 65003 bf16 in 98 us (5.4 TB/s; 8.9 vector
+// instructions an element, 81% of the issue slots) and its gradient in 194 (5.5 TB/s; 11.6 an element, 51%).  Few rows by latency and issue: 48 x
+// 131072 with 5 alternatives 9.0 us and 3.5 for joining the parts, of which the bytes are 2.1.
 #include "logprobs.h"
 
 #include <algorithm>

@@ -12,6 +12,11 @@ constexpr int kWaves = 4;      // of a workgroup at most
 
 // ------------------------------------------------------------------------------ to the form and back
 //
+// A block's scale byte is max(exponent field of its largest magnitude - 2, 0); v_cvt_scalef32_pk_fp4 divides by 2^(byte - 127),
+// rounds to the nearest (ties to even codes) and cuts off at 6, the inverse conversion is exact.  Bound by bytes: 8191 x 8192 bf16
+// become codes in 28.6 us (5.95 TB/s) and codes bf16 in 25.9 (6.6, the codes from the last cache); few rows by
+// latency: one of 2048 in 3.1 and 1.5 us.
+//
 // A wave takes a row tile's 4 chunks, 16 rows x 512 columns: a row's 512 columns are one load of 16 bytes a lane (two
 // in fp32), so that 4 lanes hold a block and neighbouring lanes neighbouring addresses.  The codes change places in 4
 // KB of LDS of the wave's own, and leave as whole 1 KB blocks.  Place p of block c and chunk s in the wave's LDS is

@@ -55,6 +55,10 @@ __device__ inline void mx4_store(const Mx4Params &p, int m, int n, f32x4 v) {
     }
 }
 
+// Few rows: bound by the weights' bytes and, below some 10 MB, by latency (launch, a chain of two loads, the joining of the waves).
+// 4 x 4096 -> 16384 takes 5.9 us of 4-bit rows (6.1 TB/s), 6.5 of bf16 ones; 1 x 2048 -> 8192 3.3 and 3.4 us; 32 x 8192 -> 8192
+// 6.8 (5.4 TB/s).
+//
 // A workgroup's tile of 16 FT features x 16 RT rows with K spread over its waves, chunk by chunk, and the waves' sums
 // added in wave order through LDS.  Operands go from memory to registers.  NL > 0: A is bf16, 4 NL >= M rows: a chunk of them is loaded in
 // rows, quantised by quads of lanes and laid out as the operand in the wave's LDS.
@@ -162,7 +166,11 @@ hipError_t launch_split(Mx4Params p, hipStream_t stream) {
                          dim3(64 * WAVES), stream, p);
 }
 
-// Many rows: a workgroup's tile of BM rows x BN features, through LDS.
+// Many rows: a workgroup's tile of BM rows x BN features, through LDS.  A lane's operand is 16 bytes for 16 x 16 x 128 x 2 / 64 operations, so that
+// a wave of 128 x 64 reads 12 KB of LDS for 32 products of 16 cycles each; registers alone (the kernel above) come to half the rate.
+// 8192^3 takes 245 us (4.5 PFLOP/s) at a clock that falls to 1.9 GHz: the matrix cores are busy for 62% of the whole and 67% of the
+// loop, the other 43 us are the first stages' loads and the output of 4 rounds of workgroups.  4096^3 37 us (3.7 PFLOP/s).  A ring of
+// four stages in place of two for 64 x 64 tiles gained nothing (201 x 4096 x 4096, 250 x 4096 x 4096, 150 x 2048 x 8192).
 //
 // The operands' 1 KB blocks are copied from global memory straight into a ring of S stages of CH chunks of K, each block by one
 // instruction, in the lane order in which the fragments are read (contiguous in both, no bank conflicts); a group of 4 chunks' scales

@@ -25,8 +25,8 @@ __device__ inline Mx4Place mx4_place(bool v, int page, int dh, int place, int ei
 // A workgroup takes a tile of following tokens of one head, a thread 8 columns of K and of V of one of them, a quad of lanes a block of
 // 32: neighbouring lanes have neighbouring addresses on the bf16 side, which is the most of the bytes.
 //
-// Bound by its bytes for prompts: 24001 tokens of 8 x 128 are written in 26 us (4.75 TB/s) and 26000 read back in 33 us (4.0; lanes
-// in the order of the pages' pieces 36); 48 tokens take 2.5 us either way, a launch and two loads in a row.
+// Bound by its bytes for prompts: 24001 tokens of 8 x 128 are written in 26.5 us (4.7 TB/s) and 26000 read back in 21.6 (6.2; with lanes
+// in the order of the pages' pieces a tenth more); 48 tokens take 2.6 us either way, a launch and two loads in a row.
 template <int DH>
 struct Tile {
     static constexpr int EIGHTHS = DH / 8, TOKENS = kTileThreads / EIGHTHS;
@@ -142,6 +142,11 @@ __global__ __launch_bounds__(kTileThreads) void paged_read_kernel(PagedCache c, 
 // keys; of 16 / HC tiles each lane keeps one by its c, and no score is worked on twice: with 4 heads a lane has 4 of the 64 x 4
 // scores of a step.  The probabilities go through 1 KB of LDS to the lanes that need them as an operand of O^T = V^T P^T, as bf16 and its
 // bf16 rest (see paged.hip).  V becomes bf16 on the way, by v_cvt_scalef32_pk_bf16_fp4 under the scale as it is stored.
+//
+// Bound by the pages' bytes, and next by the vector instructions that turn V into bf16 and the scores into probabilities: 64 requests of 4000 to 8192
+// keys, 32 / 8 heads of 128, 408 MB, take 91 us with capped scores (4.5 TB/s, 51% of the issue slots) and 4.3 for the joining (the call 98 - 106, 93 - 95 without a cap); one of 300 keys 6.6,
+// a chain of loads (length, table, page) and the joining of 8 waves.  Not kept: every lane working on all scores of its heads (103 and 115 us);
+// steps of 32 keys; the next step's loads asked for ahead, whose registers spill or halve the waves.
 //
 // The reference of the exponents need not be the largest score: it is raised, and sums and context scaled down, when a score
 // exceeds it by 2^8, which in a row of many keys is rare; probabilities up to 2^8 are as exact as those up to 1.
