@@ -755,6 +755,8 @@ class Mx4Matrix:
     wait for another stream nor keep the tensors given alive."""
 
     def __init__(self, rows: int, K: int, device="cuda:0"):
+        if rows >> 32 or K >> 32:      # ctypes would cut them to 32 bits
+            raise ValueError("a matrix has 1 to 2^24 rows and 1 to 2^20 columns")
         n = _sz()
         _check(lib().iefwd_mx4_bytes(rows, K, ctypes.byref(n)), "iefwd_mx4_bytes")
         self.rows, self.K = rows, K
@@ -805,8 +807,9 @@ class Mx4Matrix:
                 raise ValueError(f"a must have at least {m} rows, {k} columns and be on cuda:{dev}")
             name, at = "iefwd_mx4_gemm", a._at
         else:
-            if not _is(a, torch.bfloat16, dev, (m, k)):
+            if m >> 32 or not _is(a, torch.bfloat16, dev, (m, k)):
                 _need("a", a, torch.bfloat16, dev, (m, k))
+                raise ValueError("a in bf16 has at most 16 rows")
             name, at = "iefwd_mx4_gemm_bf16", a.data_ptr()
         _call(dev, stream, name, epilogue, at, self._at, None if bias is None else bias.data_ptr(),
               resid.data_ptr() if f32 else None, out.data_ptr(), m, n, k)
@@ -816,6 +819,8 @@ class Mx4Matrix:
 def token_logprobs_workspace(rows: int, vocab: int, n_top: int = 0, device="cuda:0") -> torch.Tensor:
     """A workspace for ``token_logprobs``, in memory of torch's current stream: calls on another one have to be ordered
     behind it, and the workspace to live until they have run."""
+    if rows >> 32 or vocab >> 32 or n_top >> 32:
+        raise ValueError("sizes must be below 2^32")
     n = _sz()
     _check(lib().iefwd_token_logprobs_workspace(rows, vocab, n_top, ctypes.byref(n)), "iefwd_token_logprobs_workspace")
     return torch.empty(n.value, dtype=torch.uint8, device=device)
@@ -828,6 +833,8 @@ def _logits(name: str, t) -> tuple[int, int, int, int, int]:
     if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
         raise ValueError(f"{name} must be [rows, vocab] with each row contiguous")
     rows, vocab = t.shape
+    if rows >> 32 or vocab >> 32:      # ctypes would cut them to 32 bits
+        raise ValueError(f"{name} must have at most 2^22 rows and 2^24 columns")
     return t.get_device(), _FLOATS[t.dtype], rows, vocab, t.stride(0) if rows > 1 else vocab
 
 
@@ -839,7 +846,9 @@ def token_logprobs(logits, tokens, logprobs, workspace, entropy=None, stats=None
     `stream`, by default torch's current stream of the logits' GPU."""
     dev, kind, rows, vocab, stride = _logits("logits", logits)
     f32 = torch.float32
-    n = 0 if top_ids is None else top_ids.shape[-1]
+    n = top_ids.shape[-1] if isinstance(top_ids, torch.Tensor) and top_ids.dim() else 0
+    if n >> 32:
+        raise ValueError("at most 32 most probable tokens")
     if not (_is(tokens, torch.int64, dev, (rows,)) and _is(logprobs, f32, dev, (rows,)) and
             (entropy is None or _is(entropy, f32, dev, (rows,))) and (stats is None or _is(stats, f32, dev, (rows, 2))) and
             (top_ids is None or _is(top_ids, torch.int32, dev, (rows, n))) and

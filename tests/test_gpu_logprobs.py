@@ -368,3 +368,21 @@ def test_not_a_number_among_masked_tokens_comes_first(dtype, vocab, n):
     for r, at in enumerate(bad):
         want = torch.cat([at, masked[~torch.isin(masked, at)]])[:n]
         assert torch.equal(got["top_ids"][r].cpu().long(), want), r
+
+
+def test_rows_more_than_32_bits_apart():
+    vocab, stride = 9001, (1 << 31) + 3
+    x, tokens = _logits(2, vocab, BF, 3)
+    far = torch.empty(stride + vocab, dtype=BF, device=DEV).as_strided((2, vocab), (stride, 1))
+    far.copy_(x)
+    near, td = x.to(DEV), tokens.to(DEV)
+    grads = []
+    for given in (far, near):
+        got = _run(given, tokens, 5, 1.0)
+        out = given if given is far else torch.empty_like(near)
+        ones = torch.ones(2, device=DEV)
+        ie.token_logprobs_grad(given, td, got["stats"], out, ones, got["entropy"], ones)
+        sync()
+        grads.append((out.clone().contiguous(), got))
+    assert torch.equal(grads[0][0], grads[1][0])
+    assert all(torch.equal(grads[0][1][k], grads[1][1][k]) for k in grads[0][1])

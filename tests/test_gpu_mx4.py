@@ -335,3 +335,52 @@ def test_large_matrices_are_their_parts(dtype):
             if n == 800:
                 size = part.packed.numel()
                 assert torch.equal(a.packed[at // 800 * size:][:size], part.packed)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_rows_more_than_32_bits_apart(dtype):
+    k, stride = 1000, (1 << 31) + 8
+    x = torch.empty(2 * stride if dtype is BF else stride + k, dtype=dtype, device=DEV)
+    x = x.as_strided((3, k) if dtype is BF else (2, k), (stride - 500 if dtype is BF else stride, 1))
+    rows = torch.randn(x.shape, generator=torch.Generator().manual_seed(1)).to(dtype)
+    x.copy_(rows)
+    a = ie.Mx4Matrix(len(x), k)
+    a.quantize(x)
+    x.zero_()
+    a.values(x)
+    sync()
+    codes, scales = X.quantize(f64(rows))
+    assert _same(f64(x.cpu()), X.values(codes, scales)[:, :k])
+
+
+@pytest.mark.parametrize("m", [3, 16, 24, 70, 300])
+def test_a_weight_of_more_than_32_bits(m):
+    """4.5 GB of a repeated tile with another one at the end."""
+    n, k = (1 << 20) - 5, 8192
+    w, tile, last = ie.Mx4Matrix(n, k), ie.Mx4Matrix(16, k), ie.Mx4Matrix(11, k)
+    g = torch.Generator(device=DEV).manual_seed(2)
+    tile.quantize(torch.randn(16, k, generator=g, device=DEV))
+    last.quantize(torch.randn(11, k, generator=g, device=DEV))
+    size = tile.packed.numel()
+    w.packed.view(-1, size)[:] = tile.packed
+    w.packed[-size:] = last.packed
+    x = torch.randn(m, k, generator=g, device=DEV).to(BF)
+    a = ie.Mx4Matrix(m, k)
+    a.quantize(x)
+    out = torch.empty(m, n, dtype=BF, device=DEV)
+    few = [torch.empty(m, 16, dtype=BF, device=DEV), torch.empty(m, 11, dtype=BF, device=DEV)]
+    for way in [a] + [x] * (m <= 16):
+        out.zero_()
+        w.product(way, out)
+        tile.product(way, few[0])
+        last.product(way, few[1])
+        sync()
+        # another split of K may round otherwise: half a step of the result and the sums' order
+        for got, want, terms in ((out[:, :16], few[0], tile), (out[:, -27:-11], few[0], tile), (out[:, -11:], few[1], last)):
+            wv, av = (torch.empty(t.rows, k, device=DEV) for t in (terms, a))
+            terms.values(wv)
+            a.values(av)
+            sync()
+            y = f64(av) @ f64(wv).T
+            assert (np.abs(f64(got) - y) <= X.product_tolerance(f64(av), f64(wv), y, k, False)).all()
+            assert (np.abs(f64(want) - y) <= X.product_tolerance(f64(av), f64(wv), y, k, False)).all()

@@ -63,3 +63,9 @@ def test_workspace():
     assert one[0] == more[0] == ie.OK and 0 < one[1] < more[1]
     assert ie.lib().iefwd_token_logprobs_workspace(1, 1, 0, None) == ie.EINVAL
     assert _space(5, 10, 11)[0] == ie.EINVAL and _space(5, 100, 33)[0] == ie.EINVAL
+
+
+@pytest.mark.parametrize("rows,vocab,n", [((1 << 32) + 1, 100, 0), (1, (1 << 32) + 100, 0), (1, 100, (1 << 32) + 1), (-1, 100, 0)])
+def test_sizes_beyond_32_bits_are_refused_by_the_binding(rows, vocab, n):
+    with pytest.raises(ValueError, match="2.32"):
+        ie.token_logprobs_workspace(rows, vocab, n)

@@ -125,3 +125,9 @@ def test_workspace_of_a_4_bit_cache():
         assert ie.lib().iefwd_paged_attention_workspace(ctypes.byref(_desc(kv_type=kind)), 3, 8, 200, ctypes.byref(n)) == ie.OK
         sizes.append(n.value)
     assert sizes[0] >= sizes[1] > 0
+
+
+@pytest.mark.parametrize("rows,k", [((1 << 32) + 5, 32), (5, (1 << 32) + 32), (-1, 32), (1 << 40, 1 << 40)])
+def test_sizes_beyond_32_bits_are_refused_by_the_binding(rows, k):
+    with pytest.raises(ValueError, match="rows"):
+        ie.Mx4Matrix(rows, k)
