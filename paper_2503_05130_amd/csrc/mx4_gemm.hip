@@ -23,22 +23,57 @@ struct Mx4Params {
     Epi epi;
 };
 
+// What is added to four features n .. n + 3 of row m, asked for before the sums.
+struct Tail {
+    f32x4 bias, resid;
+};
+
+typedef u32x2 u32x2_any __attribute__((aligned(2)));
+
+__device__ inline f32x4 mx4_bias(const Mx4Params &p, int n) {
+    f32x4 b = {0.f, 0.f, 0.f, 0.f};
+    if (!p.bias) return b;
+    if (n + 4 <= p.N) {
+        const u32x2 w = *reinterpret_cast<const u32x2_any *>(p.bias + n);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) b[e] = __uint_as_float(e % 2 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (n + e < p.N) b[e] = __uint_as_float((uint32_t)p.bias[n + e] << 16);
+    }
+    return b;
+}
+
+__device__ inline f32x4 mx4_resid(const Mx4Params &p, int m, int n) {
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    if (p.epi != Epi::BiasResidF32 || m >= p.M) return x;
+    const float *resid = p.resid + (size_t)m * p.N + n;
+    if ((p.N & 3) == 0) {
+        if (n < p.N) x = *reinterpret_cast<const f32x4 *>(resid);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (n + e < p.N) x[e] = resid[e];
+    }
+    return x;
+}
+
 // Four features n .. n + 3 of row m.
-__device__ inline void mx4_store(const Mx4Params &p, int m, int n, f32x4 v) {
+__device__ inline void mx4_store(const Mx4Params &p, int m, int n, f32x4 v, const Tail &t) {
     if (m >= p.M) return;
     const int count = min(4, p.N - n);
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-        if (e < count && p.bias) v[e] += __uint_as_float((uint32_t)p.bias[n + e] << 16);
+    v += t.bias;
     const size_t i = (size_t)m * p.N + n;
     if (p.epi == Epi::BiasResidF32) {
         float *out = static_cast<float *>(p.out) + i;
+        v = t.resid + v;
         if ((p.N & 3) == 0) {
-            if (count > 0) *reinterpret_cast<f32x4 *>(out) = *reinterpret_cast<const f32x4 *>(p.resid + i) + v;
+            if (count > 0) *reinterpret_cast<f32x4 *>(out) = v;
         } else {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                if (e < count) out[e] = p.resid[i + e] + v[e];
+                if (e < count) out[e] = v[e];
         }
         return;
     }
@@ -82,6 +117,10 @@ __global__ __launch_bounds__(64 * WAVES) void mx4_split_kernel(Mx4Params p) {
         for (int t = 0; t < RT; ++t) a[t] = p.a + (size_t)min(rt0 + t, last_r) * tile_bytes;
     char *stage = lds + wave * kStage;
     f32x4 acc[FT][RT] = {};
+    static_assert(FT * RT <= WAVES, "a wave stores one block at most");
+    const int m = (rt0 + wave % RT) * 16 + r, n = (ft0 + wave / RT) * 16 + 4 * c;
+    Tail tail = {};
+    if (wave < FT * RT) tail = {mx4_bias(p, n), mx4_resid(p, m, n)};
     struct Chunk {
         u32x4 w[FT], a[NL ? 1 : RT];
         uint32_t ws[FT], as[NL ? 1 : RT];
@@ -150,11 +189,11 @@ __global__ __launch_bounds__(64 * WAVES) void mx4_split_kernel(Mx4Params p) {
 #pragma unroll
         for (int t = 0; t < RT; ++t) part[wave][f * RT + t][lane] = acc[f][t];
     __syncthreads();
-    for (int b = wave; b < FT * RT; b += WAVES) {
-        f32x4 v = part[0][b][lane];
+    if (wave < FT * RT) {
+        f32x4 v = part[0][wave][lane];
 #pragma unroll
-        for (int i = 1; i < WAVES; ++i) v += part[i][b][lane];
-        mx4_store(p, (rt0 + b % RT) * 16 + r, (ft0 + b / RT) * 16 + 4 * c, v);
+        for (int i = 1; i < WAVES; ++i) v += part[i][wave][lane];
+        mx4_store(p, m, n, v, tail);
     }
 }
 
@@ -187,6 +226,9 @@ struct TileCfg {
     static constexpr int BUFFERS = (S * CH + 3) / 4 + 1;                 // of scales: the group in use and those on their way
     static constexpr int SLOT = (TA + TW) * 1024, SCALES = (TA + TW) * 256, LDS = S * CH * SLOT + BUFFERS * SCALES;
     static constexpr int WAVES_SIMD = 163840 / LDS * NW / 4 < 1 ? 1 : 163840 / LDS * NW / 4 > 4 ? 4 : 163840 / LDS * NW / 4;
+    // bias and residual are asked for before the sums where the registers have room: 512 x 4096 x 4096 with residual 19.1 -> 18.0 us with
+    // its quantisation; for 128 x 128 they would spill (1000 x 4096 x 4096 22.9 -> 26.1)
+    static constexpr bool EARLY = FN * FM <= 4;
     static_assert((TA + TW) % NW == 0 && TA % 4 == 0 && TW % 4 == 0 && FM % 2 == 0 && 4 % CH == 0 && S >= 2, "tile");
     static constexpr int ROW = BN * 2 + 16;                              // bytes of a row of the staged output
     static_assert(BM * ROW <= LDS, "output tile");
@@ -283,6 +325,18 @@ __global__ __launch_bounds__(64 * C::NW, C::WAVES_SIMD) void mx4_tile_kernel(Mx4
         for (int i = 0; i < FM; ++i) fa[i] = *reinterpret_cast<const uint32_t *>(s + (wm * FM + i) * 256);
     };
     f32x4 acc[FN][FM] = {};
+    // lane (r, c): row r of a row tile, features 4 c .. 4 c + 3
+    const int r = lane & 15, c = lane >> 4;
+    auto row_of = [&](int t) { return (rt0 + wm * FM + t) * 16 + r; };
+    auto feature_of = [&](int f) { return (ft0 + wn * FN + f) * 16 + 4 * c; };
+    f32x4 bias[FN], resid[C::EARLY ? FN : 1][C::EARLY ? FM : 1];
+    if constexpr (C::EARLY)
+#pragma unroll
+        for (int f = 0; f < FN; ++f) {
+            bias[f] = mx4_bias(p, feature_of(f));
+#pragma unroll
+            for (int t = 0; t < FM; ++t) resid[f][t] = mx4_resid(p, row_of(t), feature_of(f));
+        }
     auto barrier = [&] {
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");      // LDS accesses stay on their side
@@ -366,30 +420,38 @@ __global__ __launch_bounds__(64 * C::NW, C::WAVES_SIMD) void mx4_tile_kernel(Mx4
         if (j + 2 < chunks) step(std::integral_constant<int, 2>{}, std::false_type{}, j + 2);
         if (j + 3 < chunks) step(std::integral_constant<int, 3>{}, std::false_type{}, j + 3);
     }
-    // lane (r, c): row r of a row tile, features 4 c .. 4 c + 3
-    const int r = lane & 15, c = lane >> 4;
+    if constexpr (!C::EARLY)
+#pragma unroll
+        for (int f = 0; f < FN; ++f) bias[f] = mx4_bias(p, feature_of(f));
     if (p.epi == Epi::BiasResidF32 || (p.N & 7) != 0) {
+        // a column of tiles' residual ahead of the one that is stored: the compiler cannot know that none of it is overwritten
+        f32x4 x[2][FM];
+        auto load = [&](int f) {
 #pragma unroll
-        for (int f = 0; f < FN; ++f)
+            for (int t = 0; t < FM; ++t) {
+                if constexpr (C::EARLY) x[f & 1][t] = resid[f][t];
+                else x[f & 1][t] = mx4_resid(p, row_of(t), feature_of(f));
+            }
+        };
+        load(0);
 #pragma unroll
-            for (int t = 0; t < FM; ++t)
-                mx4_store(p, (rt0 + wm * FM + t) * 16 + r, (ft0 + wn * FN + f) * 16 + 4 * c, acc[f][t]);
+        for (int f = 0; f < FN; ++f) {
+            if (f + 1 < FN) load(f + 1);
+#pragma unroll
+            for (int t = 0; t < FM; ++t) mx4_store(p, row_of(t), feature_of(f), acc[f][t], {bias[f], x[f & 1][t]});
+        }
         return;
     }
     // bf16 by way of LDS: a store straight from the registers would cover 16 rows x 32 bytes
     __syncthreads();
 #pragma unroll
     for (int f = 0; f < FN; ++f) {
-        const int n = (ft0 + wn * FN + f) * 16 + 4 * c;
-        float bias[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) bias[e] = p.bias && n + e < p.N ? __uint_as_float((uint32_t)p.bias[n + e] << 16) : 0.f;
 #pragma unroll
         for (int t = 0; t < FM; ++t) {
             f32x4 v = acc[f][t];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                v[e] += bias[e];
+                v[e] += bias[f][e];
                 if (p.epi == Epi::BiasGeluBf16) v[e] = gelu(v[e]);
             }
             *reinterpret_cast<u32x2 *>(lds + ((wm * FM + t) * 16 + r) * C::ROW + ((wn * FN + f) * 16 + 4 * c) * 2) =
@@ -424,9 +486,11 @@ hipError_t launch_tile(const Mx4Params &p, hipStream_t stream) {
 template <int NL>
 hipError_t launch_few(const Mx4Params &p, hipStream_t stream) {
     const int tiles = (p.N + 15) / 16;
-    if (NL == 4 && tiles >= 1024) return launch_split<4, 1, 8, NL>(p, stream);
+    if constexpr (NL == 4)
+        if (tiles >= 1024) return launch_split<4, 1, 8, NL>(p, stream);
     if (tiles >= 512) return launch_split<2, 1, 8, NL>(p, stream);
-    if (NL > 0 && mx4_chunks(p.K) >= 64) return launch_split<1, 1, 16, NL>(p, stream);
+    if constexpr (NL > 0)
+        if (mx4_chunks(p.K) >= 64) return launch_split<1, 1, 16, NL>(p, stream);
     return launch_split<1, 1, 8, NL>(p, stream);
 }
 
