@@ -59,7 +59,14 @@ __device__ inline f32x4 mx4_resid(const Mx4Params &p, int m, int n) {
     return x;
 }
 
+template <bool FAR, class T>
+__device__ inline void put(T *to, T v) {
+    if constexpr (FAR) __builtin_nontemporal_store(v, to);
+    else *to = v;
+}
+
 // Four features n .. n + 3 of row m.
+template <bool FAR = false>
 __device__ inline void mx4_store(const Mx4Params &p, int m, int n, f32x4 v, const Tail &t) {
     if (m >= p.M) return;
     const int count = min(4, p.N - n);
@@ -69,7 +76,7 @@ __device__ inline void mx4_store(const Mx4Params &p, int m, int n, f32x4 v, cons
         float *out = static_cast<float *>(p.out) + i;
         v = t.resid + v;
         if ((p.N & 3) == 0) {
-            if (count > 0) *reinterpret_cast<f32x4 *>(out) = v;
+            if (count > 0) put<FAR>(reinterpret_cast<f32x4 *>(out), v);
         } else {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
@@ -217,8 +224,9 @@ hipError_t launch_split(Mx4Params p, hipStream_t stream) {
 // chunk j; products of the first half; where chunk j + 1 begins a stage, wait for the own copies of it and the own reads,
 // barrier (the stage is there, nobody reads chunk j's any more), and copy the stage S further into that slot; read chunk j +
 // 1's features and first half; products of the second half.
-template <int BM_, int BN_, int WM_, int WN_, int CH_, int S_>
+template <int BM_, int BN_, int WM_, int WN_, int CH_, int S_, bool FAR_ = false>
 struct TileCfg {
+    static constexpr bool FAR = FAR_;      // the output past the last cache
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NW = WM * WN, CH = CH_, S = S_;
     static constexpr int TA = BM / 16, TW = BN / 16, FM = TA / WM, FN = TW / WN, H = FM / 2;
     static constexpr int COPIES = (TA + TW) / NW;                        // of a wave and chunk
@@ -438,7 +446,7 @@ __global__ __launch_bounds__(64 * C::NW, C::WAVES_SIMD) void mx4_tile_kernel(Mx4
         for (int f = 0; f < FN; ++f) {
             if (f + 1 < FN) load(f + 1);
 #pragma unroll
-            for (int t = 0; t < FM; ++t) mx4_store(p, row_of(t), feature_of(f), acc[f][t], {bias[f], x[f & 1][t]});
+            for (int t = 0; t < FM; ++t) mx4_store<C::FAR>(p, row_of(t), feature_of(f), acc[f][t], {bias[f], x[f & 1][t]});
         }
         return;
     }
@@ -464,8 +472,8 @@ __global__ __launch_bounds__(64 * C::NW, C::WAVES_SIMD) void mx4_tile_kernel(Mx4
     for (int i = threadIdx.x; i < C::BM * PIECES; i += 64 * NW) {
         const int m = rt0 * 16 + i / PIECES, n = ft0 * 16 + i % PIECES * 8;
         if (m < p.M && n < p.N)
-            *reinterpret_cast<u32x4 *>(out + (size_t)m * p.N + n) =
-                *reinterpret_cast<const u32x4 *>(lds + i / PIECES * C::ROW + i % PIECES * 16);
+            put<C::FAR>(reinterpret_cast<u32x4 *>(out + (size_t)m * p.N + n),
+                        *reinterpret_cast<const u32x4 *>(lds + i / PIECES * C::ROW + i % PIECES * 16));
     }
 }
 
@@ -504,6 +512,8 @@ int64_t tiles_of(int M, int N, int side) { return (int64_t)((M + side - 1) / sid
 //   201 x  1024 x 4096   4.5  7.4  9.8            512 x  4096 x 4096  16.8  9.9 10.5
 //   128 x  8192 x 2048   7.7  5.9  7.4           1000 x  4096 x 4096  28.2 19.6 13.3
 //  4096 x  4096 x 4096             42.2 37.1     2048 x  8192 x 2048             27.4 24.2
+// An output of more than 32 MiB goes past the last cache, which the operands need (with quantisation, us, without / with the hint):
+//   8192 x 16384 x 2048 274 233     4096 x 4096 x 4096, fp32 residual 83 74     8192 x 8192 x 8192 285 278     4096 x 4096 x 4096 bf16 45.6 46.2
 hipError_t launch_mx4_gemm(Epi epi, const void *a, const void *w, const bf16_t *bias, const float *resid, void *out, int M,
                            int N, int K, hipStream_t stream) {
     const Mx4Params p{static_cast<const char *>(a), static_cast<const char *>(w), nullptr, bias, resid, out, M, N, K, 0, epi};
@@ -511,7 +521,10 @@ hipError_t launch_mx4_gemm(Epi epi, const void *a, const void *w, const bf16_t *
     if (M <= 32) return N > 8176 ? launch_split<2, 2, 8, 0>(p, stream) : launch_split<1, 2, 8, 0>(p, stream);
     if (tiles_of(M, N, 32) <= 320) return launch_split<2, 2, 8, 0>(p, stream);
     if (tiles_of(M, N, 64) <= 512) return launch_tile<TileCfg<64, 64, 2, 2, 4, 2>>(p, stream);
-    if (tiles_of(M, N, 256) >= 192) return launch_tile<TileCfg<256, 256, 2, 4, 1, 4>>(p, stream);
+    if (tiles_of(M, N, 256) >= 192) {
+        const bool far = (int64_t)M * N * (epi == Epi::BiasResidF32 ? 4 : 2) > 32 << 20;
+        return far ? launch_tile<TileCfg<256, 256, 2, 4, 1, 4, true>>(p, stream) : launch_tile<TileCfg<256, 256, 2, 4, 1, 4>>(p, stream);
+    }
     return launch_tile<TileCfg<128, 128, 4, 2, 1, 4>>(p, stream);
 }
 

@@ -269,7 +269,8 @@ def test_refusals_of_the_binding():
 
 
 @pytest.mark.parametrize("m,n,k", [(1100, 1040, 416), (1025, 1025, 128), (2100, 700, 1700), (3501, 3603, 384), (4096, 3500, 640), (8200, 1601, 96),
-                                   (2100, 2100, 300), (1601, 2304, 1152), (4000, 1500, 2700), (3500, 3600, 2176), (1100, 1040, 4160)])
+                                   (2100, 2100, 300), (1601, 2304, 1152), (4000, 1500, 2700), (3500, 3600, 2176), (1100, 1040, 4160),
+                                   (5200, 3608, 256), (6100, 3100, 160)])
 @pytest.mark.parametrize("epilogue", ["bias", "residual"])
 def test_many_rows(m, n, k, epilogue):
     w, wv = _weight(n, k, n + k)
