@@ -98,8 +98,8 @@ __device__ inline void mx4_store(const Mx4Params &p, int m, int n, f32x4 v, cons
 }
 
 // Few rows: bound by the weights' bytes and, below some 10 MB, by latency (launch, a chain of two loads, the joining of the waves).
-// 4 x 4096 -> 16384 takes 5.9 us of 4-bit rows (6.1 TB/s), 6.5 of bf16 ones; 1 x 2048 -> 8192 3.3 and 3.4 us; 32 x 8192 -> 8192
-// 6.8 (5.4 TB/s).
+// 4 x 4096 -> 16384 takes 5.9 us of 4-bit rows (6.1 TB/s), 6.4 of bf16 ones; 1 x 2048 -> 8192 3.2 and 3.4 us; 32 x 8192 -> 8192
+// 6.7 (5.4 TB/s).  Bias and residual are asked for first: at the end they cost 0.3 to 0.6 us.
 //
 // A workgroup's tile of 16 FT features x 16 RT rows with K spread over its waves, chunk by chunk, and the waves' sums
 // added in wave order through LDS.  Operands go from memory to registers.  NL > 0: A is bf16, 4 NL >= M rows: a chunk of them is loaded in
@@ -214,8 +214,8 @@ hipError_t launch_split(Mx4Params p, hipStream_t stream) {
 
 // Many rows: a workgroup's tile of BM rows x BN features, through LDS.  A lane's operand is 16 bytes for 16 x 16 x 128 x 2 / 64 operations, so that
 // a wave of 128 x 64 reads 12 KB of LDS for 32 products of 16 cycles each; registers alone (the kernel above) come to half the rate.
-// 8192^3 takes 245 us (4.5 PFLOP/s) at a clock that falls to 1.9 GHz: the matrix cores are busy for 62% of the whole and 67% of the
-// loop, the other 43 us are the first stages' loads and the output of 4 rounds of workgroups.  4096^3 37 us (3.7 PFLOP/s).  A ring of
+// 8192^3 takes 236 - 246 us (4.5 PFLOP/s) at a clock that falls to 1.9 GHz: the matrix cores are busy for 62% of the whole and 67% of the
+// loop, some 40 us are the first stages' loads and the output of 4 rounds of workgroups.  4096^3 37 us (3.7 PFLOP/s).  A ring of
 // four stages in place of two for 64 x 64 tiles gained nothing (201 x 4096 x 4096, 250 x 4096 x 4096, 150 x 2048 x 8192).
 //
 // The operands' 1 KB blocks are copied from global memory straight into a ring of S stages of CH chunks of K, each block by one
