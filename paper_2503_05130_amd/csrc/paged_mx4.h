@@ -144,7 +144,7 @@ __global__ __launch_bounds__(kTileThreads) void paged_read_kernel(PagedCache c, 
 // bf16 rest (see paged.hip).  V becomes bf16 on the way, by v_cvt_scalef32_pk_bf16_fp4 under the scale as it is stored.
 //
 // Bound by the pages' bytes, and next by the vector instructions that turn V into bf16 and the scores into probabilities: 64 requests of 4000 to 8192
-// keys, 32 / 8 heads of 128, 408 MB, take 91 us with capped scores (4.5 TB/s, 51% of the issue slots) and 4.3 for the joining (the call 98 - 106, 93 - 95 without a cap); one of 300 keys 6.6,
+// keys, 32 / 8 heads of 128, 408 MB, take 86 us with capped scores (4.7 TB/s, 51% of the issue slots) and 4.3 for the joining (the call 91 - 101, 93 - 95 without a cap); one of 300 keys 6.6,
 // a chain of loads (length, table, page) and the joining of 8 waves.  Not kept: every lane working on all scores of its heads (103 and 115 us);
 // steps of 32 keys; the next step's loads asked for ahead, whose registers spill or halve the waves.
 //
@@ -268,7 +268,7 @@ __global__ __launch_bounds__(64 * WAVES, HC < 16 ? 4 : WAVES == 8 ? 2 : 3) void 
     constexpr int ROW = DH + 4;
     __shared__ __attribute__((aligned(16))) float o_lds[WAVES][HC][ROW];
     __shared__ float m_lds[WAVES][HC], l_lds[WAVES][HC];
-    static_assert(ROW >= 16 * T, "a wave's probabilities lie where its context will");
+    static_assert(ROW > 16 * T, "a wave's probabilities lie where its context will");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, c = lane >> 4;
     const int group = a.heads / a.c.kv_heads, tiles = (group + 15) / 16;
@@ -295,10 +295,12 @@ __global__ __launch_bounds__(64 * WAVES, HC < 16 ? 4 : WAVES == 8 ? 2 : 3) void 
         const int k0 = it.part << part_log2, k1 = min(it.keys, k0 + (1 << part_log2));
         const int32_t *ids = a.table + (size_t)it.b * a.table_stride;
         const Q16<DH> q16(a.q + (int64_t)it.b * a.q_stride + (head0 + min(r % HC, n_heads - 1)) * DH, c);
-        float slope[4];
-        if constexpr (SCORED)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) slope[e] = a.slopes ? a.slopes[head0 + min(own_heads + e, n_heads - 1)] * kLog2e : 0.f;
+        // the heads' slopes wait behind the wave's probabilities: in four registers they made others spill, also where there is but a cap
+        // (64 x 4000 - 8192 capped 105 us, now 101; capped and lowered 108, now 104)
+        if constexpr (SCORED) {
+            if (a.slopes && lane < HC) p_lds[lane][16 * T] = __float_as_uint(a.slopes[head0 + min(lane, n_heads - 1)] * kLog2e);
+            wave_lds_fence();
+        }
         float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, l[4] = {0.f, 0.f, 0.f, 0.f};      // of its scores' heads
         f32x4 o[W] = {};                                                                            // of head r % HC
         const int steps = (k1 - k0 + 16 * T - 1) / (16 * T), own = (steps - wave + WAVES - 1) / WAVES;      // this wave's
@@ -376,7 +378,7 @@ __global__ __launch_bounds__(64 * WAVES, HC < 16 ? 4 : WAVES == 8 ? 2 : 3) void 
                     float y = z[e] * a.scale_log2e;
                     if constexpr (SCORED) {
                         if (a.cap_log2e != 0.f) y = capped(a, y);
-                        if (a.slopes) y = fmaf(-slope[e], (float)(it.keys - 1 - (key0 + 16 * tile_of + r)), y);
+                        if (a.slopes) y = fmaf(-__uint_as_float(p_lds[own_heads + e][16 * T]), (float)(it.keys - 1 - (key0 + 16 * tile_of + r)), y);
                     }
                     if (least < 16 && r >= keys) y = -INFINITY;
                     p[s][e] = y;
