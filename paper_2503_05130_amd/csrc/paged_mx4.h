@@ -146,7 +146,8 @@ __global__ __launch_bounds__(kTileThreads) void paged_read_kernel(PagedCache c, 
 // Bound by the pages' bytes, and next by the vector instructions that turn V into bf16 and the scores into probabilities: 64 requests of 4000 to 8192
 // keys, 32 / 8 heads of 128, 408 MB, take 86 us with capped scores (4.7 TB/s, 51% of the issue slots) and 4.3 for the joining (the call 91 - 101, 93 - 95 without a cap); one of 300 keys 6.6,
 // a chain of loads (length, table, page) and the joining of 8 waves.  Not kept: every lane working on all scores of its heads (103 and 115 us);
-// steps of 32 keys; the next step's loads asked for ahead, whose registers spill or halve the waves.
+// steps of 32 keys; the next step's loads asked for ahead, or the
+// first one's before q is converted, whose registers spill (137 us uncapped) or halve the waves.
 //
 // The reference of the exponents need not be the largest score: it is raised, and sums and context scaled down, when a score
 // exceeds it by 2^8, which in a row of many keys is rare; probabilities up to 2^8 are as exact as those up to 1.
