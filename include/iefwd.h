@@ -712,6 +712,7 @@ int iefwd_paged_attention(const iefwd_paged_cache *cache, const void *q, uint64_
 
 /* The same with other scores: with s_j = scale * q . k_j, cap tanh(s_j / cap) in its place (cap 0: s_j itself), less slopes[h] (f32
  * [n_heads], finite, or NULL: 0) times the distance lens[b] - 1 - j of the key from the newest one.  cap 0 or in [2^-60, 2^60].
+ * Slopes may be negative; from +-2^95 on, a step of the distance being more than scores differ by, they count as less than they are.
  * Over a cache of IEFWD_KV_MX4, here and above, q enters the product as two e4m3 numbers, under scales for 32 columns each:
  * exact down to 2^-13 of the largest of these, and off by 2^-21 of it below; an infinity or NaN of q makes its head's row NaN,
  * and a block of a key or value that is NaN does what the formula says. */

@@ -404,7 +404,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attention_kernel(AttnArgs
                 q[i] = *reinterpret_cast<const bf16x8 *>(qh + d);
             }
         }
-        const float slope = SCORED && a.slopes ? a.slopes[head0 + min(r, n_heads - 1)] * kLog2e : 0.f;
+        const float slope = SCORED && a.slopes ? slope_log2e(a.slopes[head0 + min(r, n_heads - 1)]) : 0.f;
         float m = -INFINITY, l = 0.f;
         f32x4 o[NV][W] = {};
         const int steps = (k1 - k0 + 31) / 32;
@@ -458,7 +458,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attention_kernel(AttnArgs
                         float z = s[e] * scale;
                         if constexpr (SCORED) {
                             if (a.cap_log2e != 0.f) z = capped(a, z);
-                            if (a.slopes) z = fmaf(-slope, (float)(it.keys - 1 - (key0 + 16 * t + 4 * c + e)), z);
+                            if (a.slopes) z = lowered(z, slope, key0 + 16 * t + 4 * c + e, it.keys - 1);
                         }
                         p[4 * t + e] = 4 * c + e < limit[t] ? z : -INFINITY;
                         mx = fmaxf(mx, p[4 * t + e]);

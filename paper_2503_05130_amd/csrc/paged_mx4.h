@@ -299,7 +299,7 @@ __global__ __launch_bounds__(64 * WAVES, HC < 16 ? 4 : WAVES == 8 ? 2 : 3) void 
         // the heads' slopes wait behind the wave's probabilities: in four registers they made others spill, also where there is but a cap
         // (64 x 4000 - 8192 capped 105 us, now 101; capped and lowered 108, now 104)
         if constexpr (SCORED) {
-            if (a.slopes && lane < HC) p_lds[lane][16 * T] = __float_as_uint(a.slopes[head0 + min(lane, n_heads - 1)] * kLog2e);
+            if (a.slopes && lane < HC) p_lds[lane][16 * T] = __float_as_uint(slope_log2e(a.slopes[head0 + min(lane, n_heads - 1)]));
             wave_lds_fence();
         }
         float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, l[4] = {0.f, 0.f, 0.f, 0.f};      // of its scores' heads
@@ -379,7 +379,7 @@ __global__ __launch_bounds__(64 * WAVES, HC < 16 ? 4 : WAVES == 8 ? 2 : 3) void 
                     float y = z[e] * a.scale_log2e;
                     if constexpr (SCORED) {
                         if (a.cap_log2e != 0.f) y = capped(a, y);
-                        if (a.slopes) y = fmaf(-__uint_as_float(p_lds[own_heads + e][16 * T]), (float)(it.keys - 1 - (key0 + 16 * tile_of + r)), y);
+                        if (a.slopes) y = lowered(y, __uint_as_float(p_lds[own_heads + e][16 * T]), key0 + 16 * tile_of + r, it.keys - 1);
                     }
                     if (least < 16 && r >= keys) y = -INFINITY;
                     p[s][e] = y;
