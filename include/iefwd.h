@@ -801,7 +801,9 @@ int iefwd_mx4_gemm_bf16(uint32_t epilogue, const void *a, const void *w, const v
  * may be captured.  logits IEFWD_BF16 or IEFWD_F32 [rows, vocab], rows stride >= vocab elements apart, no
  * alignment beyond the type's; fp32 sums relative to the row's largest logit; the same bits on every call. */
 
-/* Bytes of workspace that iefwd_token_logprobs needs (0 where rows are not cut into parts). Host only. */
+/* Bytes of workspace that iefwd_token_logprobs needs for just these sizes (0 where rows are not cut into parts): fewer rows may need
+ * more than these, since they are cut into more parts.  min(64 rows, 2048) * (12 + 8 n_top) bytes are enough for any number of rows up
+ * to `rows` and alternatives up to n_top. Host only. */
 int iefwd_token_logprobs_workspace(uint32_t rows, uint32_t vocab, uint32_t n_top, size_t *bytes);
 
 /* tokens int64 [rows]; logprobs f32 [rows], 0 for a token outside [0, vocab) (padding); entropy f32 [rows] or NULL; stats

@@ -817,13 +817,16 @@ class Mx4Matrix:
 
 # ------------------------------------------------------------------ log probabilities of tokens
 def token_logprobs_workspace(rows: int, vocab: int, n_top: int = 0, device="cuda:0") -> torch.Tensor:
-    """A workspace for ``token_logprobs``, in memory of torch's current stream: calls on another one have to be ordered
-    behind it, and the workspace to live until they have run."""
+    """A workspace for ``token_logprobs`` on up to this many rows and most probable tokens (fewer rows may need more than these, and
+    have it), in memory of torch's current stream: calls on another one have to be ordered behind it, and the workspace to live
+    until they have run."""
     if rows >> 32 or vocab >> 32 or n_top >> 32:
         raise ValueError("sizes must be below 2^32")
     n = _sz()
-    _check(lib().iefwd_token_logprobs_workspace(rows, vocab, n_top, ctypes.byref(n)), "iefwd_token_logprobs_workspace")
-    return torch.empty(n.value, dtype=torch.uint8, device=device)
+    for r in (rows, 1):
+        _check(lib().iefwd_token_logprobs_workspace(r, vocab, n_top, ctypes.byref(n)), "iefwd_token_logprobs_workspace")
+    # where a row alone is not cut into parts, none are; else the most of any number of rows
+    return torch.empty(min(64 * rows, 2048) * (12 + 8 * n_top) if n.value else 0, dtype=torch.uint8, device=device)
 
 
 def _logits(name: str, t) -> tuple[int, int, int, int, int]:

@@ -1,0 +1,26 @@
+"""A workspace that is made for the largest batch serves every smaller one (no GPU needed)."""
+import ctypes
+
+import pytest
+
+import paper_2503_05130_amd as ie
+
+ROWS = [1, 2, 3, 7, 31, 32, 33, 48, 64, 65, 100, 127, 128, 200, 256, 300, 512, 600, 682, 683, 1000, 1024, 1025, 2000, 2048, 2049, 4096, 5000]
+
+
+def _logprobs_bytes(rows, vocab, n):
+    b = ctypes.c_size_t()
+    assert ie.lib().iefwd_token_logprobs_workspace(rows, vocab, n, ctypes.byref(b)) == ie.OK
+    return b.value
+
+
+@pytest.mark.parametrize("vocab", [100, 8192, 8193, 20001, 50000, 131072, 600000, 1 << 24])
+@pytest.mark.parametrize("n", [0, 5, 32])
+def test_log_probabilities(vocab, n):
+    need = {r: _logprobs_bytes(r, vocab, n) for r in ROWS if r * vocab <= 1 << 35}
+    for r in need:
+        # the documented bound
+        assert need[r] <= min(64 * r, 2048) * (12 + 8 * n)
+        given = ie.token_logprobs_workspace(r, vocab, n, device="cpu").numel()
+        assert given >= max(need[s] for s in need if s <= r)
+        assert given <= min(64 * r, 2048) * (12 + 8 * n) and (given > 0) == (vocab > 8192)
