@@ -685,7 +685,8 @@ int iefwd_paged_read(const iefwd_paged_cache *cache, const int64_t *slots, void 
                      uint64_t k_stride, uint64_t v_stride, void *stream);
 
 /* Bytes of workspace that iefwd_paged_attention needs for a batch and a table of
- * max_pages columns (0 where no request can be long enough to be split). Host only. */
+ * max_pages columns (0 where no request can be long enough to be split).  A smaller batch may need more, since its requests are cut
+ * into more parts; a narrower table does not. Host only. */
 int iefwd_paged_attention_workspace(const iefwd_paged_cache *cache, uint32_t batch, uint32_t n_heads,
                                     uint32_t max_pages, size_t *bytes);
 

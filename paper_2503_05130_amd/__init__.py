@@ -606,12 +606,17 @@ class PagedCache:
         _call(dev, stream, "iefwd_paged_read", self._ref, slots.data_ptr(), k.data_ptr(), v.data_ptr(), n, ks, vs)
 
     def workspace(self, batch: int, n_heads: int, max_pages: int) -> torch.Tensor:
-        """A workspace for ``attention`` on a batch and a table of max_pages columns, in memory of torch's current
-        stream: calls on another one have to be ordered behind it, and the workspace to live until they have run."""
-        n = _sz()
-        _check(lib().iefwd_paged_attention_workspace(self._ref, batch, n_heads, max_pages, ctypes.byref(n)),
-               "iefwd_paged_attention_workspace")
-        return torch.empty(n.value, dtype=torch.uint8, device=self.device)
+        """A workspace for ``attention`` on a batch of up to this size (a smaller one may need more, and has it) and a table of
+        up to max_pages columns, in memory of torch's current stream: calls on another one have to be ordered behind it, and the
+        workspace to live until they have run."""
+        n, most = _sz(), 0
+        # requests are cut into fewer parts at each power of two of batch x key-value heads x tiles of 16 heads, up to 256
+        rows = max(self.n_kv_heads * -(-n_heads // (16 * self.n_kv_heads)), 1)
+        for b in {batch, *(min(batch, (1 << i) // rows) for i in range(9))} - {0} or {0}:
+            _check(lib().iefwd_paged_attention_workspace(self._ref, b, n_heads, max_pages, ctypes.byref(n)),
+                   "iefwd_paged_attention_workspace")
+            most = max(most, n.value)
+        return torch.empty(most, dtype=torch.uint8, device=self.device)
 
     def attention(self, q, table, lens, out, workspace, scale: float | None = None, stream=None, cap: float = 0.0,
                   slopes=None) -> None:

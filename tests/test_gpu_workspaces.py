@@ -32,3 +32,23 @@ def test_log_probabilities(dtype):
         assert all(torch.equal(a, b) for a, b in zip(got, want)), rows
         top = torch.topk(x[:rows].float(), n, dim=1).values
         assert torch.equal(x[:rows].gather(1, got[2].long()).float(), top)
+
+
+@pytest.mark.parametrize("mx4", [False, True])
+@pytest.mark.parametrize("keys", [1024, 2048])
+def test_paged_attention(mx4, keys):
+    heads, kv, dim, page, batch = 16, 4, 64, 32, 70
+    g = torch.Generator(device=DEV).manual_seed(2)
+    pages = 150
+    c = ie.PagedCache.empty(pages, page, kv, dim, mx4=mx4)
+    c.append(*(torch.randn(pages * page, kv, dim, generator=g, device=DEV).to(BF) for _ in range(2)), torch.arange(pages * page, device=DEV))
+    q = torch.randn(batch, heads, dim, generator=g, device=DEV).to(BF)
+    table = torch.randint(pages, (batch, keys // page), generator=g, device=DEV).int()
+    lens = torch.randint(keys // 2, keys + 1, (batch,), generator=g, device=DEV).int()
+    ws = c.workspace(batch, heads, keys // page)
+    for b in (70, 64, 33, 32, 16, 5, 1):
+        out = torch.full((2, b, heads, dim), 7.0, dtype=BF, device=DEV)
+        for i, space in enumerate((ws, torch.full((1 << 23,), 0xFF, dtype=torch.uint8, device=DEV))):
+            c.attention(q[:b], table[:b], lens[:b], out[i], space)
+        sync()
+        assert torch.equal(out[0], out[1]) and not (out[0] == 7.0).any()
