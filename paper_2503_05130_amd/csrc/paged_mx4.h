@@ -2,6 +2,8 @@
 // every kind of cache read back.  Part of paged.hip.
 #pragma once
 
+#include <algorithm>
+
 #include "paged_device.h"
 
 namespace iefwd {
@@ -527,9 +529,16 @@ hipError_t launch_mx4_heads(const AttnArgs &a, bool stream_pages, dim3 grid, hip
                         : launch_mx4_w<DH, 16, WAVES>(a, stream_pages, grid, stream);
 }
 
-dim3 grid_of(const PagedCache &c, int tokens) {
-    const int per_tile = kTileThreads / (c.head_dim / 8);
-    return dim3((unsigned)((int64_t)((tokens + per_tile - 1) / per_tile) * c.kv_heads));
+// launch(grid, first token, tokens), in one go but for the very most tokens: a grid holds less than 2^32 threads.
+template <class Launch>
+hipError_t in_grids(const PagedCache &c, int tokens, Launch launch) {
+    const int per_tile = kTileThreads / (c.head_dim / 8), most = (1 << 23) / c.kv_heads * per_tile;
+    hipError_t e = hipSuccess;
+    for (int64_t at = 0; at < tokens && e == hipSuccess; at += most) {
+        const int n = (int)std::min<int64_t>(most, tokens - at);
+        e = launch(dim3((unsigned)((n + per_tile - 1) / per_tile * c.kv_heads)), at, n);
+    }
+    return e;
 }
 
 // Of the tokens' keys and values in bf16.  From 64 MiB on new ones are read, from 32 MiB on read ones written past the last cache: append and
@@ -541,7 +550,10 @@ template <KvKind KIND>
 hipError_t launch_read(const PagedCache &c, const int64_t *slots, bf16_t *k, bf16_t *v, int tokens, int64_t k_stride,
                        int64_t v_stride, hipStream_t stream) {
     auto launch = [&](auto kernel) {
-        return launch_kernel(kernel, grid_of(c, tokens), dim3(kTileThreads), stream, c, slots, k, v, tokens, k_stride, v_stride);
+        return in_grids(c, tokens, [&](dim3 grid, int64_t at, int n) {
+            return launch_kernel(kernel, grid, dim3(kTileThreads), stream, c, slots + at, k + at * k_stride, v + at * v_stride, n, k_stride,
+                                 v_stride);
+        });
     };
     const bool far = bytes_of(c, tokens) >= 32 << 20;
     if (c.head_dim == 64) return far ? launch(paged_read_kernel<64, KIND, true>) : launch(paged_read_kernel<64, KIND, false>);
@@ -567,7 +579,10 @@ hipError_t launch_attention_mx4(const AttnArgs &a, bool stream_pages, dim3 grid,
 hipError_t launch_paged_append_mx4(const PagedCache &c, const bf16_t *k, const bf16_t *v, const int64_t *slots, int tokens,
                                    int64_t k_stride, int64_t v_stride, hipStream_t stream) {
     auto launch = [&](auto kernel) {
-        return launch_kernel(kernel, grid_of(c, tokens), dim3(kTileThreads), stream, c, k, v, slots, tokens, k_stride, v_stride);
+        return in_grids(c, tokens, [&](dim3 grid, int64_t at, int n) {
+            return launch_kernel(kernel, grid, dim3(kTileThreads), stream, c, k + at * k_stride, v + at * v_stride, slots + at, n, k_stride,
+                                 v_stride);
+        });
     };
     const bool far = bytes_of(c, tokens) >= 64 << 20;
     if (c.head_dim == 64) return far ? launch(paged_append_mx4_kernel<64, true>) : launch(paged_append_mx4_kernel<64, false>);
