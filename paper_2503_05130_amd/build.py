@@ -22,8 +22,8 @@ BUILD_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libiefwd.so")
 ARCH = "gfx950"
 
-SOURCES = ["gemm.hip", "attention.hip", "decode.hip", "layernorm.hip", "train.hip", "paged.hip", "q4.hip", "mx4.hip", "mx4_gemm.hip", "logprobs.hip", "quota.cpp", "controller.cpp", "init_weights.cpp",
-           "iefwd.cpp", "paged_abi.cpp", "mx4_abi.cpp",
+SOURCES = ["gemm.hip", "attention.hip", "decode.hip", "layernorm.hip", "train.hip", "paged.hip", "q4.hip", "mx4.hip", "mx4_gemm.hip",
+           "logprobs.hip", "quota.cpp", "controller.cpp", "init_weights.cpp", "iefwd.cpp", "paged_abi.cpp", "mx4_abi.cpp",
            "logprobs_abi.cpp"]
 
 COMMON = [

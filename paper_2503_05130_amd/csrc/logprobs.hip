@@ -6,9 +6,10 @@
 //   log p_j = s d_j - log S,  entropy = -sum p_j log p_j = log S - s T / S
 // Both are differences of small numbers where the row is sure of a token: relative to m nothing large cancels.
 //   gradient of g_l log p_t + g_h entropy:  s (g_l (1[j = t] - p_j) - g_h p_j (log p_j + entropy))
-// Bound by reading the logits once (and writing the gradient): 4095 x 65003 bf16 in 98 us (5.4 TB/s; 8.9 vector
-// instructions an element, 81% of the issue slots) and its gradient in 194 (5.5 TB/s; 11.6 an element, 51%).  Few rows by latency and issue: 48 x
-// 131072 with 5 alternatives 9.0 us and 3.5 for joining the parts, of which the bytes are 2.1.
+// Bound by reading the logits once (and writing the gradient): 4095 x 65003 bf16 in 105 us between gradients (median of a profile, 5.1
+// TB/s; alone from a graph 100; 8.9 vector instructions an element, 81% of the issue slots) and its gradient in 193 (5.5 TB/s; 11.6 an
+// element, 51%).  Few rows by latency and issue: 48 x 131072 with 5 alternatives 9.1 us and 3.4 for joining the parts, of which the
+// bytes are 2.1.  Alternatives cost many rows too: 1000 x 128000 with 32 of them 78 us, without 56; fp32 500 x 128000 64 and 50.
 #include "logprobs.h"
 
 #include <algorithm>
@@ -480,8 +481,9 @@ __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(LogprobGradArgs
     }
 }
 
-// Few rows are cut into parts that the whole chip works on: up to 2048 workgroups, whole rounds of their waves' tiles each (F32: of
-// 6144 elements, bf16 of 8192, taken for both).
+// Few rows are cut into parts that the whole chip works on: up to 2048 workgroups, whole rounds of their waves' tiles each (bf16: of
+// 8192 elements, taken for fp32 as well, whose rounds are of 6144 and whose last round in a part is a third full.  fp32, us, in parts of
+// 8192 / 6144: 48 x 131072 9.5 9.5, with 5 alternatives 15.1 14.9, 1 x 131072 5.5 4.6, with 5 10.5 9.1, 300 x 50001 15.3 14.9).
 struct Split {
     int parts, part;
 };
@@ -504,7 +506,7 @@ hipError_t launch_logprobs(const LogprobArgs &a, hipStream_t stream) {
     const Split s = split_of(a.rows, a.vocab);
     const int parts = s.parts;
     const dim3 grid((unsigned)((int64_t)a.rows * parts));
-    // a wave a row where its tiles are two at most
+    // a wave a row where its tiles are two at most (of bf16; three of fp32)
     const int waves = a.vocab <= 4096 ? 1 : 4;
     auto launch = [&](auto kernel) { return launch_kernel(kernel, grid, dim3(64 * waves), stream, a, s.parts, s.part); };
     const int lists = a.top == 0 ? 0 : a.top <= 8 || waves == 1 ? 1 : 2;

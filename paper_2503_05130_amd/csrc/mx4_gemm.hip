@@ -212,11 +212,14 @@ hipError_t launch_split(Mx4Params p, hipStream_t stream) {
                          dim3(64 * WAVES), stream, p);
 }
 
-// Many rows: a workgroup's tile of BM rows x BN features, through LDS.  A lane's operand is 16 bytes for 16 x 16 x 128 x 2 / 64 operations, so that
-// a wave of 128 x 64 reads 12 KB of LDS for 32 products of 16 cycles each; registers alone (the kernel above) come to half the rate.
-// 8192^3 takes 236 - 246 us (4.5 PFLOP/s) at a clock that falls to 1.9 GHz: the matrix cores are busy for 62% of the whole and 67% of the
-// loop, some 40 us are the first stages' loads and the output of 4 rounds of workgroups.  4096^3 37 us (3.7 PFLOP/s).  A ring of
-// four stages in place of two for 64 x 64 tiles gained nothing (201 x 4096 x 4096, 250 x 4096 x 4096, 150 x 2048 x 8192).
+// Many rows: a workgroup's tile of BM rows x BN features, through LDS.  A lane's operand is 16 bytes for 16 x 16 x 128 x 2 / 64
+// operations, so that a wave of 128 x 64 reads 12 KB of LDS for 32 products of 16 cycles each; registers alone (the kernel above) come
+// to half the rate.  8192^3 takes 240 us from a graph (4.6 PFLOP/s) and 255 between quantisations (median of a profile, least 242; 4.3) at
+// a clock that falls to 1.8 GHz: the matrix cores are busy for 62% of the whole and 67% of the loop, some 40 us are the first stages'
+// loads and the output of 4 rounds of workgroups.  4096^3 37 us (3.7 PFLOP/s).  A 256 x 256 tile has a CU for itself (144 KB of LDS), so
+// that its epilogue follows its products: 8192 x 16384 x 2048 with bias 175 us, with GELU 228; 4096^3 38, 45 and with the fp32 residual 58.
+// (The compiler spills 4 of its registers.)
+// A ring of four stages in place of two for 64 x 64 tiles gained nothing (201 x 4096 x 4096, 250 x 4096 x 4096, 150 x 2048 x 8192).
 //
 // The operands' 1 KB blocks are copied from global memory straight into a ring of S stages of CH chunks of K, each block by one
 // instruction, in the lane order in which the fragments are read (contiguous in both, no bank conflicts); a group of 4 chunks' scales
@@ -376,7 +379,8 @@ __global__ __launch_bounds__(64 * C::NW, C::WAVES_SIMD) void mx4_tile_kernel(Mx4
         if (FULL || j + 1 < chunks) {
             if constexpr (STAGE) {
                 // chunks up to j + (S - 1) CH are on their way or there; j + 1 to j + CH have to be
-                if (FULL || j + (S - 1) * CH < chunks) __builtin_amdgcn_s_waitcnt(waitcnt_imm(C::copies(I + 1 + CH, I + 1 + (S - 1) * CH), 0));
+                if (FULL || j + (S - 1) * CH < chunks)
+                    __builtin_amdgcn_s_waitcnt(waitcnt_imm(C::copies(I + 1 + CH, I + 1 + (S - 1) * CH), 0));
                 else __builtin_amdgcn_s_waitcnt(waitcnt_imm(0, 0));
                 barrier();
             }
@@ -399,7 +403,8 @@ __global__ __launch_bounds__(64 * C::NW, C::WAVES_SIMD) void mx4_tile_kernel(Mx4
 #pragma unroll
                     for (int d = q * ACTS / NM; d < (q + 1) * ACTS / NM; ++d) {
                         if (d < H) lo[d] = *reinterpret_cast<const u32x4 *>(next + (wm * FM + d) * 1024);
-                        else if (d < READS) w[(I + 1) % 2][d - H] = *reinterpret_cast<const u32x4 *>(next + (C::TA + wn * FN + d - H) * 1024);
+                        else if (d < READS)
+                            w[(I + 1) % 2][d - H] = *reinterpret_cast<const u32x4 *>(next + (C::TA + wn * FN + d - H) * 1024);
                         else copy_nth(std::integral_constant<int, I0>{}, j + 1 + (S - 1) * CH, d - READS);
                         __builtin_amdgcn_sched_barrier(0);
                     }
@@ -506,14 +511,18 @@ int64_t tiles_of(int M, int N, int side) { return (int64_t)((M + side - 1) / sid
 
 }  // namespace
 
-// More rows: the largest tile whose workgroups fill the chip, 32 x 32 with the waves along K where even 64 x 64 do not.  us, 32 / 64 / 128 /
-// 256 tiles (M x N x K):
+// More rows: the largest tile whose workgroups fill the chip, 32 x 32 with the waves along K where even 64 x 64 do not.  us, 32 / 64 /
+// 128 / 256 tiles (M x N x K), with a bias alone:
 //    64 x  4096 x 4096   4.5  8.8 12.1            201 x  4096 x 4096  12.2  7.7 10.0
 //   201 x  1024 x 4096   4.5  7.4  9.8            512 x  4096 x 4096  16.8  9.9 10.5
 //   128 x  8192 x 2048   7.7  5.9  7.4           1000 x  4096 x 4096  28.2 19.6 13.3
 //  4096 x  4096 x 4096             42.2 37.1     2048 x  8192 x 2048             27.4 24.2
+// The rule does not look at how much of a tile the rows fill: a few dozen of them by a vocabulary go to 256 x 256 tiles as well, where
+// 128 x 128 would be faster (48 x 131072 x 4096 in 64 / 128 / 256 tiles 62 57 83, 128 x 131072 x 4096 111 66 82, 48 x 65536 x 2048
+// 17 16 23; but 200 x 65536 x 4096 75 43 38).
 // An output of more than 32 MiB goes past the last cache, which the operands need (with quantisation, us, without / with the hint):
-//   8192 x 16384 x 2048 274 233     4096 x 4096 x 4096, fp32 residual 83 74     8192 x 8192 x 8192 285 278     4096 x 4096 x 4096 bf16 45.6 46.2
+//   8192 x 16384 x 2048, GELU 274 233     4096 x 4096 x 4096, fp32 residual 83 74
+//   8192 x 8192 x 8192 285 278            4096 x 4096 x 4096 bf16 45.6 46.2
 hipError_t launch_mx4_gemm(Epi epi, const void *a, const void *w, const bf16_t *bias, const float *resid, void *out, int M,
                            int N, int K, hipStream_t stream) {
     const Mx4Params p{static_cast<const char *>(a), static_cast<const char *>(w), nullptr, bias, resid, out, M, N, K, 0, epi};

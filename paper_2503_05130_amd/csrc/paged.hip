@@ -348,6 +348,8 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(PagedCache c, co
 // Bound by reading the pages once: 64 requests of 4000 - 8192 keys, 32 / 8 heads of 128, 250 us with the joining kernel (6.1
 // TB/s, what a plain read reaches), in 8 bits 134 us; one request of 32001 keys 26 us (5.0 TB/s); 96 of 5 - 12000, 16 / 4 heads
 // of 64 in 8 bits, 22 us (3.3 TB/s: 784 workgroups in one round, whose longest have 4 steps in a row, and 4 us of joining).
+// Changed scores cost little: the 64 requests capped, and lowered as well, 262 us in calls from a graph, 259 as they are, in 8 bits 139 and
+// 137 (heads of 128 in bf16 need 135 registers then in place of 124, and a SIMD holds 3 waves).
 // Each 16 query heads of a key-value head read the pages for themselves: 64 x 6000 keys with 40 / 2 heads of 128 take 141 us, with
 // 32 / 2 (one tile) 74; 64 / 1 145, 16 / 1 41.
 // Not kept: K of the next step requested before this step's V is used, and 2 or 4 steps at once (249 registers and 18% slower

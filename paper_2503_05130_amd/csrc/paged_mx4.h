@@ -53,7 +53,8 @@ __global__ __launch_bounds__(kTileThreads) void paged_append_mx4_kernel(PagedCac
     const int64_t slot = slots[at.token];
     const int col = at.head * DH + 8 * at.eighth;
     Eight x[2] = {};
-    const u32x4 *kp = reinterpret_cast<const u32x4 *>(k + at.token * k_stride + col), *vp = reinterpret_cast<const u32x4 *>(v + at.token * v_stride + col);
+    const u32x4 *kp = reinterpret_cast<const u32x4 *>(k + at.token * k_stride + col);
+    const u32x4 *vp = reinterpret_cast<const u32x4 *>(v + at.token * v_stride + col);
     x[0].lo = FAR ? __builtin_nontemporal_load(kp) : *kp;
     x[1].lo = FAR ? __builtin_nontemporal_load(vp) : *vp;
     if (slot < 0 || slot >= (int64_t)c.n_pages << c.page_log2) return;
@@ -68,7 +69,8 @@ __global__ __launch_bounds__(kTileThreads) void paged_append_mx4_kernel(PagedCac
     }
 }
 
-// 8 columns of K (of V) of a place as bf16.
+// 8 columns of K (of V) of a place as bf16.  V of the 16- and 8-bit caches comes in single elements, which lie 4 apart: 26000 tokens of
+// 8 x 128 are read back in 58 and 55 us (3.7 and 2.9 TB/s), in 80 and 55 where the slots are in any order; 4-bit ones in 20 and 22.
 template <int DH, KvKind KIND>
 __device__ inline u32x4 read_eight(const PagedCache &c, bool is_v, size_t part, int page, int place, int eighth, int head) {
     const char *src = static_cast<const char *>(is_v ? c.v : c.k);
@@ -145,11 +147,13 @@ __global__ __launch_bounds__(kTileThreads) void paged_read_kernel(PagedCache c, 
 // scores of a step.  The probabilities go through 1 KB of LDS to the lanes that need them as an operand of O^T = V^T P^T, as bf16 and its
 // bf16 rest (see paged.hip).  V becomes bf16 on the way, by v_cvt_scalef32_pk_bf16_fp4 under the scale as it is stored.
 //
-// Bound by the pages' bytes, and next by the vector instructions that turn V into bf16 and the scores into probabilities: 64 requests of 4000 to 8192
-// keys, 32 / 8 heads of 128, 408 MB, take 86 us with capped scores (4.7 TB/s, 51% of the issue slots) and 4.3 for the joining (the call 91 - 101, 93 - 95 without a cap); one of 300 keys 6.6,
-// a chain of loads (length, table, page) and the joining of 8 waves.  Not kept: every lane working on all scores of its heads (103 and 115 us);
-// steps of 32 keys; the next step's loads asked for ahead, or the
-// first one's before q is converted, whose registers spill (137 us uncapped) or halve the waves.
+// 64 requests of 4000 to 8192 keys, 32 / 8 heads of 128, 408 MB, take 87 us with capped scores (4.7 TB/s, 51% of the issue slots) and
+// 4.3 to 5.2 for the joining; calls from a graph 93, with slopes as well 96, with neither 88; 56 / 8 heads 110, 115 and 92.  Neither the
+// memory nor the issue is full: a step waits for its own pages, with nothing of the next one on its way.  One request of 300 keys
+// takes 6.7, a chain of loads (length, table, page) and the joining of 8 waves.  Not kept: every lane working on all scores of its
+// heads (103 and 115 us); steps of 32 keys; the next step's loads asked for ahead, or the first one's before q is converted, whose
+// registers spill (137 us uncapped) or halve the waves.  (Copies of the next step straight to LDS, which take no registers, have not
+// been tried.)
 //
 // The reference of the exponents need not be the largest score: it is raised, and sums and context scaled down, when a score
 // exceeds it by 2^8, which in a row of many keys is rare; probabilities up to 2^8 are as exact as those up to 1.
@@ -214,8 +218,8 @@ __device__ inline Q8 q8_operand(const Q16<DH> &q16, int r, int c) {
     return q;
 }
 
-// Columns 2 m and 2 m + 1 of the lane's W of token e of a quad, as bf16.  The conversion reads of its scale the exponent field alone, whatever
-// the other bits: a shift puts the token's byte there.
+// Columns 2 m and 2 m + 1 of the lane's W of token e of a quad, as bf16.  The conversion reads of its scale the exponent field alone,
+// whatever the other bits: a shift puts the token's byte there.
 template <int W>
 __device__ inline uint32_t v_pair(uint32_t codes, uint32_t scales, int e, int m, int r) {
     const float s = __uint_as_float(e == 3 ? scales >> 1 : scales << (23 - 8 * e));
@@ -298,8 +302,8 @@ __global__ __launch_bounds__(64 * WAVES, HC < 16 ? 4 : WAVES == 8 ? 2 : 3) void 
         const int k0 = it.part << part_log2, k1 = min(it.keys, k0 + (1 << part_log2));
         const int32_t *ids = a.table + (size_t)it.b * a.table_stride;
         const Q16<DH> q16(a.q + (int64_t)it.b * a.q_stride + (head0 + min(r % HC, n_heads - 1)) * DH, c);
-        // the heads' slopes wait behind the wave's probabilities: in four registers they made others spill, also where there is but a cap
-        // (64 x 4000 - 8192 capped 105 us, now 101; capped and lowered 108, now 104)
+        // the heads' slopes wait behind the wave's probabilities: in four registers they made more of the others spill, also where there is
+        // but a cap (2 to 3 registers do now, with 5 to 8 heads of 128 eight)
         if constexpr (SCORED) {
             if (a.slopes && lane < HC) p_lds[lane][16 * T] = __float_as_uint(slope_log2e(a.slopes[head0 + min(lane, n_heads - 1)]));
             wave_lds_fence();
@@ -431,8 +435,9 @@ __global__ __launch_bounds__(64 * WAVES, HC < 16 ? 4 : WAVES == 8 ? 2 : 3) void 
                 const u32x4 pa = *reinterpret_cast<const u32x4 *>(&p_lds[r % HC][32 * g + 4 * c]);
                 const u32x4 pb = *reinterpret_cast<const u32x4 *>(&p_lds[r % HC][32 * g + 16 + 4 * c]);
                 auto halves = [&](uint32_t pick) {
-                    return __builtin_bit_cast(bf16x8, u32x4{__builtin_amdgcn_perm(pa[1], pa[0], pick), __builtin_amdgcn_perm(pa[3], pa[2], pick),
-                                                            __builtin_amdgcn_perm(pb[1], pb[0], pick), __builtin_amdgcn_perm(pb[3], pb[2], pick)});
+                    return __builtin_bit_cast(
+                        bf16x8, u32x4{__builtin_amdgcn_perm(pa[1], pa[0], pick), __builtin_amdgcn_perm(pa[3], pa[2], pick),
+                                      __builtin_amdgcn_perm(pb[1], pb[0], pick), __builtin_amdgcn_perm(pb[3], pb[2], pick)});
                 };
                 const bf16x8 p_hi = halves(0x07060302u), p_lo = halves(0x05040100u);
                 // a byte holds two columns of one token: the pairs of tokens that the operand wants come of two bytes
@@ -541,8 +546,8 @@ hipError_t in_grids(const PagedCache &c, int tokens, Launch launch) {
     return e;
 }
 
-// Of the tokens' keys and values in bf16.  From 64 MiB on new ones are read, from 32 MiB on read ones written past the last cache: append and
-// read of tokens of 8 x 128, us, without a hint / stores / both:
+// Of the tokens' keys and values in bf16.  From 64 MiB on new ones are read, from 32 MiB on read ones written past the last cache:
+// append and read of tokens of 8 x 128, us, without a hint / stores / both:
 //   2000  7.7  7.4  7.0     4000 10.9  9.8  9.8     8000 18.7 16.8 17.9     16000 41.2 33.3 33.7     24001 and 26000 62.2 53.3 49.4
 int64_t bytes_of(const PagedCache &c, int tokens) { return (int64_t)tokens * c.kv_heads * c.head_dim * 4; }
 

@@ -40,6 +40,7 @@ inline __host__ __device__ int log2_up(int n) { return n <= 1 ? 0 : 32 - __built
 // rows, 4 up to 2047 and 2 from there (us; 32 / 8 heads of 128 unless stated):
 //   parts of up to 512, 1024, 2048, 4096, 8192 keys: 64 x 4000 - 8192  102 92 92 95 88     256 x 800 - 1600  89 88 74 75 73
 //     96 x 5 - 12000, 16 / 4 heads of 64  23 22 25 33 45     16 x 600 - 1200, 12 heads of 64  12.2 12.6 10.6 10.6 10.6
+// (1024 would serve that ragged batch better and cost others more; the rule knows neither the lengths nor how evenly parts fill the chip.)
 //   8 / 4 waves: 64 x 4000 - 8192  95 / 92     64 x 2000 - 4096, 16 / 16 heads  95 / 93     1 x 32001  14.9 / 15.8
 //     64 x 2000 - 8192, 16 / 1 heads  20 / 23     256 x 800 - 1600 with 8 / 2 waves  88 / 79
 inline __host__ __device__ PagedSplit paged_split(int batch, int n_heads, int n_kv_heads, bool mx4 = false) {

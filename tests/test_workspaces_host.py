@@ -5,7 +5,8 @@ import pytest
 
 import paper_2503_05130_amd as ie
 
-ROWS = [1, 2, 3, 7, 31, 32, 33, 48, 64, 65, 100, 127, 128, 200, 256, 300, 512, 600, 682, 683, 1000, 1024, 1025, 2000, 2048, 2049, 4096, 5000]
+ROWS = [1, 2, 3, 7, 31, 32, 33, 48, 64, 65, 100, 127, 128, 200, 256, 300, 512, 600, 682, 683, 1000, 1024, 1025, 2000, 2048, 2049, 4096,
+        5000]
 
 
 def _logprobs_bytes(rows, vocab, n):
